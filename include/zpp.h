@@ -375,6 +375,145 @@ ZPP_API zpp_status zpp_qgz_receive_step_refresh_quantize_interleaved(
     uint32_t block, const zpp_adam_hparams *hp, hipStream_t stream, const hipEvent_t *wait_events,
     uint32_t num_wait, hipEvent_t done_after);
 
+/* ------------------------------------------------------------------------
+ * Layer operators: what a layer's forward and backward pass (Algorithm 1,
+ * L_i.forward() and L_i.backward()) keeps and uses of its activations.  ZeRO
+ * shards the weights, gradients and optimizer states over the ranks; what a
+ * GPU holds whole are the activations saved for the backward pass.  These
+ * calls save them in 8 bits and run the backward pass from the 8 bits.
+ *
+ * Operands are matrices of `rows` tokens by `cols` features.  A row's
+ * elements are consecutive; rows lie `stride` elements apart (stride >= cols
+ * where rows > 1), so that an operand may be a column range of a wider matrix.
+ * The conventions at the head of this file hold: device pointers, element
+ * alignment, validation before anything is enqueued (ZPP_EINVAL, ZPP_EALIGN),
+ * events.  No output may share an element with another argument
+ * (ZPP_EOVERLAP); column ranges of one wider matrix are apart.
+ * Sums, statistics and gradients of weights are held in fp32; bf16 results
+ * are rounded once, to nearest even.  Every call gives the same bits each
+ * time it is run.
+ * ------------------------------------------------------------------------ */
+
+/* Element types of a matrix. */
+typedef enum {
+    ZPP_BF16 = 0, /* uint16_t bit patterns */
+    ZPP_F32 = 1,  /* float */
+    ZPP_I8 = 2    /* an activation checkpoint in 8 bits */
+} zpp_type;
+
+/* A matrix in device memory, described at call time.  ZPP_I8: `data` are the
+ * int8_t codes and `exps` the scale exponents, uint8_t[rows][ceil(cols/64)]
+ * without gaps; exps is ignored for the other types.
+ *
+ * A checkpoint's row is cut into blocks of 64 consecutive elements (the last
+ * may be shorter), each with one power of two as its scale:
+ *   block holds an Inf or NaN -> exp = 255, codes 0; every element reads as NaN
+ *   otherwise e is the smallest integer >= -126 with max |x| <= 127 * 2^e,
+ *       exp = e + 127, code = rint(x * 2^-e) (ties to even), and an element
+ *       reads as code * 2^e.  (|code| is kept to 63 where e = 122, the largest
+ *       e there is, so that what is read is finite.)
+ * An element is off by at most 2^e / 2 <= max |x| / 127 (2^-127 below that).
+ * The scale being a power of two, code * 2^e has 7 significant bits: it is a
+ * bf16 number, and no product of the backward pass rounds it again.  1 + 1/64
+ * bytes an element. */
+typedef struct {
+    void *data;
+    uint8_t *exps;
+    size_t stride;
+    int32_t type;
+} zpp_matrix;
+
+/* Saves x (ZPP_BF16 or ZPP_F32) as a checkpoint (`saved`, ZPP_I8), and reads
+ * one back into `out` (ZPP_BF16 or ZPP_F32; both hold the value exactly). */
+ZPP_API zpp_status zpp_checkpoint_save(const zpp_matrix *x, const zpp_matrix *saved, size_t rows,
+                                       size_t cols, hipStream_t stream, hipEvent_t wait_before,
+                                       hipEvent_t done_after);
+ZPP_API zpp_status zpp_checkpoint_load(const zpp_matrix *saved, const zpp_matrix *out, size_t rows,
+                                       size_t cols, hipStream_t stream, hipEvent_t wait_before,
+                                       hipEvent_t done_after);
+
+/* Layer norm of every row, in fp32:
+ *     s = x, or with `residual` s = x + residual rounded to the matrices' type
+ *     mean = sum s / cols;  rstd = 1 / sqrt(sum (s - mean)^2 / cols + eps)
+ *     y = (s - mean) * rstd * gamma + beta
+ * x, residual, y, total: the same type, ZPP_BF16 or ZPP_F32.  residual and
+ *   total are given together or are both NULL; total = s, the residual stream.
+ * gamma, beta: [cols] of param_type (ZPP_BF16 or ZPP_F32); beta may be NULL.
+ * mean, rstd: float[rows] out, for the backward pass; either may be NULL.
+ * saved: NULL, or the checkpoint (ZPP_I8) of s, written in the same pass.
+ * eps: finite, >= 0. */
+ZPP_API zpp_status zpp_layer_norm_forward(const zpp_matrix *x, const zpp_matrix *residual,
+                                          const void *gamma, const void *beta, int32_t param_type,
+                                          size_t rows, size_t cols, float eps, const zpp_matrix *y,
+                                          const zpp_matrix *total, const zpp_matrix *saved,
+                                          float *mean, float *rstd, hipStream_t stream,
+                                          hipEvent_t wait_before, hipEvent_t done_after);
+
+/* Bytes of workspace of zpp_layer_norm_backward of this size. */
+ZPP_API size_t zpp_layer_norm_backward_workspace(size_t rows, size_t cols);
+
+/* Layer norm's backward pass, in fp32, with h = (x - mean) * rstd:
+ *     g = dy * gamma
+ *     dx = rstd * (g - sum(g) / cols - h * sum(g h) / cols) (+ dresidual)
+ *     dgamma (+)= sum over rows dy h;  dbeta (+)= sum over rows dy
+ * dy, dresidual, dx, y: the same type, ZPP_BF16 or ZPP_F32.
+ * x: what the forward pass normalised (its `total` where it added a residual):
+ *   that type, or the checkpoint (ZPP_I8).  mean, rstd: float[rows], the
+ *   forward pass's.
+ * dresidual: NULL, or the gradient that reaches x past the norm.
+ * y: NULL, or the forward pass's output computed again from x (the input of
+ *   the next linear layer, whose weight gradient needs it); beta (NULL: none)
+ *   is used for it alone.
+ * dgamma, dbeta: float[cols], either may be NULL; added to where `accumulate`,
+ *   otherwise written (with rows == 0: zeros).
+ * workspace: zpp_layer_norm_backward_workspace(rows, cols) bytes at 16-byte
+ *   alignment, of undefined contents; it is this call's until the call's work
+ *   on `stream` has finished. */
+ZPP_API zpp_status zpp_layer_norm_backward(const zpp_matrix *dy, const zpp_matrix *x,
+                                           const void *gamma, const void *beta, int32_t param_type,
+                                           const float *mean, const float *rstd,
+                                           const zpp_matrix *dresidual, size_t rows, size_t cols,
+                                           const zpp_matrix *dx, const zpp_matrix *y,
+                                           float *dgamma, float *dbeta, int32_t accumulate,
+                                           void *workspace, size_t workspace_bytes,
+                                           hipStream_t stream, hipEvent_t wait_before,
+                                           hipEvent_t done_after);
+
+/* GELU, a = u P(u), P the distribution function of the normal distribution
+ * (the exact form, not tanh's), and its backward pass
+ *     du = da * (P(u) + u p(u)),  p the density.
+ * At -Inf they take their limits (0), at NaN they are NaN.
+ * u, a, da, du: the same type, ZPP_BF16 or ZPP_F32.
+ * saved: NULL, or the checkpoint (ZPP_I8) of u, written in the same pass.
+ * Backward, u: that type, or the checkpoint; a: NULL, or the forward pass's
+ *   output computed again from u (the input of the next linear layer). */
+ZPP_API zpp_status zpp_gelu_forward(const zpp_matrix *u, size_t rows, size_t cols,
+                                    const zpp_matrix *a, const zpp_matrix *saved,
+                                    hipStream_t stream, hipEvent_t wait_before,
+                                    hipEvent_t done_after);
+ZPP_API zpp_status zpp_gelu_backward(const zpp_matrix *da, const zpp_matrix *u, size_t rows,
+                                     size_t cols, const zpp_matrix *du, const zpp_matrix *a,
+                                     hipStream_t stream, hipEvent_t wait_before,
+                                     hipEvent_t done_after);
+
+/* Bytes of workspace of zpp_weight_grad of this size (0: none needed). */
+ZPP_API size_t zpp_weight_grad_workspace(size_t rows, size_t n, size_t k);
+
+/* A linear layer's weight gradient (y = x W^T, W [n][k]):
+ *     dw[i][j] (+)= sum over rows t of dy[t][i] * x[t][j]
+ * dy: [rows][n], ZPP_BF16.  x: [rows][k], ZPP_BF16 or a checkpoint (ZPP_I8),
+ *   whose elements enter the matrix cores as the bf16 numbers that they are.
+ * dw: [n][k], ZPP_F32, the gradient that the partition step and the qgZ
+ *   quantizers take; added to where `accumulate`, otherwise written (with
+ *   rows == 0: zeros).  Sums in fp32.
+ * workspace: zpp_weight_grad_workspace(rows, n, k) bytes at 16-byte alignment,
+ *   as for zpp_layer_norm_backward; may be NULL where that is 0.
+ * rows, n, k < 2^31. */
+ZPP_API zpp_status zpp_weight_grad(const zpp_matrix *dy, const zpp_matrix *x, size_t rows,
+                                   size_t n, size_t k, const zpp_matrix *dw, int32_t accumulate,
+                                   void *workspace, size_t workspace_bytes, hipStream_t stream,
+                                   hipEvent_t wait_before, hipEvent_t done_after);
+
 /* Static, NUL-terminated description of a status code.  Takes any int, so
  * that a caller may pass whatever status value it holds: a value that is not
  * one of zpp_status gives "unknown status". */

@@ -20,7 +20,8 @@ MARSHAL_LIB = os.path.join(PKG, "_marshal.so")
 MARSHAL_SOURCE = "marshal.cpp"
 
 SOURCES = ["zpp_api.hip", "adam.hip", "refresh.hip", "quant.hip", "gather.hip", "fused.hip",
-           "qgz.hip", "receive_adam.hip"]
+           "qgz.hip", "receive_adam.hip", "layer_api.hip", "activations.hip", "layer_norm.hip",
+           "weight_grad.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

@@ -118,7 +118,107 @@ PyObject *address_array(PyObject *, PyObject *const *args, Py_ssize_t n) {
     }
 }
 
+// A matrix argument as the C ABI takes it (zpp_matrix in zpp.h).
+struct Matrix {
+    void *data;
+    void *exps;
+    size_t stride;
+    int32_t type;
+};
+
+// Element type of a matrix (zpp_type), or -1.
+int matrix_type(at::ScalarType t) {
+    switch (t) {
+    case at::kBFloat16:
+    case at::kShort:
+    case at::kUInt16: return 0;
+    case at::kFloat: return 1;
+    case at::kChar: return 2;
+    default: return -1;
+    }
+}
+
+// A [rows, cols] tensor of device `device`, its rows' elements consecutive.
+bool matrix_tensor(PyObject *o, long device, long long rows, long long cols, Matrix *out) {
+    if (!THPVariable_CheckExact(o))
+        return false;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || t.device().index() != device || t.dim() != 2 || t.size(0) != rows ||
+        t.size(1) != cols || (cols > 1 && t.stride(1) != 1))
+        return false;
+    out->data = t.data_ptr();
+    out->exps = nullptr;
+    out->stride = (size_t)t.stride(0);
+    out->type = matrix_type(t.scalar_type());
+    return out->type >= 0;
+}
+
+// matrices(device, block, (object, mask, rows, cols)...): for each object the
+// bytes of its zpp_matrix (None for an optional one that is not given), or
+// None.  An object is a tensor, or a checkpoint's pair of codes and exponents;
+// mask: the zpp_types it may have, as bits (8: None may stand in its place).
+PyObject *matrices(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    if (n < 2 || (n - 2) % 4) {
+        PyErr_SetString(PyExc_TypeError, "matrices(device, block, (object, mask, rows, cols)...)");
+        return nullptr;
+    }
+    const long device = PyLong_AsLong(args[0]);
+    const long long block = PyLong_AsLongLong(args[1]);
+    const Py_ssize_t count = (n - 2) / 4;
+    PyObject *result = PyTuple_New(count);
+    if (!result)
+        return nullptr;
+    bool good = !PyErr_Occurred() && block > 0;
+    try {
+        for (Py_ssize_t i = 0; good && i < count; ++i) {
+            PyObject *const *a = args + 2 + 4 * i;
+            const unsigned mask = (unsigned)PyLong_AsUnsignedLong(a[1]);
+            const long long rows = PyLong_AsLongLong(a[2]), cols = PyLong_AsLongLong(a[3]);
+            PyObject *value = Py_None;
+            Matrix m = {nullptr, nullptr, 0, 0};
+            if (PyErr_Occurred()) {
+                good = false;
+            } else if (a[0] == Py_None && (mask & 8)) {
+                Py_INCREF(value);
+            } else {
+                PyObject *data = a[0];
+                if (PyTuple_CheckExact(data) && PyTuple_GET_SIZE(data) == 2) {
+                    PyObject *exps = PyTuple_GET_ITEM(a[0], 1);
+                    data = PyTuple_GET_ITEM(a[0], 0);
+                    void *p = nullptr;
+                    const long long blocks = (cols + block - 1) / block;
+                    good = matrix_tensor(data, device, rows, cols, &m) && m.type == 2 &&
+                           address(exps, device, kU8, rows * blocks, &p);
+                    m.exps = p;
+                } else {
+                    good = matrix_tensor(data, device, rows, cols, &m) && m.type != 2;
+                }
+                good = good && ((mask >> m.type) & 1u);
+                if (!good)
+                    break;
+                value = PyBytes_FromStringAndSize(reinterpret_cast<const char *>(&m),
+                                                  (Py_ssize_t)sizeof(m));
+                if (!value) {
+                    Py_DECREF(result);
+                    return nullptr;
+                }
+            }
+            if (good)
+                PyTuple_SET_ITEM(result, i, value);
+        }
+    } catch (const std::exception &) {
+        good = false;
+    }
+    if (good)
+        return result;
+    Py_DECREF(result);
+    PyErr_Clear();
+    Py_RETURN_NONE;
+}
+
 PyMethodDef methods[] = {
+    {"matrices", (PyCFunction)(void (*)(void))matrices, METH_FASTCALL,
+     "matrices(device, block, object, mask, rows, cols, ...) -> tuple or None"},
     {"addresses", (PyCFunction)(void (*)(void))addresses, METH_FASTCALL,
      "addresses(device, tensor, mask, need, ...) -> tuple or None"},
     {"address_array", (PyCFunction)(void (*)(void))address_array, METH_FASTCALL,

@@ -1,0 +1,259 @@
+// Device-side pieces of the layer operators: eight consecutive elements of a
+// row as a lane's share (bf16, fp32 or a checkpoint's codes), the decisions of
+// the 8-bit checkpoint, and sums over lanes.
+#pragma once
+
+#include "zpp_device.h"
+#include "zpp_layer.h"
+#include "zpp_quant.h"
+
+namespace zpp {
+
+// Eight elements as they are loaded; turned to fp32 only where they are used,
+// so that loads in flight hold 4 (bf16), 8 (fp32) or 3 (codes) registers.
+template <int TYPE>
+struct Chunk;
+template <>
+struct Chunk<kBf16> {
+    u32x4 w;
+};
+template <>
+struct Chunk<kF32> {
+    f32x4 lo, hi;
+};
+template <>
+struct Chunk<kI8> {
+    u32x2 codes;
+    uint32_t exp;
+};
+
+template <class E>
+__device__ __forceinline__ const E *at(const Mat &m, size_t row, uint32_t col) {
+    return reinterpret_cast<const E *>(m.data) + row * m.stride + col;
+}
+template <class E>
+__device__ __forceinline__ E *out_at(const Mat &m, size_t row, uint32_t col) {
+    return reinterpret_cast<E *>(m.data) + row * m.stride + col;
+}
+
+// Elements col .. col+7 of a row with `valid` >= 1 of them inside it (those
+// past them read as the row's last).  A row's last, partial chunk takes single
+// loads at clamped columns, which do not wait for each other; RAGGED false:
+// there is none, `valid` is 8.
+template <int TYPE, bool RAGGED = true>
+__device__ __forceinline__ Chunk<TYPE> load_chunk(const Mat &m, size_t row, uint32_t col,
+                                                  uint32_t valid, uint32_t blocks) {
+    Chunk<TYPE> c;
+    if constexpr (TYPE == kBf16) {
+        const uint16_t *p = at<uint16_t>(m, row, col);
+        if (!RAGGED || valid >= 8) {
+            c.w = ld_nt_at<u32x4, 2>(p);
+        } else {
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e)
+                c.w[e] = (uint32_t)p[clamped(2 * e, valid)] |
+                         ((uint32_t)p[clamped(2 * e + 1, valid)] << 16);
+        }
+    } else if constexpr (TYPE == kF32) {
+        const float *p = at<float>(m, row, col);
+        if (!RAGGED || valid >= 8) {
+            c.lo = ld_nt_at<f32x4, 4>(p);
+            c.hi = ld_nt_at<f32x4, 4>(p + 4);
+        } else {
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e) {
+                c.lo[e] = p[clamped(e, valid)];
+                c.hi[e] = p[clamped(e + 4, valid)];
+            }
+        }
+    } else {
+        const uint8_t *p = at<uint8_t>(m, row, col);
+        if (!RAGGED || valid >= 8) {
+            c.codes = ld_nt_at<u32x2, 1>(p);
+        } else {
+            c.codes = u32x2{0, 0};
+#pragma unroll
+            for (uint32_t e = 0; e < 8; ++e)
+                c.codes[e / 4] |= (uint32_t)p[clamped(e, valid)] << (8 * (e % 4));
+        }
+        c.exp = m.exps[row * blocks + col / kActBlock];
+    }
+    return c;
+}
+
+// The scale of a checkpoint's block.
+__device__ __forceinline__ float act_scale(uint32_t exp) {
+    return __uint_as_float(exp == 255u ? kScaleNaNBits : exp << 23);
+}
+
+__device__ __forceinline__ void chunk_values(const Chunk<kBf16> &c, float (&x)[8]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[2 * e] = bf16_lo(c.w[e]);
+        x[2 * e + 1] = bf16_hi(c.w[e]);
+    }
+}
+__device__ __forceinline__ void chunk_values(const Chunk<kF32> &c, float (&x)[8]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[e] = c.lo[e];
+        x[e + 4] = c.hi[e];
+    }
+}
+__device__ __forceinline__ void chunk_values(const Chunk<kI8> &c, float (&x)[8]) {
+    const float s = act_scale(c.exp);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        x[e] = (float)(int8_t)(c.codes[e / 4] >> (8 * (e % 4))) * s;
+}
+
+// Two floats as packed bf16, to nearest even (NaN stays NaN).
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+    const bf16x2 v = __builtin_convertvector((f32x2){lo, hi}, bf16x2);
+    return __builtin_bit_cast(uint32_t, v);
+}
+
+template <int TYPE>
+__device__ __forceinline__ Chunk<TYPE> make_chunk(const float (&x)[8]) {
+    Chunk<TYPE> c;
+    if constexpr (TYPE == kBf16) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            c.w[e] = bf16_pair(x[2 * e], x[2 * e + 1]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            c.lo[e] = x[e];
+            c.hi[e] = x[e + 4];
+        }
+    }
+    return c;
+}
+
+// Stores the first `valid` >= 1 elements of the chunk.
+template <int TYPE, bool RAGGED = true>
+__device__ __forceinline__ void store_chunk(const Mat &m, size_t row, uint32_t col, uint32_t valid,
+                                            const Chunk<TYPE> &c) {
+    if constexpr (TYPE == kBf16) {
+        uint16_t *p = out_at<uint16_t>(m, row, col);
+        if (!RAGGED || valid >= 8) {
+            st_nt_at<u32x4, 2>(p, c.w);
+        } else {
+#pragma unroll
+            for (uint32_t e = 0; e < 8; ++e)
+                if (e < valid)
+                    p[e] = (uint16_t)(c.w[e / 2] >> (16 * (e % 2)));
+        }
+    } else {
+        float *p = out_at<float>(m, row, col);
+        if (!RAGGED || valid >= 8) {
+            st_nt_at<f32x4, 4>(p, c.lo);
+            st_nt_at<f32x4, 4>(p + 4, c.hi);
+        } else {
+#pragma unroll
+            for (uint32_t e = 0; e < 8; ++e)
+                if (e < valid)
+                    p[e] = e < 4 ? c.lo[e] : c.hi[e - 4];
+        }
+    }
+}
+
+// x moved by DPP; every lane has a source lane in these patterns.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, true);
+}
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+    return __uint_as_float(dpp<CTRL>(__float_as_uint(x)));
+}
+constexpr int kSwap1 = 0xB1;     // quad_perm 1,0,3,2
+constexpr int kSwap2 = 0x4E;     // quad_perm 2,3,0,1
+constexpr int kMirror8 = 0x141;  // the other half of 8 lanes, reversed
+constexpr int kMirror16 = 0x140; // the other half of 16 lanes, reversed
+
+// Sum of 16 neighbouring lanes, in all of them.
+__device__ __forceinline__ float sum16(float x) {
+    x += dpp<kSwap1>(x);
+    x += dpp<kSwap2>(x);
+    x += dpp<kMirror8>(x);
+    x += dpp<kMirror16>(x);
+    return x;
+}
+__device__ __forceinline__ float lane_value(float x, int lane) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), lane));
+}
+// Sum of the wave, the same in every lane.
+__device__ __forceinline__ float sum64(float x) {
+    x = sum16(x);
+    return (lane_value(x, 0) + lane_value(x, 16)) + (lane_value(x, 32) + lane_value(x, 48));
+}
+
+// The exponent byte of a block from the bits of its largest magnitude: the
+// smallest e with a <= 127 * 2^e.  127 = 1.984375 * 2^6, so with a = m 2^E, e
+// is E - 6 up to m = 1.984375 and E - 5 beyond, which adding the distance from
+// there to the next power of two makes a carry into the exponent field.  Inf
+// and NaN, whose bits are at least 0x7F800000, are 255.
+__device__ __forceinline__ uint32_t act_exp(uint32_t absbits) {
+    const int e = (int)((absbits + 0x1FFFFu) >> 23) - 6;
+    return absbits >= 0x7F800000u ? 255u : (uint32_t)(e < 1 ? 1 : e);
+}
+
+// A lane's share of a block's largest magnitude, as fp32 bits (whose order is
+// that of the magnitudes, NaN above Inf above all).
+__device__ __forceinline__ uint32_t max_bits(const float (&x)[8], uint32_t valid) {
+    uint32_t a = 0;
+#pragma unroll
+    for (uint32_t e = 0; e < 8; ++e) {
+        const uint32_t b = __float_as_uint(x[e]) & 0x7FFFFFFFu;
+        a = e < valid && b > a ? b : a;
+    }
+    return a;
+}
+// Largest of 8 neighbouring lanes' (one block's), in all of them.
+__device__ __forceinline__ uint32_t max8(uint32_t a) {
+    uint32_t b = dpp<kSwap1>(a);
+    a = a > b ? a : b;
+    b = dpp<kSwap2>(a);
+    a = a > b ? a : b;
+    b = dpp<kMirror8>(a);
+    return a > b ? a : b;
+}
+
+// Codes of eight elements of a block with this exponent byte.  x * 2^-e is
+// exact (its magnitude is at most 127, at e = 122 up to 64 and kept to 63),
+// and the addition of 1.5 * 2^23 rounds it to the integer as rint does.
+__device__ __forceinline__ u32x2 act_codes(const float (&x)[8], uint32_t exp) {
+    const float inv = __uint_as_float((exp == 255u ? 0u : 254u - exp) << 23);
+    const float most = exp >= 249u ? 63.0f : 127.0f;
+    uint32_t b[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        b[e] = code_bits(__builtin_amdgcn_fmed3f(x[e] * inv, -most, most));
+    const u32x2 w = {pack_low_bytes(b[0], b[1], b[2], b[3]), pack_low_bytes(b[4], b[5], b[6], b[7])};
+    return exp == 255u ? u32x2{0, 0} : w;
+}
+
+// Writes the checkpoint of the elements that the 8 lanes of a block hold.  All
+// 8 lanes take part, with `valid` 0 where a lane is past the row's end.
+template <bool RAGGED = true>
+__device__ __forceinline__ void save_chunk(const Mat &m, size_t row, uint32_t col, uint32_t valid,
+                                           uint32_t blocks, const float (&x)[8]) {
+    const uint32_t exp = act_exp(max8(max_bits(x, valid)));
+    if (valid) {
+        const u32x2 w = act_codes(x, exp);
+        uint8_t *p = out_at<uint8_t>(m, row, col);
+        if (!RAGGED || valid >= 8) {
+            st_nt_at<u32x2, 1>(p, w);
+        } else {
+#pragma unroll
+            for (uint32_t e = 0; e < 8; ++e)
+                if (e < valid)
+                    p[e] = (uint8_t)(w[e / 4] >> (8 * (e % 4)));
+        }
+        if ((col & (kActBlock - 1)) == 0)
+            m.exps[row * blocks + col / kActBlock] = (uint8_t)exp;
+    }
+}
+
+}  // namespace zpp

@@ -6,18 +6,15 @@
 #include <initializer_list>
 
 #include "zpp.h"
+#include "zpp_abi.h"
 #include "zpp_launch.h"
 
 namespace {
 
-thread_local int g_last_hip_error = 0;
-
-zpp_status hip_fail(hipError_t e) {
-    g_last_hip_error = (int)e;
-    return ZPP_EHIP;
-}
-
-bool aligned(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
+using zpp::aligned;
+using zpp::hip_fail;
+using zpp::record;
+using zpp::wait_on;
 
 // Whether every array (NULL: not asked for) starts at a multiple of `line`
 // bytes.  Which outputs have to, for a launch's workgroups to keep the plain
@@ -103,13 +100,6 @@ zpp::AdamConsts adam_consts(const zpp_adam_hparams &hp) {
     return c;
 }
 
-zpp_status wait_on(hipStream_t stream, hipEvent_t ev) {
-    if (!ev)
-        return ZPP_OK;
-    const hipError_t e = hipStreamWaitEvent(stream, ev, 0);
-    return e == hipSuccess ? ZPP_OK : hip_fail(e);
-}
-
 // Bytes of codes and count of scales of an interleaved receive buffer of
 // num_src int4 copies of n elements in blocks of `block`.
 size_t il_code_bytes(size_t n, uint32_t block, uint32_t num_src) {
@@ -117,13 +107,6 @@ size_t il_code_bytes(size_t n, uint32_t block, uint32_t num_src) {
 }
 size_t il_scale_count(size_t n, uint32_t block, uint32_t num_src) {
     return (n + block - 1) / block * num_src;
-}
-
-zpp_status record(hipStream_t stream, hipEvent_t ev) {
-    if (!ev)
-        return ZPP_OK;
-    const hipError_t e = hipEventRecord(ev, stream);
-    return e == hipSuccess ? ZPP_OK : hip_fail(e);
 }
 
 }  // namespace
@@ -741,6 +724,6 @@ ZPP_API const char *zpp_status_string(int status) {
     return "unknown status";
 }
 
-ZPP_API int zpp_last_hip_error(void) { return g_last_hip_error; }
+ZPP_API int zpp_last_hip_error(void) { return zpp::g_last_hip_error; }
 
 }  // extern "C"

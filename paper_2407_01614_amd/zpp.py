@@ -80,6 +80,28 @@ _lib.zpp_qgz_receive_step_refresh_quantize_interleaved.restype = ctypes.c_int
 _lib.zpp_qgz_receive_step_refresh_quantize_interleaved.argtypes = [
     _P, _P, _P, _P, _P, _u32, _u32, ctypes.c_float, _P, _P, _P, _P, _sz, _u32,
     ctypes.POINTER(AdamHParams), _P, _P, _u32, _P]
+_mat = _P  # a zpp_matrix, as the bytes that _matrices makes of a tensor
+_i32 = ctypes.c_int32
+_lib.zpp_checkpoint_save.restype = ctypes.c_int
+_lib.zpp_checkpoint_save.argtypes = [_mat, _mat, _sz, _sz, _P, _P, _P]
+_lib.zpp_checkpoint_load.restype = ctypes.c_int
+_lib.zpp_checkpoint_load.argtypes = [_mat, _mat, _sz, _sz, _P, _P, _P]
+_lib.zpp_layer_norm_forward.restype = ctypes.c_int
+_lib.zpp_layer_norm_forward.argtypes = [_mat, _mat, _P, _P, _i32, _sz, _sz, ctypes.c_float, _mat,
+                                        _mat, _mat, _P, _P, _P, _P, _P]
+_lib.zpp_layer_norm_backward_workspace.restype = _sz
+_lib.zpp_layer_norm_backward_workspace.argtypes = [_sz, _sz]
+_lib.zpp_layer_norm_backward.restype = ctypes.c_int
+_lib.zpp_layer_norm_backward.argtypes = [_mat, _mat, _P, _P, _i32, _P, _P, _mat, _sz, _sz, _mat,
+                                         _mat, _P, _P, _i32, _P, _sz, _P, _P, _P]
+_lib.zpp_gelu_forward.restype = ctypes.c_int
+_lib.zpp_gelu_forward.argtypes = [_mat, _sz, _sz, _mat, _mat, _P, _P, _P]
+_lib.zpp_gelu_backward.restype = ctypes.c_int
+_lib.zpp_gelu_backward.argtypes = [_mat, _mat, _sz, _sz, _mat, _mat, _P, _P, _P]
+_lib.zpp_weight_grad_workspace.restype = _sz
+_lib.zpp_weight_grad_workspace.argtypes = [_sz, _sz, _sz]
+_lib.zpp_weight_grad.restype = ctypes.c_int
+_lib.zpp_weight_grad.argtypes = [_mat, _mat, _sz, _sz, _sz, _mat, _i32, _P, _sz, _P, _P, _P]
 _lib.zpp_status_string.restype = ctypes.c_char_p
 _lib.zpp_status_string.argtypes = [ctypes.c_int]
 _lib.zpp_last_hip_error.restype = ctypes.c_int
@@ -91,7 +113,10 @@ EXPORTS = ("zpp_adam_partition_step", "zpp_adam_step_refresh_quantize", "zpp_ref
            "zpp_dequant_reduce_i4", "zpp_qgz_receive_adam_step",
            "zpp_qgz_receive_step_refresh_quantize", "zpp_quantize_blockwise_i4_interleaved",
            "zpp_dequant_reduce_i4_interleaved", "zpp_qgz_receive_adam_step_interleaved",
-           "zpp_qgz_receive_step_refresh_quantize_interleaved", "zpp_status_string",
+           "zpp_qgz_receive_step_refresh_quantize_interleaved", "zpp_checkpoint_save",
+           "zpp_checkpoint_load", "zpp_layer_norm_forward", "zpp_layer_norm_backward_workspace",
+           "zpp_layer_norm_backward", "zpp_gelu_forward", "zpp_gelu_backward",
+           "zpp_weight_grad_workspace", "zpp_weight_grad", "zpp_status_string",
            "zpp_last_hip_error")
 
 
@@ -566,6 +591,219 @@ def qgz_receive_step_refresh_quantize_interleaved(
         p, m, v, c, sc, num_src, grad_block, scale_out, *outs, n, block, ctypes.byref(hp),
         stream_handle(stream), warr, waits, _event_handle(done_after))
     _check(st, "zpp_qgz_receive_step_refresh_quantize_interleaved")
+
+
+# --------------------------------------------------------------------------
+# Layer operators.  Matrices are 2-D tensors [tokens, features], bf16 (or its
+# bits as int16 or uint16) or fp32, the features of a token consecutive; a
+# checkpoint in 8 bits is a tuple (codes, exps) as `empty_checkpoint` makes.
+# --------------------------------------------------------------------------
+ACT_BLOCK = 64  # features of a checkpoint's block
+
+_PARAM = _F32 | _BF16
+_DTYPES[_PARAM] = _DTYPES[_BF16] + _DTYPES[_F32]
+_DTYPES[_marshal.U8] = (torch.uint8,)
+
+# types a matrix may have, as bits of 1 << zpp_type
+_PLAIN = 1 | 2
+_SAVED = 4
+_ABSENT = 8
+_MATRIX_TYPES = {torch.bfloat16: 0, torch.int16: 0, torch.uint16: 0, torch.float32: 1,
+                 torch.int8: 2}
+_TYPE_NAMES = ("bf16", "fp32", "a checkpoint (codes, exps)")
+
+
+class Matrix(ctypes.Structure):
+    """Mirror of ``zpp_matrix``."""
+    _fields_ = [("data", _P), ("exps", _P), ("stride", _sz), ("type", _i32)]
+
+
+def empty_checkpoint(rows, cols, device="cuda"):
+    """Memory for a checkpoint of [rows, cols]: int8 codes and uint8 exponents."""
+    return (torch.empty(rows, cols, dtype=torch.int8, device=device),
+            torch.empty(rows, num_blocks(cols, ACT_BLOCK), dtype=torch.uint8, device=device))
+
+
+def _shape(m, name):
+    """Rows and columns of the matrix that sets a call's size."""
+    t = m[0] if isinstance(m, tuple) and len(m) == 2 else m
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor or a checkpoint (codes, exps)" % name)
+    if t.dim() != 2:
+        raise ValueError("%s must be a matrix [tokens, features]" % name)
+    return t.shape
+
+
+def _matrix(m, mask, rows, cols, name):
+    """One argument's checks in Python: its zpp_matrix, or the error."""
+    if m is None and mask & _ABSENT:
+        return None
+    pair = isinstance(m, tuple)
+    if pair and len(m) != 2:
+        raise TypeError("%s: a checkpoint is a tuple (codes, exps)" % name)
+    t = m[0] if pair else m
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor or a checkpoint (codes, exps)" % name)
+    kind = _MATRIX_TYPES.get(t.dtype, -1)
+    if kind < 0 or not mask >> kind & 1 or pair != (kind == 2):
+        raise TypeError("%s must be %s" % (name, " or ".join(
+            n for i, n in enumerate(_TYPE_NAMES) if mask >> i & 1)))
+    if not t.is_cuda:
+        raise ValueError("%s must be on the GPU" % name)
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError("%s is on %s, not on the current device cuda:%d"
+                         % (name, t.device, torch.cuda.current_device()))
+    if tuple(t.shape) != (rows, cols):
+        raise ValueError("%s must be [%d, %d], not %s" % (name, rows, cols, list(t.shape)))
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError("%s: the features of a token must be consecutive" % name)
+    exps = None
+    if pair:
+        _dev(m[1], (torch.uint8,), name + "[1]")
+        if m[1].numel() < rows * num_blocks(cols, ACT_BLOCK):
+            raise ValueError("%s: too few exponents" % name)
+        exps = m[1].data_ptr()
+    return bytes(Matrix(t.data_ptr(), exps, t.stride(0), kind))
+
+
+def _matrices(names, *args):
+    """The zpp_matrix of each object in args = (object, mask, rows, cols, ...),
+    in order; an optional one's None stays None."""
+    found = _marshal.matrices(_device(), ACT_BLOCK, *args)
+    if found is not None:
+        return found
+    return tuple(_matrix(*a, name) for name, a in
+                 zip(names, zip(args[::4], args[1::4], args[2::4], args[3::4])))
+
+
+def _params(gamma, beta, cols):
+    """Addresses of layer norm's weight and bias and their zpp_type."""
+    g, b = _addresses(("gamma", "beta"), "gamma and beta hold one value a feature",
+                      gamma, _PARAM, cols, beta, _PARAM | _OPTIONAL, cols)
+    kind = _MATRIX_TYPES[gamma.dtype]
+    if beta is not None and _MATRIX_TYPES[beta.dtype] != kind:
+        raise TypeError("gamma and beta must have one type")
+    return g, b, kind
+
+
+def _workspace(t, need, name):
+    """Address and size of a call's workspace; None where none is needed."""
+    if t is None and not need:
+        return None, 0
+    _dev(t, (torch.uint8,), "workspace")
+    if t.numel() < need:
+        raise ValueError("workspace: %s needs %d bytes, not %d" % (name, need, t.numel()))
+    return t.data_ptr(), t.numel()
+
+
+def checkpoint_save(x, saved, *, stream=None, wait_before=None, done_after=None):
+    """zpp_checkpoint_save: x in 8 bits into ``saved`` = (codes, exps)."""
+    rows, cols = _shape(x, "x")
+    mx, ms = _matrices(("x", "saved"), x, _PLAIN, rows, cols, saved, _SAVED, rows, cols)
+    st = _lib.zpp_checkpoint_save(mx, ms, rows, cols, stream_handle(stream),
+                                  _event_handle(wait_before), _event_handle(done_after))
+    _check(st, "zpp_checkpoint_save")
+
+
+def checkpoint_load(saved, out, *, stream=None, wait_before=None, done_after=None):
+    """zpp_checkpoint_load: the values of ``saved`` into out."""
+    rows, cols = _shape(saved, "saved")
+    ms, mo = _matrices(("saved", "out"), saved, _SAVED, rows, cols, out, _PLAIN, rows, cols)
+    st = _lib.zpp_checkpoint_load(ms, mo, rows, cols, stream_handle(stream),
+                                  _event_handle(wait_before), _event_handle(done_after))
+    _check(st, "zpp_checkpoint_load")
+
+
+def layer_norm_forward(x, gamma, beta, y, mean, rstd, *, eps, residual=None, total=None,
+                       saved=None, stream=None, wait_before=None, done_after=None):
+    """zpp_layer_norm_forward: y of x (of x + ``residual``, stored as
+    ``total``); ``saved``: the checkpoint of what is normalised.  ``beta``,
+    ``mean`` and ``rstd`` may be None."""
+    rows, cols = _shape(x, "x")
+    given = _PLAIN | _ABSENT
+    mx, mr, my, mt, ms = _matrices(
+        ("x", "residual", "y", "total", "saved"), x, _PLAIN, rows, cols, residual, given, rows,
+        cols, y, _PLAIN, rows, cols, total, given, rows, cols, saved, _SAVED | _ABSENT, rows, cols)
+    g, b, kind = _params(gamma, beta, cols)
+    pm, pr = _addresses(("mean", "rstd"), "mean and rstd hold one value a row",
+                        mean, _F32 | _OPTIONAL, rows, rstd, _F32 | _OPTIONAL, rows)
+    st = _lib.zpp_layer_norm_forward(mx, mr, g, b, kind, rows, cols, eps, my, mt, ms, pm, pr,
+                                     stream_handle(stream), _event_handle(wait_before),
+                                     _event_handle(done_after))
+    _check(st, "zpp_layer_norm_forward")
+
+
+def layer_norm_backward_workspace(rows, cols):
+    """Bytes of workspace of `layer_norm_backward` of this size."""
+    return _lib.zpp_layer_norm_backward_workspace(rows, cols)
+
+
+def layer_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace, *, dresidual=None,
+                        beta=None, y=None, accumulate=False, stream=None, wait_before=None,
+                        done_after=None):
+    """zpp_layer_norm_backward; ``x`` is what the forward pass normalised or its
+    checkpoint; ``y``: the forward pass's output again (with ``beta``);
+    ``dgamma`` and ``dbeta`` may be None."""
+    rows, cols = _shape(dy, "dy")
+    given = _PLAIN | _ABSENT
+    md, mx, mr, mo, my = _matrices(
+        ("dy", "x", "dresidual", "dx", "y"), dy, _PLAIN, rows, cols, x, _PLAIN | _SAVED, rows,
+        cols, dresidual, given, rows, cols, dx, _PLAIN, rows, cols, y, given, rows, cols)
+    g, b, kind = _params(gamma, beta, cols)
+    pm, pr, pg, pb = _addresses(
+        ("mean", "rstd", "dgamma", "dbeta"),
+        "mean and rstd hold one value a row, dgamma and dbeta one a feature",
+        mean, _F32, rows, rstd, _F32, rows, dgamma, _F32 | _OPTIONAL, cols,
+        dbeta, _F32 | _OPTIONAL, cols)
+    ws, size = _workspace(workspace, _lib.zpp_layer_norm_backward_workspace(rows, cols),
+                          "layer_norm_backward")
+    st = _lib.zpp_layer_norm_backward(md, mx, g, b, kind, pm, pr, mr, rows, cols, mo, my, pg, pb,
+                                      1 if accumulate else 0, ws, size, stream_handle(stream),
+                                      _event_handle(wait_before), _event_handle(done_after))
+    _check(st, "zpp_layer_norm_backward")
+
+
+def gelu_forward(u, a, *, saved=None, stream=None, wait_before=None, done_after=None):
+    """zpp_gelu_forward: a of u; ``saved``: the checkpoint of u."""
+    rows, cols = _shape(u, "u")
+    mu, ma, ms = _matrices(("u", "a", "saved"), u, _PLAIN, rows, cols, a, _PLAIN, rows, cols,
+                           saved, _SAVED | _ABSENT, rows, cols)
+    st = _lib.zpp_gelu_forward(mu, rows, cols, ma, ms, stream_handle(stream),
+                               _event_handle(wait_before), _event_handle(done_after))
+    _check(st, "zpp_gelu_forward")
+
+
+def gelu_backward(da, u, du, *, a=None, stream=None, wait_before=None, done_after=None):
+    """zpp_gelu_backward; ``u`` is the forward pass's input or its checkpoint;
+    ``a``: the forward pass's output again."""
+    rows, cols = _shape(da, "da")
+    md, mu, mo, ma = _matrices(
+        ("da", "u", "du", "a"), da, _PLAIN, rows, cols, u, _PLAIN | _SAVED, rows, cols,
+        du, _PLAIN, rows, cols, a, _PLAIN | _ABSENT, rows, cols)
+    st = _lib.zpp_gelu_backward(md, mu, rows, cols, mo, ma, stream_handle(stream),
+                                _event_handle(wait_before), _event_handle(done_after))
+    _check(st, "zpp_gelu_backward")
+
+
+def weight_grad_workspace(rows, n, k):
+    """Bytes of workspace of `weight_grad` of this size."""
+    return _lib.zpp_weight_grad_workspace(rows, n, k)
+
+
+def weight_grad(dy, x, dw, workspace, *, accumulate=False, stream=None, wait_before=None,
+                done_after=None):
+    """zpp_weight_grad: dw = dy^T x (added to it where ``accumulate``); ``x`` is
+    the layer's input in bf16 or its checkpoint, ``workspace`` may be None where
+    `weight_grad_workspace` is 0."""
+    rows, n = _shape(dy, "dy")
+    k = _shape(x, "x")[1]
+    md, mx, mw = _matrices(("dy", "x", "dw"), dy, 1, rows, n, x, 1 | _SAVED, rows, k,
+                           dw, 2, n, k)
+    ws, size = _workspace(workspace, _lib.zpp_weight_grad_workspace(rows, n, k), "weight_grad")
+    st = _lib.zpp_weight_grad(md, mx, rows, n, k, mw, 1 if accumulate else 0, ws, size,
+                              stream_handle(stream), _event_handle(wait_before),
+                              _event_handle(done_after))
+    _check(st, "zpp_weight_grad")
 
 
 # --------------------------------------------------------------------------
