@@ -22,7 +22,7 @@ struct WeightGradArgs {
     size_t out_stride;  // between rows
     size_t out_split;   // between splits
     size_t rows, split_rows;
-    uint32_t n, k, tiles_k;
+    uint32_t n, k, tiles_n, tiles_k;
     int accumulate;
 };
 
@@ -32,14 +32,85 @@ struct Piece {
     Chunk<TYPE> t[4];
 };
 
+// One operand as a lane sees it: where its pieces start.  A piece that starts
+// past the last feature takes the last chunk instead, and a chunk's elements
+// past the row's end whatever is there: both only reach results that are not
+// stored.
 template <int TYPE>
-__device__ __forceinline__ void fetch(Piece<TYPE> &p, const Mat &m, size_t row, size_t rows,
-                                      uint32_t col, uint32_t cols, uint32_t blocks) {
+struct Operand {
+    const uint8_t *data;  // of token 0, the same in all lanes
+    const uint8_t *exps;
+    size_t pitch;         // bytes between tokens
+    uint32_t blocks;      // exponents between tokens
+    uint32_t at, exp_at;  // the lane's bytes and exponents past the turn's first token
+    uint32_t valid;       // elements of its chunk inside the row
+    uint32_t margin;      // tokens before the matrix's end whose chunks may pass it
+};
+
+template <int TYPE>
+__device__ __forceinline__ Operand<TYPE> operand(const Mat &m, uint32_t cols, uint32_t col,
+                                                 uint32_t token) {
+    constexpr uint32_t kSize = TYPE == kBf16 ? 2 : 1;
+    Operand<TYPE> o;
+    const uint32_t last = (cols - 1) / 8 * 8;
+    col = col < last ? col : last;
+    o.data = reinterpret_cast<const uint8_t *>(m.data);
+    o.exps = m.exps;
+    o.pitch = m.stride * kSize;
+    o.blocks = (cols + kActBlock - 1) / kActBlock;
+    o.at = token * (uint32_t)o.pitch + col * kSize;
+    o.exp_at = token * o.blocks + col / kActBlock;
+    o.valid = cols - col < 8 ? cols - col : 8;
+    // the last chunk ends last + 8 - cols elements past its row
+    o.margin = cols % 8 ? (uint32_t)((last + 8 - cols + m.stride - 1) / m.stride) : 0;
+    return o;
+}
+
+__device__ __forceinline__ void fetch_chunk(Chunk<kBf16> &c, const Operand<kBf16> &o, size_t token) {
+    c.w = ld_at<u32x4, 2>(o.data + token * o.pitch + o.at);
+}
+__device__ __forceinline__ void fetch_chunk(Chunk<kI8> &c, const Operand<kI8> &o, size_t token) {
+    c.codes = ld_at<u32x2, 1>(o.data + token * o.pitch + o.at);
+    c.exp = (o.exps + token * o.blocks)[o.exp_at];
+}
+
+// A turn whose tokens all lie `margin` and more before the matrix's end: whole
+// chunks, which end inside the matrix.
+template <int TYPE>
+__device__ __forceinline__ void fetch(Piece<TYPE> &p, const Operand<TYPE> &o, size_t token) {
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i)
+        fetch_chunk(p.t[i], o, token + i);
+}
+
+// A row's last elements where a whole chunk would pass the matrix's end.
+__device__ __forceinline__ void fetch_part(Chunk<kBf16> &c, const Operand<kBf16> &o, size_t token) {
+    const uint16_t *p = reinterpret_cast<const uint16_t *>(o.data + token * o.pitch + o.at);
+    for (uint32_t e = 0; e < o.valid; ++e)
+        c.w[e / 2] |= (uint32_t)p[e] << (16 * (e % 2));
+}
+__device__ __forceinline__ void fetch_part(Chunk<kI8> &c, const Operand<kI8> &o, size_t token) {
+    const uint8_t *p = o.data + token * o.pitch + o.at;
+    for (uint32_t e = 0; e < o.valid; ++e)
+        c.codes[e / 4] |= (uint32_t)p[e] << (8 * (e % 4));
+    c.exp = (o.exps + token * o.blocks)[o.exp_at];
+}
+
+// A turn at the end: tokens from `end` on are zeros.  `mine`: the lane's first
+// token in the turn (which `at` holds as well).
+template <int TYPE>
+__device__ __forceinline__ void fetch_end(Piece<TYPE> &p, const Operand<TYPE> &o, size_t token,
+                                          uint32_t mine, size_t end, size_t rows) {
 #pragma unroll
     for (uint32_t i = 0; i < 4; ++i) {
         p.t[i] = Chunk<TYPE>{};
-        if (row + i < rows && col < cols)
-            p.t[i] = load_chunk<TYPE>(m, row + i, col, cols - col, blocks);
+        const size_t t = token + mine + i;
+        if (t < end) {
+            if (t + o.margin < rows || o.valid == 8)
+                fetch_chunk(p.t[i], o, token + i);
+            else
+                fetch_part(p.t[i], o, token + i);
+        }
     }
 }
 
@@ -53,45 +124,77 @@ __device__ __forceinline__ void turn(const Piece<kBf16> &p, u32x2 (&w)[8]) {
         w[e].y = __builtin_amdgcn_perm(p.t[3].w[e / 2], p.t[2].w[e / 2], sel);
     }
 }
+// code * 2^e is a bf16 number: its high half is all of it.
 __device__ __forceinline__ void turn(const Piece<kI8> &p, u32x2 (&w)[8]) {
-    float x[4][8];
+    float scale[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        chunk_values(p.t[i], x[i]);
-    // code * 2^e is a bf16 number: its high half is all of it
+        scale[i] = act_scale(p.t[i].exp);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        w[e].x = __builtin_amdgcn_perm(__float_as_uint(x[1][e]), __float_as_uint(x[0][e]),
-                                       0x07060302u);
-        w[e].y = __builtin_amdgcn_perm(__float_as_uint(x[3][e]), __float_as_uint(x[2][e]),
-                                       0x07060302u);
+        uint32_t x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            x[i] = __float_as_uint((float)(int8_t)(p.t[i].codes[e / 4] >> (8 * (e % 4))) *
+                                   scale[i]);
+        w[e].x = __builtin_amdgcn_perm(x[1], x[0], 0x07060302u);
+        w[e].y = __builtin_amdgcn_perm(x[3], x[2], 0x07060302u);
     }
 }
 
 // LDS holds a tile as [feature][64 tokens] bf16, 128 bytes a feature, in 16-byte
-// units of 8 tokens.  Unit u of feature f lies at place u ^ f % 8 ^ f / 8 % 8:
-// lanes that read one unit of 8 features in a row, and lanes that write one
-// feature of 8 neighbouring pieces, meet 8 different places.
+// units of 8 tokens.  Unit u of feature f lies at place u ^ key(f), the key made
+// of f's low three bits, its bits 3 and 4 and the tile's highest: lanes that
+// read one unit of 8 features in a row meet 8 different places, lanes that
+// write one feature of 8 pieces as well (chunk_of), and the 32-feature steps
+// of a wave's reads keep the key, so that they differ by a constant.
+template <uint32_t TILE>
 __device__ __forceinline__ uint32_t unit_at(uint32_t f, uint32_t u) {
-    return f * (kStep * 2) + ((u ^ f ^ (f >> 3)) & 7) * 16;
+    const uint32_t key = (f ^ (f >> 3 & 3) ^ (f / (TILE / 2) << 2)) & 7;
+    return f * (kStep * 2) + (u ^ key) * 16;
+}
+// The chunk of the p-th pair of lanes: bit 2 and the highest exchanged.
+template <uint32_t TILE>
+__device__ __forceinline__ uint32_t chunk_of(uint32_t p) {
+    constexpr uint32_t kHigh = TILE / 16;
+    const uint32_t low = p >> 2 & 1, high = p / kHigh & 1;
+    return (p & ~(kHigh | 4u)) | high << 2 | low * kHigh;
+}
+
+// Workgroup w's tile.  The dispatcher deals workgroups to the 8 XCDs in turn;
+// each XCD takes a run of consecutive tiles, ordered in bands of kBand tile rows,
+// so that the 32 tiles an XCD works on at a time share few rows and columns in
+// its L2.
+constexpr uint32_t kBand = 8;
+__device__ __forceinline__ void tile_of_group(uint32_t w, uint32_t tiles_n, uint32_t tiles_k,
+                                              uint32_t &tile_n, uint32_t &tile_k) {
+    const uint32_t total = tiles_n * tiles_k, xcd = w % 8, q = total / 8, r = total % 8;
+    const uint32_t t = xcd * q + (xcd < r ? xcd : r) + w / 8;
+    const uint32_t band = t / (kBand * tiles_k), first = band * kBand;
+    const uint32_t high = tiles_n - first < kBand ? tiles_n - first : kBand;
+    const uint32_t at = t - first * tiles_k;
+    tile_n = first + at % high;
+    tile_k = at / high;
 }
 
 template <int X, int TILE, int WAVES_N, int WAVES_K>
 __global__ __launch_bounds__(WAVES_N *WAVES_K *kWave) void weight_grad_kernel(WeightGradArgs a) {
     constexpr int MN = TILE / WAVES_N / 32, MK = TILE / WAVES_K / 32;
-    constexpr uint32_t kChunks = TILE / 8;
+    constexpr uint32_t kChunks = TILE / 8, kBytes = TILE * kStep * 2;
     static_assert(WAVES_N * WAVES_K * kWave == kChunks * kStep / 4, "one piece a lane");
-    __shared__ __attribute__((aligned(16))) uint8_t lds[2][TILE * kStep * 2];
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];  // [2 turns][2 operands][kBytes]
     const uint32_t tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-    const uint32_t tile_n = blockIdx.x / a.tiles_k, tile_k = blockIdx.x - tile_n * a.tiles_k;
+    uint32_t tile_n, tile_k;
+    tile_of_group(blockIdx.x, a.tiles_n, a.tiles_k, tile_n, tile_k);
     const uint32_t n0 = tile_n * TILE, k0 = tile_k * TILE;
-    const uint32_t blocks = (a.k + kActBlock - 1) / kActBlock;
     const size_t begin = (size_t)blockIdx.y * a.split_rows;
     const size_t end = begin + a.split_rows < a.rows ? begin + a.split_rows : a.rows;
 
     // the lane's piece: neighbouring lanes take the two halves of a unit
-    const uint32_t chunk = tid / 2 % kChunks, group = tid % 2 + 2 * (tid / (2 * kChunks));
+    const uint32_t chunk = chunk_of<TILE>(tid / 2 % kChunks), group = tid % 2 + 2 * (tid / (2 * kChunks));
     const uint32_t wn = wave / WAVES_K * (TILE / WAVES_N), wk = wave % WAVES_K * (TILE / WAVES_K);
+    const Operand<kBf16> od = operand<kBf16>(a.dy, a.n, n0 + chunk * 8, group * 4);
+    const Operand<X> ox = operand<X>(a.x, a.k, k0 + chunk * 8, group * 4);
 
     f32x16 acc[MN][MK];
 #pragma unroll
@@ -104,45 +207,76 @@ __global__ __launch_bounds__(WAVES_N *WAVES_K *kWave) void weight_grad_kernel(We
 
     Piece<kBf16> pd;
     Piece<X> px;
-    fetch(pd, a.dy, begin + group * 4, end, n0 + chunk * 8, a.n, 0);
-    fetch(px, a.x, begin + group * 4, end, k0 + chunk * 8, a.k, blocks);
-    for (size_t row = begin; row < end; row += kStep) {
+    auto get = [&](size_t token) {
+        fetch(pd, od, token);
+        fetch(px, ox, token);
+    };
+    auto put = [&](uint32_t buffer) {
         u32x2 w[8];
-        __syncthreads();
+        uint8_t *to = lds + buffer * (2 * kBytes) + group % 2 * 8;
         turn(pd, w);
 #pragma unroll
         for (uint32_t e = 0; e < 8; ++e)
-            *reinterpret_cast<u32x2 *>(&lds[0][unit_at(chunk * 8 + e, group / 2) + group % 2 * 8]) =
-                w[e];
+            *reinterpret_cast<u32x2 *>(to + unit_at<TILE>(chunk * 8 + e, group / 2)) = w[e];
         turn(px, w);
 #pragma unroll
         for (uint32_t e = 0; e < 8; ++e)
-            *reinterpret_cast<u32x2 *>(&lds[1][unit_at(chunk * 8 + e, group / 2) + group % 2 * 8]) =
-                w[e];
-        __syncthreads();
-        if (row + kStep < end) {
-            fetch(pd, a.dy, row + kStep + group * 4, end, n0 + chunk * 8, a.n, 0);
-            fetch(px, a.x, row + kStep + group * 4, end, k0 + chunk * 8, a.k, blocks);
-        }
+            *reinterpret_cast<u32x2 *>(to + kBytes + unit_at<TILE>(chunk * 8 + e, group / 2)) = w[e];
+    };
+    auto multiply = [&](uint32_t buffer, uint32_t kk) {
+        const uint8_t *from = lds + buffer * (2 * kBytes);
+        bf16x8 fd[MN], fx[MK];
+        const uint32_t unit = kk * 2 + lane / 32;
 #pragma unroll
-        for (uint32_t kk = 0; kk < kStep / 16; ++kk) {
-            bf16x8 fd[MN], fx[MK];
-            const uint32_t unit = kk * 2 + lane / 32;
+        for (int i = 0; i < MN; ++i)
+            fd[i] = *reinterpret_cast<const bf16x8 *>(from + unit_at<TILE>(wn + i * 32 + lane % 32, unit));
 #pragma unroll
-            for (int i = 0; i < MN; ++i)
-                fd[i] = *reinterpret_cast<const bf16x8 *>(
-                    &lds[0][unit_at(wn + i * 32 + lane % 32, unit)]);
+        for (int j = 0; j < MK; ++j)
+            fx[j] = *reinterpret_cast<const bf16x8 *>(from + kBytes +
+                                                      unit_at<TILE>(wk + j * 32 + lane % 32, unit));
+#pragma unroll
+        for (int i = 0; i < MN; ++i)
 #pragma unroll
             for (int j = 0; j < MK; ++j)
-                fx[j] = *reinterpret_cast<const bf16x8 *>(
-                    &lds[1][unit_at(wk + j * 32 + lane % 32, unit)]);
-#pragma unroll
-            for (int i = 0; i < MN; ++i)
-#pragma unroll
-                for (int j = 0; j < MK; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fd[i], fx[j], acc[i][j], 0,
-                                                                        0, 0);
-        }
+                acc[i][j] =
+                    __builtin_amdgcn_mfma_f32_32x32x16_bf16(fd[i], fx[j], acc[i][j], 0, 0, 0);
+    };
+
+    // Turn s is multiplied from one buffer while turn s + 1, fetched a turn ago,
+    // is laid into the other and turn s + 2 is on its way to registers.
+    const uint32_t margin = od.margin > ox.margin ? od.margin : ox.margin;
+    size_t turns = (end - begin) / kStep;
+    if (turns && begin + turns * kStep + margin > a.rows)
+        --turns;
+    uint32_t buffer = 0;
+    if (turns) {
+        get(begin);
+        put(0);
+        if (turns > 1)
+            get(begin + kStep);
+    }
+    for (size_t s = 0; s < turns; ++s) {
+        __syncthreads();
+        multiply(buffer, 0);
+        multiply(buffer, 1);
+        if (s + 1 < turns)
+            put(buffer ^ 1);
+        if (s + 2 < turns)
+            get(begin + (s + 2) * kStep);
+        multiply(buffer, 2);
+        multiply(buffer, 3);
+        buffer ^= 1;
+    }
+    for (size_t token = begin + turns * kStep; token < end; token += kStep) {
+        fetch_end(pd, od, token, group * 4, end, a.rows);
+        fetch_end(px, ox, token, group * 4, end, a.rows);
+        // the other buffer's readers are past the last barrier
+        put(buffer);
+        __syncthreads();
+#pragma unroll 1
+        for (uint32_t kk = 0; kk < kStep / 16; ++kk)
+            multiply(buffer, kk);
+        buffer ^= 1;
     }
 
     // lane l holds column l % 32 and, in register r, row 8 (r / 4) + 4 (l / 32) + r % 4
@@ -187,9 +321,28 @@ struct GradShape {
 };
 
 GradShape grad_shape(size_t rows, size_t n, size_t k) {
-    (void)n;
-    (void)k;
-    return {128, 1, (rows + kStep - 1) / kStep * kStep};
+    const size_t big = ((n + 255) / 256) * ((k + 255) / 256);
+    return {big >= kCus / 2 ? 256u : 128u, 1, (rows + kStep - 1) / kStep * kStep};
+}
+
+template <int X, int TILE, int WAVES_N, int WAVES_K>
+void start(const WeightGradArgs &a, uint32_t splits, hipStream_t stream) {
+    constexpr size_t kLds = 2 * 2 * TILE * kStep * 2;
+    static const hipError_t allowed = hipFuncSetAttribute(
+        reinterpret_cast<const void *>(weight_grad_kernel<X, TILE, WAVES_N, WAVES_K>),
+        hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
+    (void)allowed;
+    hipLaunchKernelGGL((weight_grad_kernel<X, TILE, WAVES_N, WAVES_K>),
+                       dim3(a.tiles_n * a.tiles_k, splits), dim3(WAVES_N * WAVES_K * kWave), kLds,
+                       stream, a);
+}
+
+template <int X>
+void start(const WeightGradArgs &a, const GradShape &s, hipStream_t stream) {
+    if (s.tile == 256)
+        start<X, 256, 2, 4>(a, s.splits, stream);
+    else
+        start<X, 128, 2, 2>(a, s.splits, stream);
 }
 
 }  // namespace
@@ -222,13 +375,13 @@ hipError_t launch_weight_grad(const Mat &dy, const Mat &x, int x_type, size_t ro
     a.split_rows = s.split_rows;
     a.n = (uint32_t)n;
     a.k = (uint32_t)k;
+    a.tiles_n = (uint32_t)((n + s.tile - 1) / s.tile);
     a.tiles_k = (uint32_t)((k + s.tile - 1) / s.tile);
     a.accumulate = s.splits > 1 ? 0 : accumulate;
-    const dim3 grid((unsigned)((n + s.tile - 1) / s.tile * a.tiles_k), s.splits);
     if (x_type == kI8)
-        hipLaunchKernelGGL((weight_grad_kernel<kI8, 128, 2, 2>), grid, dim3(256), 0, stream, a);
+        start<kI8>(a, s, stream);
     else
-        hipLaunchKernelGGL((weight_grad_kernel<kBf16, 128, 2, 2>), grid, dim3(256), 0, stream, a);
+        start<kBf16>(a, s, stream);
     if (s.splits > 1)
         hipLaunchKernelGGL(weight_grad_join, dim3(join_grid), dim3(256), 0, stream,
                            reinterpret_cast<const float *>(workspace), s.splits, (uint32_t)n,

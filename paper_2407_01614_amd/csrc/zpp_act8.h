@@ -27,6 +27,13 @@ struct Chunk<kI8> {
     uint32_t exp;
 };
 
+// A vector at an address aligned to A bytes, of memory that is read again.
+template <class V, int A>
+__device__ __forceinline__ V ld_at(const void *p) {
+    typedef V U __attribute__((aligned(A)));
+    return *reinterpret_cast<const U *>(p);
+}
+
 template <class E>
 __device__ __forceinline__ const E *at(const Mat &m, size_t row, uint32_t col) {
     return reinterpret_cast<const E *>(m.data) + row * m.stride + col;
