@@ -6,6 +6,11 @@
 // features, turns them in registers (byte permutes pair the tokens; a
 // checkpoint's codes are scaled on the way, exactly) and lays them into LDS
 // feature by feature, from where a lane reads its 16 bytes at once.
+#include <math.h>
+
+#include <initializer_list>
+#include <type_traits>
+
 #include "zpp_act8.h"
 
 namespace zpp {
@@ -66,12 +71,37 @@ __device__ __forceinline__ Operand<TYPE> operand(const Mat &m, uint32_t cols, ui
     return o;
 }
 
+// Memory at an address that is the same in all lanes, told to be global memory
+// and kept in scalar registers: loads add the lane's 32-bit offset themselves.
+#define ZPP_GLOBAL __attribute__((address_space(1)))
+typedef const ZPP_GLOBAL uint8_t *GlobalBytes;
+__device__ __forceinline__ GlobalBytes uniform(const uint8_t *p) {
+    const uint64_t u = reinterpret_cast<uint64_t>(p);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)u);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(u >> 32));
+    return reinterpret_cast<GlobalBytes>((uint64_t)hi << 32 | lo);
+}
+template <class V, int A>
+__device__ __forceinline__ V ld_uniform(const uint8_t *base, uint32_t offset) {
+    typedef V U __attribute__((aligned(A)));
+    return *reinterpret_cast<const ZPP_GLOBAL U *>(uniform(base) + offset);
+}
+
 __device__ __forceinline__ void fetch_chunk(Chunk<kBf16> &c, const Operand<kBf16> &o, size_t token) {
     c.w = ld_at<u32x4, 2>(o.data + token * o.pitch + o.at);
 }
 __device__ __forceinline__ void fetch_chunk(Chunk<kI8> &c, const Operand<kI8> &o, size_t token) {
-    c.codes = ld_at<u32x2, 1>(o.data + token * o.pitch + o.at);
-    c.exp = (o.exps + token * o.blocks)[o.exp_at];
+    c.codes = ld_uniform<u32x2, 1>(o.data + token * o.pitch, o.at);
+    c.exp = ld_uniform<uint8_t, 1>(o.exps + token * o.blocks, o.exp_at);
+}
+
+// Keeps what is computed from a loaded chunk behind this point: the compiler
+// would cut codes apart right after their load, and wait for it there.
+__device__ __forceinline__ void hold(Piece<kBf16> &) {}
+__device__ __forceinline__ void hold(Piece<kI8> &p) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        asm volatile("" : "+v"(p.t[i].codes.x), "+v"(p.t[i].codes.y), "+v"(p.t[i].exp));
 }
 
 // A turn whose tokens all lie `margin` and more before the matrix's end: whole
@@ -114,32 +144,21 @@ __device__ __forceinline__ void fetch_end(Piece<TYPE> &p, const Operand<TYPE> &o
     }
 }
 
-// The piece with its tokens side by side: word pair e holds feature e's four
-// tokens as bf16.
-__device__ __forceinline__ void turn(const Piece<kBf16> &p, u32x2 (&w)[8]) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const uint32_t sel = e % 2 ? 0x07060302u : 0x05040100u;
-        w[e].x = __builtin_amdgcn_perm(p.t[1].w[e / 2], p.t[0].w[e / 2], sel);
-        w[e].y = __builtin_amdgcn_perm(p.t[3].w[e / 2], p.t[2].w[e / 2], sel);
-    }
+// Feature e of a piece with its four tokens side by side, as bf16.
+__device__ __forceinline__ u32x2 turned(const Piece<kBf16> &p, int e, const float (&)[4]) {
+    const uint32_t sel = e % 2 ? 0x07060302u : 0x05040100u;
+    return u32x2{__builtin_amdgcn_perm(p.t[1].w[e / 2], p.t[0].w[e / 2], sel),
+                 __builtin_amdgcn_perm(p.t[3].w[e / 2], p.t[2].w[e / 2], sel)};
 }
 // code * 2^e is a bf16 number: its high half is all of it.
-__device__ __forceinline__ void turn(const Piece<kI8> &p, u32x2 (&w)[8]) {
-    float scale[4];
+__device__ __forceinline__ u32x2 turned(const Piece<kI8> &p, int e, const float (&scale)[4]) {
+    uint32_t x[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        scale[i] = act_scale(p.t[i].exp);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        uint32_t x[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            x[i] = __float_as_uint((float)(int8_t)(p.t[i].codes[e / 4] >> (8 * (e % 4))) *
-                                   scale[i]);
-        w[e].x = __builtin_amdgcn_perm(x[1], x[0], 0x07060302u);
-        w[e].y = __builtin_amdgcn_perm(x[3], x[2], 0x07060302u);
-    }
+        x[i] =
+            __float_as_uint((float)(int8_t)(p.t[i].codes[e / 4] >> (8 * (e % 4))) * scale[i]);
+    return u32x2{__builtin_amdgcn_perm(x[1], x[0], 0x07060302u),
+                 __builtin_amdgcn_perm(x[3], x[2], 0x07060302u)};
 }
 
 // LDS holds a tile as [feature][64 tokens] bf16, 128 bytes a feature, in 16-byte
@@ -159,6 +178,22 @@ __device__ __forceinline__ uint32_t chunk_of(uint32_t p) {
     constexpr uint32_t kHigh = TILE / 16;
     const uint32_t low = p >> 2 & 1, high = p / kHigh & 1;
     return (p & ~(kHigh | 4u)) | high << 2 | low * kHigh;
+}
+
+// Four of a piece's features laid into a tile.
+template <uint32_t TILE, int HALF, int TYPE>
+__device__ __forceinline__ void put_half(uint8_t *tile, const Piece<TYPE> &p, uint32_t chunk,
+                                         uint32_t group) {
+    float scale[4] = {};
+    if constexpr (TYPE == kI8) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            scale[i] = act_scale(p.t[i].exp);
+    }
+#pragma unroll
+    for (int e = HALF * 4; e < HALF * 4 + 4; ++e)
+        *reinterpret_cast<u32x2 *>(tile + unit_at<TILE>(chunk * 8 + e, group / 2) + group % 2 * 8) =
+            turned(p, e, scale);
 }
 
 // Workgroup w's tile.  The dispatcher deals workgroups to the 8 XCDs in turn;
@@ -181,7 +216,9 @@ template <int X, int TILE, int WAVES_N, int WAVES_K>
 __global__ __launch_bounds__(WAVES_N *WAVES_K *kWave) void weight_grad_kernel(WeightGradArgs a) {
     constexpr int MN = TILE / WAVES_N / 32, MK = TILE / WAVES_K / 32;
     constexpr uint32_t kChunks = TILE / 8, kBytes = TILE * kStep * 2;
-    static_assert(WAVES_N * WAVES_K * kWave == kChunks * kStep / 4, "one piece a lane");
+    // pieces a lane, kApart tokens from each other
+    constexpr uint32_t kPieces = kChunks * kStep / 4 / (WAVES_N * WAVES_K * kWave);
+    constexpr uint32_t kApart = kStep / kPieces;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];  // [2 turns][2 operands][kBytes]
     const uint32_t tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     uint32_t tile_n, tile_k;
@@ -205,77 +242,132 @@ __global__ __launch_bounds__(WAVES_N *WAVES_K *kWave) void weight_grad_kernel(We
             for (int e = 0; e < 16; ++e)
                 acc[i][j][e] = 0.0f;
 
-    Piece<kBf16> pd;
-    Piece<X> px;
-    auto get = [&](size_t token) {
-        fetch(pd, od, token);
-        fetch(px, ox, token);
+    Piece<kBf16> pd[kPieces];
+    Piece<X> px[kPieces];
+    auto get_dy = [&](size_t token) {
+#pragma unroll
+        for (uint32_t p = 0; p < kPieces; ++p)
+            fetch(pd[p], od, token + p * kApart);
     };
+    auto get_x = [&](size_t token) {
+#pragma unroll
+        for (uint32_t p = 0; p < kPieces; ++p)
+            fetch(px[p], ox, token + p * kApart);
+    };
+    // half of a piece's features laid into LDS
+    auto put_dy = [&](uint32_t buffer, auto half) {
+#pragma unroll
+        for (uint32_t p = 0; p < kPieces; ++p)
+            put_half<TILE, decltype(half)::value>(lds + buffer * (2 * kBytes), pd[p], chunk,
+                                                  group + p * kApart / 4);
+    };
+    auto put_x = [&](uint32_t buffer, auto half) {
+#pragma unroll
+        for (uint32_t p = 0; p < kPieces; ++p)
+            hold(px[p]);
+#pragma unroll
+        for (uint32_t p = 0; p < kPieces; ++p)
+            put_half<TILE, decltype(half)::value>(lds + buffer * (2 * kBytes) + kBytes, px[p],
+                                                  chunk, group + p * kApart / 4);
+    };
+    constexpr std::integral_constant<int, 0> low;
+    constexpr std::integral_constant<int, 1> high;
     auto put = [&](uint32_t buffer) {
-        u32x2 w[8];
-        uint8_t *to = lds + buffer * (2 * kBytes) + group % 2 * 8;
-        turn(pd, w);
-#pragma unroll
-        for (uint32_t e = 0; e < 8; ++e)
-            *reinterpret_cast<u32x2 *>(to + unit_at<TILE>(chunk * 8 + e, group / 2)) = w[e];
-        turn(px, w);
-#pragma unroll
-        for (uint32_t e = 0; e < 8; ++e)
-            *reinterpret_cast<u32x2 *>(to + kBytes + unit_at<TILE>(chunk * 8 + e, group / 2)) = w[e];
+        put_dy(buffer, low);
+        put_dy(buffer, high);
+        put_x(buffer, low);
+        put_x(buffer, high);
     };
-    auto multiply = [&](uint32_t buffer, uint32_t kk) {
+    bf16x8 fd[2][MN], fx[2][MK];
+    auto read = [&](uint32_t buffer, uint32_t kk, auto set) {
+        constexpr int S = decltype(set)::value;
         const uint8_t *from = lds + buffer * (2 * kBytes);
-        bf16x8 fd[MN], fx[MK];
         const uint32_t unit = kk * 2 + lane / 32;
 #pragma unroll
-        for (int i = 0; i < MN; ++i)
-            fd[i] = *reinterpret_cast<const bf16x8 *>(from + unit_at<TILE>(wn + i * 32 + lane % 32, unit));
-#pragma unroll
         for (int j = 0; j < MK; ++j)
-            fx[j] = *reinterpret_cast<const bf16x8 *>(from + kBytes +
-                                                      unit_at<TILE>(wk + j * 32 + lane % 32, unit));
+            fx[S][j] = *reinterpret_cast<const bf16x8 *>(
+                from + kBytes + unit_at<TILE>(wk + j * 32 + lane % 32, unit));
+#pragma unroll
+        for (int i = 0; i < MN; ++i)
+            fd[S][i] = *reinterpret_cast<const bf16x8 *>(
+                from + unit_at<TILE>(wn + i * 32 + lane % 32, unit));
+    };
+    auto multiply = [&](auto set) {
+        constexpr int S = decltype(set)::value;
 #pragma unroll
         for (int i = 0; i < MN; ++i)
 #pragma unroll
             for (int j = 0; j < MK; ++j)
                 acc[i][j] =
-                    __builtin_amdgcn_mfma_f32_32x32x16_bf16(fd[i], fx[j], acc[i][j], 0, 0, 0);
+                    __builtin_amdgcn_mfma_f32_32x32x16_bf16(fd[S][i], fx[S][j], acc[i][j], 0, 0, 0);
     };
+    auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
 
     // Turn s is multiplied from one buffer while turn s + 1, fetched a turn ago,
-    // is laid into the other and turn s + 2 is on its way to registers.
+    // is laid into the other and turn s + 2 is on its way to registers.  A turn is
+    // four steps of 16 tokens, each with the next step's LDS reads ahead of its
+    // products; the barrier stands before the last step, whose products then cover
+    // the other buffer's first reads.
     const uint32_t margin = od.margin > ox.margin ? od.margin : ox.margin;
     size_t turns = (end - begin) / kStep;
     if (turns && begin + turns * kStep + margin > a.rows)
         --turns;
     uint32_t buffer = 0;
     if (turns) {
-        get(begin);
+        const size_t last = begin + (turns - 1) * kStep;
+        get_x(begin);
+        get_dy(begin);
         put(0);
-        if (turns > 1)
-            get(begin + kStep);
-    }
-    for (size_t s = 0; s < turns; ++s) {
+        get_x(begin + kStep < last ? begin + kStep : last);
+        get_dy(begin + kStep < last ? begin + kStep : last);
         __syncthreads();
-        multiply(buffer, 0);
-        multiply(buffer, 1);
-        if (s + 1 < turns)
-            put(buffer ^ 1);
-        if (s + 2 < turns)
-            get(begin + (s + 2) * kStep);
-        multiply(buffer, 2);
-        multiply(buffer, 3);
+        read(0, 0, low);
+        for (size_t token = begin; token < last; token += kStep) {
+            const size_t next = token + 2 * kStep < last ? token + 2 * kStep : last;
+            fence();
+            read(buffer, 1, high);
+            put_x(buffer ^ 1, low);
+            multiply(low);
+            fence();
+            read(buffer, 2, low);
+            put_x(buffer ^ 1, high);
+            get_x(next);
+            multiply(high);
+            fence();
+            read(buffer, 3, high);
+            put_dy(buffer ^ 1, low);
+            put_dy(buffer ^ 1, high);
+            get_dy(next);
+            multiply(low);
+            fence();
+            __syncthreads();
+            buffer ^= 1;
+            read(buffer, 0, low);
+            multiply(high);
+        }
+        read(buffer, 1, high);
+        multiply(low);
+        read(buffer, 2, low);
+        multiply(high);
+        read(buffer, 3, high);
+        multiply(low);
+        multiply(high);
         buffer ^= 1;
     }
     for (size_t token = begin + turns * kStep; token < end; token += kStep) {
-        fetch_end(pd, od, token, group * 4, end, a.rows);
-        fetch_end(px, ox, token, group * 4, end, a.rows);
+#pragma unroll
+        for (uint32_t p = 0; p < kPieces; ++p) {
+            fetch_end(pd[p], od, token + p * kApart, group * 4, end, a.rows);
+            fetch_end(px[p], ox, token + p * kApart, group * 4, end, a.rows);
+        }
         // the other buffer's readers are past the last barrier
         put(buffer);
         __syncthreads();
 #pragma unroll 1
-        for (uint32_t kk = 0; kk < kStep / 16; ++kk)
-            multiply(buffer, kk);
+        for (uint32_t kk = 0; kk < kStep / 16; ++kk) {
+            read(buffer, kk, low);
+            multiply(low);
+        }
         buffer ^= 1;
     }
 
@@ -315,34 +407,73 @@ __global__ __launch_bounds__(256) void weight_grad_join(const float *parts, uint
     }
 }
 
+constexpr size_t kMostSplits = 64;
+
 struct GradShape {
     uint32_t tile, splits;
     size_t split_rows;
 };
 
+// Tile and number of splits of the tokens with the smallest expected time: the
+// rounds that the workgroups take over the CUs (two of tile 128 fit a CU, one of
+// tile 256), each as long as its turns and a fixed part, and with splits the
+// traffic of their partial results.  The constants, in us, are what bf16 and
+// checkpoints (a tenth more) measure.  Tile 128 against 256, without splits:
+// 4096x18176x4544 841 / 626, 2048x4096x4096 89 / 72, 4096x2048x2048 55 / 96,
+// 300x2048x2048 13 / 20.  Splits of tile 128, 1 / 4 / 16: 8192x1024x1024 91 / 38 /
+// 52, 8192x256x256 86 / 30 / 19, 1000x1000x1000 18 / 20 / 35.
 GradShape grad_shape(size_t rows, size_t n, size_t k) {
-    const size_t big = ((n + 255) / 256) * ((k + 255) / 256);
-    return {big >= kCus / 2 ? 256u : 128u, 1, (rows + kStep - 1) / kStep * kStep};
+    const size_t turns = (rows + kStep - 1) / kStep;
+    GradShape best = {128, 1, turns * kStep};
+    double least = 1e30;
+    for (const uint32_t tile : {128u, 256u}) {
+        const size_t tiles = ((n + tile - 1) / tile) * ((k + tile - 1) / tile);
+        for (size_t splits = 1; splits <= kMostSplits && splits <= turns; ++splits) {
+            const size_t per = (turns + splits - 1) / splits;
+            if ((turns + per - 1) / per != splits)
+                continue;  // the same as a smaller number
+            const double groups = (double)tiles * (double)splits;
+            double each, time = 5.0;
+            if (tile == 256) {
+                each = 1.95 * (double)per + 6.0;
+                time += ceil(groups / kCus) * each;
+            } else if (groups <= kCus) {
+                time += 0.7 * (double)per + 3.0;
+            } else {
+                each = 1.31 * (double)per + 4.0;
+                time += ceil(groups / (2 * kCus)) * each;
+            }
+            if (splits > 1)
+                time += 3.0 + 2.0 * (double)splits * (double)n * (double)k * 4.0 / 4.8e6;
+            if (time < least) {
+                least = time;
+                best = {tile, (uint32_t)splits, per * kStep};
+            }
+        }
+    }
+    return best;
 }
 
 template <int X, int TILE, int WAVES_N, int WAVES_K>
-void start(const WeightGradArgs &a, uint32_t splits, hipStream_t stream) {
+hipError_t start(const WeightGradArgs &a, uint32_t splits, hipStream_t stream) {
     constexpr size_t kLds = 2 * 2 * TILE * kStep * 2;
-    static const hipError_t allowed = hipFuncSetAttribute(
-        reinterpret_cast<const void *>(weight_grad_kernel<X, TILE, WAVES_N, WAVES_K>),
-        hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
-    (void)allowed;
+    const void *kernel =
+        reinterpret_cast<const void *>(weight_grad_kernel<X, TILE, WAVES_N, WAVES_K>);
+    // more than 64 KB of LDS has to be asked for, once
+    static const hipError_t allowed =
+        hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
+    if (allowed != hipSuccess)
+        return allowed;
     hipLaunchKernelGGL((weight_grad_kernel<X, TILE, WAVES_N, WAVES_K>),
                        dim3(a.tiles_n * a.tiles_k, splits), dim3(WAVES_N * WAVES_K * kWave), kLds,
                        stream, a);
+    return hipGetLastError();
 }
 
 template <int X>
-void start(const WeightGradArgs &a, const GradShape &s, hipStream_t stream) {
-    if (s.tile == 256)
-        start<X, 256, 2, 4>(a, s.splits, stream);
-    else
-        start<X, 128, 2, 2>(a, s.splits, stream);
+hipError_t start(const WeightGradArgs &a, const GradShape &s, hipStream_t stream) {
+    return s.tile == 256 ? start<X, 256, 2, 4>(a, s.splits, stream)
+                         : start<X, 128, 2, 2>(a, s.splits, stream);
 }
 
 }  // namespace
@@ -378,10 +509,10 @@ hipError_t launch_weight_grad(const Mat &dy, const Mat &x, int x_type, size_t ro
     a.tiles_n = (uint32_t)((n + s.tile - 1) / s.tile);
     a.tiles_k = (uint32_t)((k + s.tile - 1) / s.tile);
     a.accumulate = s.splits > 1 ? 0 : accumulate;
-    if (x_type == kI8)
-        start<kI8>(a, s, stream);
-    else
-        start<kBf16>(a, s, stream);
+    const hipError_t e =
+        x_type == kI8 ? start<kI8>(a, s, stream) : start<kBf16>(a, s, stream);
+    if (e != hipSuccess)
+        return e;
     if (s.splits > 1)
         hipLaunchKernelGGL(weight_grad_join, dim3(join_grid), dim3(256), 0, stream,
                            reinterpret_cast<const float *>(workspace), s.splits, (uint32_t)n,
