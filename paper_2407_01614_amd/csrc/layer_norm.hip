@@ -6,9 +6,10 @@
 // waves (4544 features: 568 chunks on 576 lanes).  Longer rows are read again
 // for each sum.
 //
-// RAGGED: rows whose last chunk of 8 is partial.  Its single loads and stores
-// need registers of their own, which a workgroup of 1024 lanes has only 128 of
-// each, so the kernels for whole chunks are compiled without them.
+// RAGGED: rows whose last chunk of 8 is partial.  The lane that has it takes the
+// row's last 8 elements instead and leaves out those that are the lane's before
+// (single loads would need registers of their own, and a workgroup of 1024 lanes
+// has 128 of each).  Rows of less than 8 go with the long ones.
 #include <type_traits>
 
 #include "zpp_act8.h"
@@ -19,34 +20,44 @@ namespace {
 constexpr uint32_t kMaxThreads = 1024;
 constexpr uint32_t kMostRegCols = kMaxThreads * 8;  // features of a row in registers
 
-// Sums of Q values over the workgroup's lanes, the same in every lane.  Two
-// buffers in turn: a wave writes a buffer again only after the barrier of the
-// call between, which every wave reaches after it has read this one.
+// Sums of Q values over a row's lanes, the same in every lane.  Two buffers in
+// turn: a wave writes a buffer again only after the barrier of the call between,
+// which every wave reaches after it has read this one.
 template <int Q>
 struct GroupSum {
-    float part[2][Q][16];
+    float part[2][16][Q];
 };
 
-// Sum of q over the `waves` waves that a row's lanes make up, first of them
+// Sums of q over the `waves` waves that a row's lanes make up, first of them
 // `wave0` (a workgroup may hold several rows).
 template <int Q>
 __device__ __forceinline__ void group_sum(float (&q)[Q], GroupSum<Q> &s, uint32_t &turn,
                                           uint32_t wave0, uint32_t waves) {
 #pragma unroll
     for (int i = 0; i < Q; ++i)
-        q[i] = sum64(q[i]);
-    if (waves == 1)
-        return;
-    if ((threadIdx.x & (kWave - 1)) == 0) {
+        q[i] = sum64_last(q[i]);
+    if (waves == 1) {
 #pragma unroll
         for (int i = 0; i < Q; ++i)
-            s.part[turn][i][threadIdx.x / kWave] = q[i];
+            q[i] = lane_value(q[i], kWave - 1);
+        return;
+    }
+    const uint32_t lane = threadIdx.x & (kWave - 1);
+    if (lane == kWave - 1) {
+#pragma unroll
+        for (int i = 0; i < Q; ++i)
+            s.part[turn][threadIdx.x / kWave][i] = q[i];
     }
     __syncthreads();
-    const uint32_t lane = threadIdx.x & 15;
+    // every 16 lanes read all of the row's waves
+    const uint32_t wave = lane & 15;
+    float v[Q];
 #pragma unroll
     for (int i = 0; i < Q; ++i)
-        q[i] = lane_value(sum16(lane < waves ? s.part[turn][i][wave0 + lane] : 0.0f), 0);
+        v[i] = s.part[turn][wave < waves ? wave0 + wave : wave0][i];
+#pragma unroll
+    for (int i = 0; i < Q; ++i)
+        q[i] = sum16(wave < waves ? v[i] : 0.0f);
     turn ^= 1;
 }
 
@@ -54,35 +65,109 @@ __device__ __forceinline__ void group_sum(float (&q)[Q], GroupSum<Q> &s, uint32_
 __device__ __forceinline__ void load_param(const void *p, int type, uint32_t col, uint32_t valid,
                                            float (&x)[8]) {
 #pragma unroll
-    for (uint32_t e = 0; e < 8; ++e) {
-        const uint32_t c = col + clamped(e, valid ? valid : 1);
+    for (int e = 0; e < 8; ++e)
         x[e] = 0.0f;
-        if (p && valid)
-            x[e] = type == kF32 ? reinterpret_cast<const float *>(p)[c]
-                                : __uint_as_float((uint32_t) reinterpret_cast<const uint16_t *>(p)[c]
-                                                  << 16);
-    }
+    if (!p || !valid)
+        return;
+    const Mat m = {const_cast<void *>(p), nullptr, 0};
+    if (type == kF32)
+        chunk_values(load_chunk<kF32>(m, 0, col, valid, 0), x);
+    else
+        chunk_values(load_chunk<kBf16>(m, 0, col, valid, 0), x);
 }
 
 __device__ __forceinline__ uint32_t valid_at(uint32_t col, uint32_t cols) {
     return col >= cols ? 0 : cols - col < 8 ? cols - col : 8;
 }
 
-// Elements past the row's end set to 0.
+// A lane's share of a row.
+struct RowLane {
+    uint32_t col;    // its 8 elements start here
+    uint32_t first;  // of them, those before this one are the lane's before
+    uint32_t block;  // the checkpoint's block of its elements
+    bool in;         // the row reaches it
+};
+
 template <bool RAGGED>
-__device__ __forceinline__ void clear_past(float (&x)[8], uint32_t valid) {
+__device__ __forceinline__ RowLane row_lane(uint32_t lane, uint32_t cols) {
+    RowLane l;
+    l.col = lane * 8;
+    l.block = l.col / kActBlock;
+    l.in = l.col < cols;
+    l.first = 0;
+    if (RAGGED && l.in && cols - l.col < 8) {
+        l.first = 8 - (cols - l.col);
+        l.col = cols - 8;
+    }
+    return l;
+}
+
+template <int TYPE>
+__device__ __forceinline__ Chunk<TYPE> load_row(const Mat &m, size_t row, const RowLane &l,
+                                                uint32_t blocks) {
+    if constexpr (TYPE == kI8) {
+        Chunk<kI8> c;
+        c.codes = ld_nt_at<u32x2, 1>(at<uint8_t>(m, row, l.col));
+        c.exp = m.exps[row * blocks + l.block];
+        return c;
+    } else {
+        return load_chunk<TYPE, false>(m, row, l.col, 8, blocks);
+    }
+}
+
+template <int TYPE, bool RAGGED>
+__device__ __forceinline__ void store_row(const Mat &m, size_t row, const RowLane &l,
+                                          const Chunk<TYPE> &c) {
+    if (!RAGGED || l.first == 0) {
+        store_chunk<TYPE, false>(m, row, l.col, 8, c);
+        return;
+    }
+#pragma unroll
+    for (uint32_t e = 1; e < 8; ++e)
+        if (e >= l.first) {
+            if constexpr (TYPE == kBf16)
+                out_at<uint16_t>(m, row, l.col)[e] = (uint16_t)(c.w[e / 2] >> (16 * (e % 2)));
+            else
+                out_at<float>(m, row, l.col)[e] = e < 4 ? c.lo[e] : c.hi[e - 4];
+        }
+}
+
+// Writes the checkpoint of the elements that the 8 lanes of a block hold, all
+// of which take part.  x is 0 in elements that are not the lane's.
+template <bool RAGGED>
+__device__ __forceinline__ void save_row(const Mat &m, size_t row, const RowLane &l,
+                                         uint32_t blocks, const float (&x)[8]) {
+    const uint32_t exp = act_exp(max8(max_bits(x, 8)));
+    if (!l.in)
+        return;
+    const u32x2 w = act_codes(x, exp);
+    uint8_t *p = out_at<uint8_t>(m, row, l.col);
+    if (!RAGGED || l.first == 0) {
+        st_nt_at<u32x2, 1>(p, w);
+    } else {
+#pragma unroll
+        for (uint32_t e = 1; e < 8; ++e)
+            if (e >= l.first)
+                p[e] = (uint8_t)(w[e / 4] >> (8 * (e % 4)));
+    }
+    if ((threadIdx.x & 7) == 0)
+        m.exps[row * blocks + l.block] = (uint8_t)exp;
+}
+
+// Elements that are not the lane's set to 0.
+template <bool RAGGED>
+__device__ __forceinline__ void clear_others(float (&x)[8], const RowLane &l) {
     if constexpr (RAGGED) {
 #pragma unroll
-        for (uint32_t e = 0; e < 8; ++e)
-            x[e] = e < valid ? x[e] : 0.0f;
+        for (uint32_t e = 0; e < 7; ++e)
+            x[e] = e < l.first ? 0.0f : x[e];
     }
 }
 
 // x, or x + residual rounded to the matrices' type (and stored as `total`).
-template <int TYPE, bool RAGGED>
-__device__ __forceinline__ void norm_input(const NormForwardArgs &a, size_t row, uint32_t col,
-                                           uint32_t valid, const Chunk<TYPE> &cx,
-                                           const Chunk<TYPE> &cr, bool store, float (&x)[8]) {
+template <int TYPE, class Store>
+__device__ __forceinline__ void norm_input(const NormForwardArgs &a, const Chunk<TYPE> &cx,
+                                           const Chunk<TYPE> &cr, float (&x)[8], Store &&store) {
     chunk_values(cx, x);
     if (a.residual.data) {
         float r[8];
@@ -91,46 +176,55 @@ __device__ __forceinline__ void norm_input(const NormForwardArgs &a, size_t row,
         for (int e = 0; e < 8; ++e)
             x[e] += r[e];
         const Chunk<TYPE> t = make_chunk<TYPE>(x);
-        if (store)
-            store_chunk<TYPE, RAGGED>(a.total, row, col, valid, t);
+        store(t);
         chunk_values(t, x);
     }
 }
 
-// R rows in flight a turn, one lane a chunk; blockDim.x lanes a row.
+// R rows a turn, blockDim.x lanes a row; the next turn's rows are on their way
+// while this turn's are summed.
 template <int TYPE, int R, bool RAGGED>
 __global__ __launch_bounds__(kMaxThreads) void norm_forward_kernel(NormForwardArgs a) {
     __shared__ GroupSum<R> scratch;
     const uint32_t blocks = (a.cols + kActBlock - 1) / kActBlock;
     const uint32_t waves = blockDim.x / kWave;
-    const uint32_t col = threadIdx.x * 8, valid = valid_at(col, a.cols);
+    const RowLane l = row_lane<RAGGED>(threadIdx.x, a.cols);
     const float per = 1.0f / (float)a.cols;
     uint32_t turn = 0;
     float gamma[8], beta[8];
-    load_param(a.gamma, a.param_type, col, valid, gamma);
-    load_param(a.beta, a.param_type, col, valid, beta);
-    for (size_t row0 = (size_t)blockIdx.x * R; row0 < a.rows; row0 += (size_t)gridDim.x * R) {
-        Chunk<TYPE> cx[R] = {}, cr[R] = {};
-        if (valid) {
+    load_param(a.gamma, a.param_type, l.col, l.in ? 8 : 0, gamma);
+    load_param(a.beta, a.param_type, l.col, l.in ? 8 : 0, beta);
+    Chunk<TYPE> cx[R] = {}, cr[R] = {};
+    // rows past the last are the last again
+    auto fetch = [&](size_t row0) {
+        if (l.in) {
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const size_t row = row0 + r < a.rows ? row0 + r : a.rows - 1;
-                cx[r] = load_chunk<TYPE, RAGGED>(a.x, row, col, valid, blocks);
+                cx[r] = load_row<TYPE>(a.x, row, l, blocks);
                 if (a.residual.data)
-                    cr[r] = load_chunk<TYPE, RAGGED>(a.residual, row, col, valid, blocks);
+                    cr[r] = load_row<TYPE>(a.residual, row, l, blocks);
             }
         }
+    };
+    const size_t step = (size_t)gridDim.x * R;
+    fetch((size_t)blockIdx.x * R);
+    for (size_t row0 = (size_t)blockIdx.x * R; row0 < a.rows; row0 += step) {
         float x[R][8], sum[R], mean[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            norm_input<TYPE, RAGGED>(a, row0 + r, col, valid, cx[r], cr[r],
-                                     row0 + r < a.rows && valid, x[r]);
-            clear_past<RAGGED>(x[r], valid);
+            norm_input<TYPE>(a, cx[r], cr[r], x[r], [&](const Chunk<TYPE> &t) {
+                if (l.in && row0 + r < a.rows)
+                    store_row<TYPE, RAGGED>(a.total, row0 + r, l, t);
+            });
+            clear_others<RAGGED>(x[r], l);
             sum[r] = 0.0f;
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 sum[r] += x[r][e];
         }
+        if (row0 + step < a.rows)
+            fetch(row0 + step);
         group_sum(sum, scratch, turn, 0, waves);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -139,8 +233,9 @@ __global__ __launch_bounds__(kMaxThreads) void norm_forward_kernel(NormForwardAr
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float d = x[r][e] - mean[r];
-                sum[r] += (RAGGED ? (uint32_t)e < valid : valid != 0) ? d * d : 0.0f;
+                sum[r] += !RAGGED || (uint32_t)e >= l.first ? d * d : 0.0f;
             }
+            sum[r] = l.in ? sum[r] : 0.0f;
         }
         group_sum(sum, scratch, turn, 0, waves);
 #pragma unroll
@@ -159,10 +254,10 @@ __global__ __launch_bounds__(kMaxThreads) void norm_forward_kernel(NormForwardAr
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 y[e] = __builtin_fmaf((x[r][e] - mean[r]) * rstd, gamma[e], beta[e]);
-            if (valid)
-                store_chunk<TYPE, RAGGED>(a.y, row, col, valid, make_chunk<TYPE>(y));
+            if (l.in)
+                store_row<TYPE, RAGGED>(a.y, row, l, make_chunk<TYPE>(y));
             if (a.saved.data)
-                save_chunk<RAGGED>(a.saved, row, col, valid, blocks, x[r]);
+                save_row<RAGGED>(a.saved, row, l, blocks, x[r]);
         }
     }
 }
@@ -189,7 +284,10 @@ __global__ __launch_bounds__(kMaxThreads) void norm_forward_long_kernel(NormForw
                         cr = load_chunk<TYPE>(a.residual, row, col, valid, blocks);
                 }
                 float x[8];
-                norm_input<TYPE, true>(a, row, col, valid, cx, cr, pass == 2 && valid, x);
+                norm_input<TYPE>(a, cx, cr, x, [&](const Chunk<TYPE> &t) {
+                    if (pass == 2 && valid)
+                        store_chunk<TYPE>(a.total, row, col, valid, t);
+                });
                 if (pass < 2) {
 #pragma unroll
                     for (uint32_t e = 0; e < 8; ++e) {
@@ -239,17 +337,17 @@ struct RowShape {
     uint32_t grid;     // its workgroups, pairs of arrays in the workspace
 };
 
-constexpr uint32_t kRowsAtOnce = 1;  // rows of a team in flight
+constexpr uint32_t kRowsAtOnce = 1;  // rows of a team in a turn
 
 RowShape row_shape(size_t rows, size_t cols) {
     RowShape s = {0, 0, 0};
-    if (cols > kMostRegCols)
+    if (cols > kMostRegCols || cols < 8)
         return s;
     const size_t chunks = (cols + 7) / 8;
     s.threads = (uint32_t)((chunks + kWave - 1) / kWave * kWave);
     s.teams = kMaxThreads / s.threads;
     const size_t groups = (rows + s.teams * kRowsAtOnce - 1) / (s.teams * kRowsAtOnce);
-    s.grid = (uint32_t)(groups < 2 * kCus ? groups : 2 * kCus);
+    s.grid = (uint32_t)(groups < kCus ? groups : kCus);
     return s;
 }
 
@@ -258,64 +356,99 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward_kernel(NormBackward
                                                                     uint32_t threads,
                                                                     uint32_t teams) {
     __shared__ GroupSum<2 * R> scratch;
-    extern __shared__ float joined[];  // [2][cols] where a workgroup has several teams
+    // gamma (and beta) in fp32, then, where a workgroup has several teams, the
+    // join of their sums
+    extern __shared__ float shared[];
     const uint32_t blocks = (a.cols + kActBlock - 1) / kActBlock;
     const uint32_t team = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / threads));
     const uint32_t lane = threadIdx.x - team * threads;
     const uint32_t waves = threads / kWave, wave0 = team * waves;
-    const uint32_t col = lane * 8, valid = valid_at(col, a.cols);
+    const RowLane l = row_lane<RAGGED>(lane, a.cols);
     const float per = 1.0f / (float)a.cols;
     uint32_t turn = 0;
-    float gamma[8], beta[8], dg[8], db[8];
-    load_param(a.gamma, a.param_type, col, valid, gamma);
-    if constexpr (AGAIN)
-        load_param(a.beta, a.param_type, col, valid, beta);
+    float dg[8], db[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         dg[e] = db[e] = 0.0f;
-    // every team takes as many turns, so that all meet at the barriers
-    const size_t step = (size_t)gridDim.x * teams * R;
-    for (size_t base = (size_t)blockIdx.x * teams * R; base < a.rows; base += step) {
-        const size_t row0 = base + (size_t)team * R;
-        Chunk<TYPE> cd[R] = {}, cr[R] = {};
-        Chunk<X> cx[R] = {};
-        float mean[R], rstd[R];
-        if (valid) {
+    // gamma and beta as two halves of four features a lane, so that neighbouring
+    // lanes read neighbouring 16 bytes
+    f32x4 *const params = reinterpret_cast<f32x4 *>(shared) + lane;
+    auto param = [&](int which, float (&v)[8]) {
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const size_t row = row0 + r < a.rows ? row0 + r : a.rows - 1;
-                cd[r] = load_chunk<TYPE, RAGGED>(a.dy, row, col, valid, blocks);
-                cx[r] = load_chunk<X, RAGGED>(a.x, row, col, valid, blocks);
-                if (a.dresidual.data)
-                    cr[r] = load_chunk<TYPE, RAGGED>(a.dresidual, row, col, valid, blocks);
-            }
+        for (int half = 0; half < 2; ++half) {
+            const f32x4 p = params[(2 * which + half) * threads];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[4 * half + e] = p[e];
         }
-        float s[2 * R];
+    };
+    if (team == 0) {
+#pragma unroll
+        for (int which = 0; which < (AGAIN ? 2 : 1); ++which) {
+            float v[8];
+            load_param(which ? a.beta : a.gamma, a.param_type, l.col, l.in ? 8 : 0, v);
+            params[2 * which * threads] = f32x4{v[0], v[1], v[2], v[3]};
+            params[(2 * which + 1) * threads] = f32x4{v[4], v[5], v[6], v[7]};
+        }
+    }
+    __syncthreads();
+    // the next turn's rows as loaded
+    Chunk<TYPE> nd[R] = {}, nr[R] = {};
+    Chunk<X> nx[R] = {};
+    float mean[R], rstd[R];
+    // Rows past the last are zeros, and so are their means and factors: they add
+    // nothing to any sum.
+    auto fetch = [&](size_t row0) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const size_t row = row0 + r < a.rows ? row0 + r : a.rows - 1;
-            mean[r] = a.mean[row];
-            rstd[r] = a.rstd[row];
-            // a row past the last, whose values are the last row's, adds nothing
-            const uint32_t in = row0 + r < a.rows ? valid : 0;
-            float d[8], h[8];
-            chunk_values(cd[r], d);
-            chunk_values(cx[r], h);
+            if (row0 + r < a.rows) {
+                if (l.in) {
+                    nd[r] = load_row<TYPE>(a.dy, row0 + r, l, blocks);
+                    nx[r] = load_row<X>(a.x, row0 + r, l, blocks);
+                    if (a.dresidual.data)
+                        nr[r] = load_row<TYPE>(a.dresidual, row0 + r, l, blocks);
+                }
+                mean[r] = a.mean[row0 + r];
+                rstd[r] = a.rstd[row0 + r];
+            } else {
+                nd[r] = Chunk<TYPE>{};
+                nx[r] = Chunk<X>{};
+                mean[r] = rstd[r] = 0.0f;
+            }
+        }
+    };
+    // every team takes as many turns, so that all meet at the barriers
+    const size_t step = (size_t)gridDim.x * teams * R;
+    const size_t mine = (size_t)team * R;
+    fetch((size_t)blockIdx.x * teams * R + mine);
+    for (size_t base = (size_t)blockIdx.x * teams * R; base < a.rows; base += step) {
+        const size_t row0 = base + mine;
+        Chunk<TYPE> cr[R];
+        float s[2 * R], g[R][8], h[R][8], scale[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float d[8];
+            chunk_values(nd[r], d);
+            clear_others<RAGGED>(d, l);
+            chunk_values(nx[r], h[r]);
+            param(0, g[r]);
+            scale[r] = rstd[r];
+            cr[r] = nr[r];
             s[2 * r] = s[2 * r + 1] = 0.0f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const bool inside = RAGGED ? (uint32_t)e < in : in != 0;
-                h[e] = inside ? (h[e] - mean[r]) * rstd[r] : 0.0f;
-                d[e] = inside ? d[e] : 0.0f;
-                dg[e] = __builtin_fmaf(d[e], h[e], dg[e]);
+                h[r][e] = (h[r][e] - mean[r]) * scale[r];
+                dg[e] = __builtin_fmaf(d[e], h[r][e], dg[e]);
                 db[e] += d[e];
-                const float g = d[e] * gamma[e];
-                s[2 * r] += g;
-                s[2 * r + 1] = __builtin_fmaf(g, h[e], s[2 * r + 1]);
+                g[r][e] *= d[e];
+                s[2 * r] += g[r][e];
+                s[2 * r + 1] = __builtin_fmaf(g[r][e], h[r][e], s[2 * r + 1]);
             }
         }
+        if (base + step < a.rows)
+            fetch(row0 + step);
         group_sum(s, scratch, turn, wave0, waves);
-        if (!valid)
+        if (!l.in)
             continue;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -323,17 +456,10 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward_kernel(NormBackward
             if (row >= a.rows)
                 break;
             const float c1 = s[2 * r] * per, c2 = s[2 * r + 1] * per;
-            float d[8], h[8], y[8];
-            chunk_values(cd[r], d);
-            chunk_values(cx[r], h);
+            float d[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                h[e] = (h[e] - mean[r]) * rstd[r];
-                if constexpr (AGAIN)
-                    y[e] = __builtin_fmaf(h[e], gamma[e], beta[e]);
-                const float g = __builtin_fmaf(d[e], gamma[e], -c1);
-                d[e] = rstd[r] * __builtin_fmaf(-h[e], c2, g);
-            }
+            for (int e = 0; e < 8; ++e)
+                d[e] = scale[r] * __builtin_fmaf(-h[r][e], c2, g[r][e] - c1);
             if (a.dresidual.data) {
                 float past[8];
                 chunk_values(cr[r], past);
@@ -341,36 +467,42 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward_kernel(NormBackward
                 for (int e = 0; e < 8; ++e)
                     d[e] += past[e];
             }
-            store_chunk<TYPE, RAGGED>(a.dx, row, col, valid, make_chunk<TYPE>(d));
-            if constexpr (AGAIN)
-                store_chunk<TYPE, RAGGED>(a.y, row, col, valid, make_chunk<TYPE>(y));
+            store_row<TYPE, RAGGED>(a.dx, row, l, make_chunk<TYPE>(d));
+            if constexpr (AGAIN) {
+                float w[8], y[8];
+                param(0, w);
+                param(1, y);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    y[e] = __builtin_fmaf(h[r][e], w[e], y[e]);
+                store_row<TYPE, RAGGED>(a.y, row, l, make_chunk<TYPE>(y));
+            }
         }
     }
     if (!a.partials)
         return;
-    // the teams' sums, one team after the other, then the workgroup's pair
+    // The teams' sums, one team after the other, then the workgroup's pair; the
+    // join's memory is gamma's, which all are done with.  Both are laid out as
+    // gamma is, [2][2 halves][threads][4].
+    f32x4 v[4] = {{dg[0], dg[1], dg[2], dg[3]},
+                  {dg[4], dg[5], dg[6], dg[7]},
+                  {db[0], db[1], db[2], db[3]},
+                  {db[4], db[5], db[6], db[7]}};
     for (uint32_t t = 0; t < teams; ++t) {
-        if (team == t) {
-#pragma unroll
-            for (uint32_t e = 0; e < 8; ++e)
-                if (e < valid) {
-                    const uint32_t c = col + e;
-                    if (t > 0) {
-                        dg[e] += joined[c];
-                        db[e] += joined[a.cols + c];
-                    }
-                    if (t + 1 < teams) {
-                        joined[c] = dg[e];
-                        joined[a.cols + c] = db[e];
-                    } else {
-                        float *p = a.partials + (size_t)blockIdx.x * 2 * a.cols;
-                        p[c] = dg[e];
-                        p[a.cols + c] = db[e];
-                    }
-                }
-        }
-        if (t + 1 < teams)
+        if (teams > 1)
             __syncthreads();
+        if (team != t)
+            continue;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (t > 0)
+                v[i] += params[i * threads];
+            if (t + 1 < teams)
+                params[i * threads] = v[i];
+            else
+                reinterpret_cast<f32x4 *>(a.partials)[((size_t)blockIdx.x * 4 + i) * threads + lane] =
+                    v[i];
+        }
     }
 }
 
@@ -459,28 +591,50 @@ __global__ __launch_bounds__(kStripThreads) void norm_backward_long_kernel(NormB
 }
 
 // The workgroups' pairs of arrays added: 64 columns a workgroup, its 16 waves
-// taking every 16th pair, joined in order.
+// taking every 16th pair, joined in order.  An array holds `width` columns, in
+// their order (threads == 0) or as the register kernels lay them out.
 constexpr uint32_t kJoinWaves = 16;
-__global__ __launch_bounds__(kJoinWaves *kWave) void norm_backward_join(const float *partials,
-                                                                        uint32_t count,
-                                                                        uint32_t cols,
-                                                                        float *dgamma,
-                                                                        float *dbeta,
-                                                                        int accumulate) {
+__global__ __launch_bounds__(kJoinWaves *kWave) void norm_backward_join(
+    const float *partials, uint32_t count, uint32_t width, uint32_t threads, uint32_t cols,
+    float *dgamma, float *dbeta, int accumulate) {
     __shared__ float part[kJoinWaves][kWave];
     const uint32_t wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
     float *out = blockIdx.y ? dbeta : dgamma;
     if (!out)
         return;
-    const size_t col = (size_t)blockIdx.x * kWave + lane;
-    const float *p = partials + (size_t)blockIdx.y * cols + col;
+    const uint32_t at = blockIdx.x * kWave + lane;
+    uint32_t col = at;
+    bool in = at < width;
+    if (threads && in) {
+        const uint32_t half = at / (4 * threads), i = at % (4 * threads);
+        const uint32_t e = 4 * half + i % 4, start = i / 4 * 8;
+        // a last, partial chunk holds the row's last 8 columns
+        in = start < cols;
+        col = start + e;
+        if (in && cols - start < 8) {
+            col = cols - 8 + e;
+            in = col >= start;
+        }
+    }
+    const float *p = partials + (size_t)blockIdx.y * width + at;
     float sum = 0.0f;
-    if (col < cols)
-        for (uint32_t i = wave; i < count; i += kJoinWaves)
-            sum += p[(size_t)i * 2 * cols];
+    if (in) {
+        // eight loads at a time; those past the last are not added
+        for (uint32_t i = wave; i < count; i += 8 * kJoinWaves) {
+            float v[8];
+#pragma unroll
+            for (uint32_t u = 0; u < 8; ++u) {
+                const uint32_t pair = i + u * kJoinWaves;
+                v[u] = p[(size_t)(pair < count ? pair : count - 1) * 2 * width];
+            }
+#pragma unroll
+            for (uint32_t u = 0; u < 8; ++u)
+                sum += i + u * kJoinWaves < count ? v[u] : 0.0f;
+        }
+    }
     part[wave][lane] = sum;
     __syncthreads();
-    if (wave == 0 && col < cols) {
+    if (wave == 0 && in) {
 #pragma unroll
         for (uint32_t w = 1; w < kJoinWaves; ++w)
             sum += part[w][lane];
@@ -506,11 +660,11 @@ uint32_t long_row_groups(size_t rows, size_t cols) {
 
 template <int TYPE, int X, bool AGAIN>
 void start_backward(const NormBackwardArgs &a, const RowShape &s, hipStream_t stream) {
-    const size_t lds = s.teams > 1 ? 2 * sizeof(float) * a.cols : 0;
+    const size_t lds = 2 * sizeof(float) * s.threads * 8;
     const dim3 grid(s.grid), threads(s.threads * s.teams);
     if (a.cols % 8)
-        hipLaunchKernelGGL((norm_backward_kernel<TYPE, X, 1, AGAIN, true>), grid, threads, lds,
-                           stream, a, s.threads, s.teams);
+        hipLaunchKernelGGL((norm_backward_kernel<TYPE, X, kRowsAtOnce, AGAIN, true>), grid, threads,
+                           lds, stream, a, s.threads, s.teams);
     else
         hipLaunchKernelGGL((norm_backward_kernel<TYPE, X, kRowsAtOnce, AGAIN, false>), grid,
                            threads, lds, stream, a, s.threads, s.teams);
@@ -546,12 +700,14 @@ hipError_t launch_norm_forward(const NormForwardArgs &a, int type, hipStream_t s
                                dim3(kMaxThreads), 0, stream, a);
             return;
         }
-        // workgroups that fit the GPU's 2048 lanes per CU at once; two rows in
-        // flight each where there are rows for all
-        const size_t fit = (size_t)kCus * (2048 / threads);
+        // workgroups that the GPU holds at once, at the 128 registers a lane that
+        // workgroups of 1024 leave; two rows a turn where there are rows for all
+        const size_t fit = (size_t)kCus * (1024 / threads);
         const dim3 grid((unsigned)(a.rows < fit ? a.rows : fit));
-        if (a.cols % 8)
+        if (a.cols % 8 && a.rows < 2 * fit)
             hipLaunchKernelGGL((norm_forward_kernel<T, 1, true>), grid, dim3(threads), 0, stream, a);
+        else if (a.cols % 8)
+            hipLaunchKernelGGL((norm_forward_kernel<T, 2, true>), grid, dim3(threads), 0, stream, a);
         else if (a.rows < 2 * fit)
             hipLaunchKernelGGL((norm_forward_kernel<T, 1, false>), grid, dim3(threads), 0, stream,
                                a);
@@ -566,7 +722,7 @@ size_t norm_backward_workspace(size_t rows, size_t cols) {
         return 0;
     const RowShape s = row_shape(rows, cols);
     if (s.threads)
-        return (size_t)s.grid * 2 * cols * sizeof(float);
+        return (size_t)s.grid * 2 * s.threads * 8 * sizeof(float);
     return (2 * rows + (size_t)long_row_groups(rows, cols) * 2 * cols) * sizeof(float);
 }
 
@@ -593,9 +749,10 @@ hipError_t launch_norm_backward(const NormBackwardArgs &args, int type, int x_ty
     const uint32_t pairs =
         !a.rows ? 0 : s.threads ? s.grid : long_row_groups(a.rows, a.cols);
     const float *partials = args.partials + (s.threads ? 0 : 2 * a.rows);
-    hipLaunchKernelGGL(norm_backward_join, dim3((a.cols + kWave - 1) / kWave, 2),
-                       dim3(kJoinWaves * kWave), 0, stream, partials, pairs, a.cols, a.dgamma,
-                       a.dbeta, a.accumulate);
+    const uint32_t width = s.threads ? s.threads * 8 : a.cols;
+    hipLaunchKernelGGL(norm_backward_join, dim3((width + kWave - 1) / kWave, 2),
+                       dim3(kJoinWaves * kWave), 0, stream, partials, pairs, width, s.threads,
+                       a.cols, a.dgamma, a.dbeta, a.accumulate);
     return hipGetLastError();
 }
 

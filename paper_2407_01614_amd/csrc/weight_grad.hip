@@ -95,15 +95,6 @@ __device__ __forceinline__ void fetch_chunk(Chunk<kI8> &c, const Operand<kI8> &o
     c.exp = ld_uniform<uint8_t, 1>(o.exps + token * o.blocks, o.exp_at);
 }
 
-// Keeps what is computed from a loaded chunk behind this point: the compiler
-// would cut codes apart right after their load, and wait for it there.
-__device__ __forceinline__ void hold(Piece<kBf16> &) {}
-__device__ __forceinline__ void hold(Piece<kI8> &p) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        asm volatile("" : "+v"(p.t[i].codes.x), "+v"(p.t[i].codes.y), "+v"(p.t[i].exp));
-}
-
 // A turn whose tokens all lie `margin` and more before the matrix's end: whole
 // chunks, which end inside the matrix.
 template <int TYPE>
@@ -142,6 +133,15 @@ __device__ __forceinline__ void fetch_end(Piece<TYPE> &p, const Operand<TYPE> &o
                 fetch_part(p.t[i], o, token + i);
         }
     }
+}
+
+// Codes are kept whole until they are laid into LDS: the compiler cut them apart
+// at their load, and waited for it there (4096x18176x4544: 790 us, 661 so).
+__device__ __forceinline__ void hold_piece(Piece<kBf16> &) {}
+__device__ __forceinline__ void hold_piece(Piece<kI8> &p) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        hold(p.t[i]);
 }
 
 // Feature e of a piece with its four tokens side by side, as bf16.
@@ -264,7 +264,7 @@ __global__ __launch_bounds__(WAVES_N *WAVES_K *kWave) void weight_grad_kernel(We
     auto put_x = [&](uint32_t buffer, auto half) {
 #pragma unroll
         for (uint32_t p = 0; p < kPieces; ++p)
-            hold(px[p]);
+            hold_piece(px[p]);
 #pragma unroll
         for (uint32_t p = 0; p < kPieces; ++p)
             put_half<TILE, decltype(half)::value>(lds + buffer * (2 * kBytes) + kBytes, px[p],
@@ -496,6 +496,9 @@ hipError_t launch_weight_grad(const Mat &dy, const Mat &x, int x_type, size_t ro
         return hipGetLastError();
     }
     const GradShape s = grad_shape(rows, n, k);
+    // a grid has 2^32 - 1 work-items at most
+    if (((n + s.tile - 1) / s.tile) * ((k + s.tile - 1) / s.tile) > UINT32_MAX / 512 / s.splits)
+        return hipErrorInvalidConfiguration;
     WeightGradArgs a;
     a.dy = dy;
     a.x = x;

@@ -88,6 +88,16 @@ __device__ __forceinline__ Chunk<TYPE> load_chunk(const Mat &m, size_t row, uint
     return c;
 }
 
+// Keeps what is made of a loaded chunk behind this point: the compiler would
+// make it early and hold that in registers instead.
+__device__ __forceinline__ void hold(Chunk<kBf16> &c) {
+    asm volatile("" : "+v"(c.w.x), "+v"(c.w.y), "+v"(c.w.z), "+v"(c.w.w));
+}
+__device__ __forceinline__ void hold(Chunk<kF32> &) {}
+__device__ __forceinline__ void hold(Chunk<kI8> &c) {
+    asm volatile("" : "+v"(c.codes.x), "+v"(c.codes.y), "+v"(c.exp));
+}
+
 // The scale of a checkpoint's block.
 __device__ __forceinline__ float act_scale(uint32_t exp) {
     return __uint_as_float(exp == 255u ? kScaleNaNBits : exp << 23);
@@ -190,10 +200,15 @@ __device__ __forceinline__ float sum16(float x) {
 __device__ __forceinline__ float lane_value(float x, int lane) {
     return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(x), lane));
 }
-// Sum of the wave, the same in every lane.
-__device__ __forceinline__ float sum64(float x) {
+// Sum of the wave, in its last lane: the rows of 16 lanes, then row 0 to 1 and 2
+// to 3, then the lower two to the upper two.
+__device__ __forceinline__ float sum64_last(float x) {
     x = sum16(x);
-    return (lane_value(x, 0) + lane_value(x, 16)) + (lane_value(x, 32) + lane_value(x, 48));
+    x += __uint_as_float(
+        (uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x142, 0xA, 0xF, false));
+    x += __uint_as_float(
+        (uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x143, 0xC, 0xF, false));
+    return x;
 }
 
 // The exponent byte of a block from the bits of its largest magnitude: the
