@@ -4,40 +4,53 @@
 // All four are one pass over matrices: eight neighbouring lanes take one block
 // of 64 elements of a row, 16 bytes of bf16 a lane, so the block's largest
 // magnitude is three DPP steps over values that are in registers anyway.
+#include <initializer_list>
+
 #include "zpp_act8.h"
 
 namespace zpp {
 namespace {
 
 constexpr uint32_t kThreads = 256;
-constexpr uint32_t kUnroll = 2;                              // blocks a lane group takes
-constexpr uint32_t kBlocksPerWg = kThreads / 8 * kUnroll;    // blocks of 64 elements
+constexpr uint32_t kGroups = kThreads / 8;  // lane groups, blocks side by side
+
+// Where a lane's eight elements are: row and column, or, where all matrices are
+// without gaps and rows are whole blocks (FLAT), the place in one long row.
+struct Place {
+    size_t row, col, block;
+    uint32_t valid;  // 0 past the row's or the matrix's end
+    __device__ __forceinline__ size_t in(const Mat &m) const { return row * m.stride + col; }
+};
 
 // The blocks of a [rows, cols] matrix are numbered along its rows.  A
 // workgroup's first block is found by one 64-bit division that the whole
-// workgroup shares; a lane's own lies less than blocks + kBlocksPerWg further on,
-// which the high half of a 32-bit product divides: with blocks < 2^26 and x <
-// 2^26 + 64, magic = ceil(2^58 / blocks) gives x magic / 2^58 - x / blocks <
-// x / 2^58 < 1 / blocks, so the quotient is exact (in 64-bit arithmetic).
+// workgroup shares; a lane's own lies less than per_row + 64 blocks further on,
+// which the high half of a product divides: with per_row < 2^26 and x < 2^26 + 64,
+// magic = ceil(2^58 / per_row) gives x magic / 2^58 - x / per_row < x / 2^58 <
+// 1 / per_row, so the quotient is exact.
 struct Blocks {
-    size_t rows, total;
+    size_t total;
     uint32_t cols, per_row;
     uint64_t magic;
 };
 
-struct Place {
-    size_t row;
-    uint32_t col, valid;  // valid: 0 past the row's or the matrix's end
-};
-
-__device__ __forceinline__ Place place_of(const Blocks &b, size_t row0, uint32_t rem0, size_t left,
-                                          uint32_t i) {
-    const uint32_t x = rem0 + i;
-    const uint32_t q = (uint32_t)__umul64hi((uint64_t)x << 6, b.magic);
+template <bool FLAT>
+__device__ __forceinline__ Place place_of(const Blocks &b, size_t block0, size_t row0,
+                                          uint32_t rem0, uint32_t i) {
     Place p;
-    p.row = row0 + q;
-    p.col = (x - q * b.per_row) * kActBlock + (threadIdx.x & 7) * 8;
-    p.valid = i < left && p.col < b.cols ? (b.cols - p.col < 8 ? b.cols - p.col : 8) : 0;
+    p.block = block0 + i;
+    if constexpr (FLAT) {
+        p.row = 0;
+        p.col = block0 * kActBlock + (i * kActBlock + (threadIdx.x & 7) * 8);
+        p.valid = i < b.total - block0 ? 8 : 0;
+    } else {
+        const uint32_t x = rem0 + i;
+        const uint32_t q = (uint32_t)__umul64hi((uint64_t)x << 6, b.magic);
+        const uint32_t col = (x - q * b.per_row) * kActBlock + (threadIdx.x & 7) * 8;
+        p.row = row0 + q;
+        p.col = col;
+        p.valid = i < b.total - block0 && col < b.cols ? (b.cols - col < 8 ? b.cols - col : 8) : 0;
+    }
     return p;
 }
 
@@ -82,43 +95,55 @@ struct GeluBackwardArgs {
     Mat da, u, du, a;
 };
 
+// The operators: what a lane loads, and what it makes of it.  kUnroll: blocks a
+// lane group takes (GELU's backward pass from bf16, 8192x8192, one / two: 70 / 76
+// us; its forward pass 54 / 48).
 template <int TYPE>
 struct SaveOp {
+    static constexpr uint32_t kUnroll = 2;
     typedef SaveArgs Args;
     Chunk<TYPE> x;
-    __device__ void load(const Args &a, const Blocks &b, const Place &p) {
-        x = load_chunk<TYPE>(a.in, p.row, p.col, p.valid, b.per_row);
+    template <bool RAGGED>
+    __device__ void load(const Args &a, const Place &p) {
+        x = load_chunk<TYPE, RAGGED>(a.in, p.in(a.in), p.valid, p.block);
     }
-    __device__ void store(const Args &a, const Blocks &b, const Place &p) {
+    template <bool RAGGED>
+    __device__ void store(const Args &a, const Place &p) {
         float v[8];
         chunk_values(x, v);
-        save_chunk(a.saved, p.row, p.col, p.valid, b.per_row, v);
+        save_chunk<RAGGED>(a.saved, p.in(a.saved), p.valid, p.block, v);
     }
 };
 
 template <int TYPE>
 struct LoadOp {
+    static constexpr uint32_t kUnroll = 2;
     typedef LoadArgs Args;
     Chunk<kI8> x;
-    __device__ void load(const Args &a, const Blocks &b, const Place &p) {
-        x = load_chunk<kI8>(a.saved, p.row, p.col, p.valid, b.per_row);
+    template <bool RAGGED>
+    __device__ void load(const Args &a, const Place &p) {
+        x = load_chunk<kI8, RAGGED>(a.saved, p.in(a.saved), p.valid, p.block);
     }
-    __device__ void store(const Args &a, const Blocks &, const Place &p) {
+    template <bool RAGGED>
+    __device__ void store(const Args &a, const Place &p) {
         float v[8];
         chunk_values(x, v);
         if (p.valid)
-            store_chunk<TYPE>(a.out, p.row, p.col, p.valid, make_chunk<TYPE>(v));
+            store_chunk<TYPE, RAGGED>(a.out, p.in(a.out), p.valid, make_chunk<TYPE>(v));
     }
 };
 
 template <int TYPE>
 struct GeluForwardOp {
+    static constexpr uint32_t kUnroll = 2;
     typedef GeluForwardArgs Args;
     Chunk<TYPE> x;
-    __device__ void load(const Args &a, const Blocks &b, const Place &p) {
-        x = load_chunk<TYPE>(a.u, p.row, p.col, p.valid, b.per_row);
+    template <bool RAGGED>
+    __device__ void load(const Args &a, const Place &p) {
+        x = load_chunk<TYPE, RAGGED>(a.u, p.in(a.u), p.valid, p.block);
     }
-    __device__ void store(const Args &a, const Blocks &b, const Place &p) {
+    template <bool RAGGED>
+    __device__ void store(const Args &a, const Place &p) {
         float v[8], y[8];
         chunk_values(x, v);
 #pragma unroll
@@ -127,22 +152,25 @@ struct GeluForwardOp {
             y[e] = u * normal(u).cdf;
         }
         if (p.valid)
-            store_chunk<TYPE>(a.a, p.row, p.col, p.valid, make_chunk<TYPE>(y));
+            store_chunk<TYPE, RAGGED>(a.a, p.in(a.a), p.valid, make_chunk<TYPE>(y));
         if (a.saved.data)
-            save_chunk(a.saved, p.row, p.col, p.valid, b.per_row, v);
+            save_chunk<RAGGED>(a.saved, p.in(a.saved), p.valid, p.block, v);
     }
 };
 
 template <int TYPE, int SAVED>
 struct GeluBackwardOp {
+    static constexpr uint32_t kUnroll = SAVED == kI8 ? 2 : 1;
     typedef GeluBackwardArgs Args;
     Chunk<TYPE> d;
     Chunk<SAVED> x;
-    __device__ void load(const Args &a, const Blocks &b, const Place &p) {
-        d = load_chunk<TYPE>(a.da, p.row, p.col, p.valid, b.per_row);
-        x = load_chunk<SAVED>(a.u, p.row, p.col, p.valid, b.per_row);
+    template <bool RAGGED>
+    __device__ void load(const Args &a, const Place &p) {
+        d = load_chunk<TYPE, RAGGED>(a.da, p.in(a.da), p.valid, p.block);
+        x = load_chunk<SAVED, RAGGED>(a.u, p.in(a.u), p.valid, p.block);
     }
-    __device__ void store(const Args &a, const Blocks &, const Place &p) {
+    template <bool RAGGED>
+    __device__ void store(const Args &a, const Place &p) {
         float v[8], g[8], y[8];
         chunk_values(x, v);
         chunk_values(d, g);
@@ -156,53 +184,70 @@ struct GeluBackwardOp {
             y[e] = u * n.cdf;
         }
         if (p.valid) {
-            store_chunk<TYPE>(a.du, p.row, p.col, p.valid, make_chunk<TYPE>(g));
+            store_chunk<TYPE, RAGGED>(a.du, p.in(a.du), p.valid, make_chunk<TYPE>(g));
             if (a.a.data)
-                store_chunk<TYPE>(a.a, p.row, p.col, p.valid, make_chunk<TYPE>(y));
+                store_chunk<TYPE, RAGGED>(a.a, p.in(a.a), p.valid, make_chunk<TYPE>(y));
         }
     }
 };
 
-template <class Op>
+template <class Op, bool FLAT>
 __global__ __launch_bounds__(kThreads) void blocks_kernel(typename Op::Args args, Blocks b,
                                                           size_t first) {
-    const size_t block0 = first + (size_t)blockIdx.x * kBlocksPerWg;
-    const size_t row0 = block0 / b.per_row;
-    const uint32_t rem0 = (uint32_t)(block0 - row0 * b.per_row);
-    const size_t left = b.total - block0;
+    constexpr uint32_t kUnroll = Op::kUnroll;
+    const size_t block0 = first + (size_t)blockIdx.x * (kGroups * kUnroll);
+    size_t row0 = 0;
+    uint32_t rem0 = 0;
+    if constexpr (!FLAT) {
+        row0 = block0 / b.per_row;
+        rem0 = (uint32_t)(block0 - row0 * b.per_row);
+    }
     Op op[kUnroll];
     Place p[kUnroll];
 #pragma unroll
     for (uint32_t i = 0; i < kUnroll; ++i) {
-        p[i] = place_of(b, row0, rem0, left, (i * kThreads + threadIdx.x) / 8);
+        p[i] = place_of<FLAT>(b, block0, row0, rem0, i * kGroups + threadIdx.x / 8);
         if (p[i].valid)
-            op[i].load(args, b, p[i]);
+            op[i].template load<!FLAT>(args, p[i]);
         else
             op[i] = Op{};
     }
 #pragma unroll
     for (uint32_t i = 0; i < kUnroll; ++i)
-        op[i].store(args, b, p[i]);
+        op[i].template store<!FLAT>(args, p[i]);
 }
 
+// One launch over the matrices; `flat`: none has gaps between its rows.
 template <class Op>
-hipError_t launch_blocks(const typename Op::Args &args, size_t rows, size_t cols,
+hipError_t launch_blocks(const typename Op::Args &args, size_t rows, size_t cols, bool flat,
                          hipStream_t stream) {
+    constexpr size_t kPerGroup = (size_t)kGroups * Op::kUnroll;
     Blocks b;
-    b.rows = rows;
     b.cols = (uint32_t)cols;
     b.per_row = (uint32_t)((cols + kActBlock - 1) / kActBlock);
     b.total = rows * b.per_row;
     // ceil(2^58 / per_row), as the high half of (x << 6) * magic takes it
     b.magic = (((uint64_t)1 << 58) + b.per_row - 1) / b.per_row;
-    const size_t most = ((size_t)1 << 22) * kBlocksPerWg;
+    const size_t most = ((size_t)1 << 22) * kPerGroup;
     for (size_t first = 0; first < b.total; first += most) {
         const size_t count = b.total - first < most ? b.total - first : most;
-        const unsigned grid = (unsigned)((count + kBlocksPerWg - 1) / kBlocksPerWg);
-        hipLaunchKernelGGL((blocks_kernel<Op>), dim3(grid), dim3(kThreads), 0, stream, args, b,
-                           first);
+        const dim3 grid((unsigned)((count + kPerGroup - 1) / kPerGroup));
+        if (flat && cols % kActBlock == 0)
+            hipLaunchKernelGGL((blocks_kernel<Op, true>), grid, dim3(kThreads), 0, stream, args, b,
+                               first);
+        else
+            hipLaunchKernelGGL((blocks_kernel<Op, false>), grid, dim3(kThreads), 0, stream, args, b,
+                               first);
     }
     return hipGetLastError();
+}
+
+// Whether the rows of all matrices (those that are given) follow each other.
+bool no_gaps(size_t rows, size_t cols, std::initializer_list<const Mat *> mats) {
+    for (const Mat *m : mats)
+        if (m->data && rows > 1 && m->stride != cols)
+            return false;
+    return true;
 }
 
 }  // namespace
@@ -210,33 +255,37 @@ hipError_t launch_blocks(const typename Op::Args &args, size_t rows, size_t cols
 hipError_t launch_checkpoint_save(const Mat &x, const Mat &saved, int type, size_t rows,
                                   size_t cols, hipStream_t stream) {
     const SaveArgs a = {x, saved};
-    return type == kBf16 ? launch_blocks<SaveOp<kBf16>>(a, rows, cols, stream)
-                         : launch_blocks<SaveOp<kF32>>(a, rows, cols, stream);
+    const bool flat = no_gaps(rows, cols, {&x, &saved});
+    return type == kBf16 ? launch_blocks<SaveOp<kBf16>>(a, rows, cols, flat, stream)
+                         : launch_blocks<SaveOp<kF32>>(a, rows, cols, flat, stream);
 }
 
 hipError_t launch_checkpoint_load(const Mat &saved, const Mat &out, int type, size_t rows,
                                   size_t cols, hipStream_t stream) {
     const LoadArgs a = {saved, out};
-    return type == kBf16 ? launch_blocks<LoadOp<kBf16>>(a, rows, cols, stream)
-                         : launch_blocks<LoadOp<kF32>>(a, rows, cols, stream);
+    const bool flat = no_gaps(rows, cols, {&saved, &out});
+    return type == kBf16 ? launch_blocks<LoadOp<kBf16>>(a, rows, cols, flat, stream)
+                         : launch_blocks<LoadOp<kF32>>(a, rows, cols, flat, stream);
 }
 
 hipError_t launch_gelu_forward(const Mat &u, const Mat &a, const Mat &saved, int type, size_t rows,
                                size_t cols, hipStream_t stream) {
     const GeluForwardArgs g = {u, a, saved};
-    return type == kBf16 ? launch_blocks<GeluForwardOp<kBf16>>(g, rows, cols, stream)
-                         : launch_blocks<GeluForwardOp<kF32>>(g, rows, cols, stream);
+    const bool flat = no_gaps(rows, cols, {&u, &a, &saved});
+    return type == kBf16 ? launch_blocks<GeluForwardOp<kBf16>>(g, rows, cols, flat, stream)
+                         : launch_blocks<GeluForwardOp<kF32>>(g, rows, cols, flat, stream);
 }
 
 hipError_t launch_gelu_backward(const Mat &da, const Mat &u, const Mat &du, const Mat &a, int type,
                                 int u_type, size_t rows, size_t cols, hipStream_t stream) {
     const GeluBackwardArgs g = {da, u, du, a};
+    const bool flat = no_gaps(rows, cols, {&da, &u, &du, &a});
     if (type == kBf16)
         return u_type == kI8
-                   ? launch_blocks<GeluBackwardOp<kBf16, kI8>>(g, rows, cols, stream)
-                   : launch_blocks<GeluBackwardOp<kBf16, kBf16>>(g, rows, cols, stream);
-    return u_type == kI8 ? launch_blocks<GeluBackwardOp<kF32, kI8>>(g, rows, cols, stream)
-                         : launch_blocks<GeluBackwardOp<kF32, kF32>>(g, rows, cols, stream);
+                   ? launch_blocks<GeluBackwardOp<kBf16, kI8>>(g, rows, cols, flat, stream)
+                   : launch_blocks<GeluBackwardOp<kBf16, kBf16>>(g, rows, cols, flat, stream);
+    return u_type == kI8 ? launch_blocks<GeluBackwardOp<kF32, kI8>>(g, rows, cols, flat, stream)
+                         : launch_blocks<GeluBackwardOp<kF32, kF32>>(g, rows, cols, flat, stream);
 }
 
 }  // namespace zpp

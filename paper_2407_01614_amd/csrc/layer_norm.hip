@@ -3,8 +3,8 @@
 // A row of up to 8192 features lives in the registers of one workgroup, eight
 // consecutive elements a lane, so HBM is read once and the mean is known before
 // the squares are summed.  A row's lanes are as many as it asks for, in whole
-// waves (4544 features: 568 chunks on 576 lanes).  Longer rows are read again
-// for each sum.
+// waves (4544 features: 568 chunks on 576 lanes).  The forward pass takes rows of
+// up to 16384 so, two chunks a lane; longer rows are read again for each sum.
 //
 // RAGGED: rows whose last chunk of 8 is partial.  The lane that has it takes the
 // row's last 8 elements instead and leaves out those that are the lane's before
@@ -71,9 +71,9 @@ __device__ __forceinline__ void load_param(const void *p, int type, uint32_t col
         return;
     const Mat m = {const_cast<void *>(p), nullptr, 0};
     if (type == kF32)
-        chunk_values(load_chunk<kF32>(m, 0, col, valid, 0), x);
+        chunk_values(load_chunk<kF32>(m, col, valid, 0), x);
     else
-        chunk_values(load_chunk<kBf16>(m, 0, col, valid, 0), x);
+        chunk_values(load_chunk<kBf16>(m, col, valid, 0), x);
 }
 
 __device__ __forceinline__ uint32_t valid_at(uint32_t col, uint32_t cols) {
@@ -105,30 +105,25 @@ __device__ __forceinline__ RowLane row_lane(uint32_t lane, uint32_t cols) {
 template <int TYPE>
 __device__ __forceinline__ Chunk<TYPE> load_row(const Mat &m, size_t row, const RowLane &l,
                                                 uint32_t blocks) {
-    if constexpr (TYPE == kI8) {
-        Chunk<kI8> c;
-        c.codes = ld_nt_at<u32x2, 1>(at<uint8_t>(m, row, l.col));
-        c.exp = m.exps[row * blocks + l.block];
-        return c;
-    } else {
-        return load_chunk<TYPE, false>(m, row, l.col, 8, blocks);
-    }
+    return load_chunk<TYPE, false>(m, row * m.stride + l.col, 8, row * blocks + l.block);
 }
 
 template <int TYPE, bool RAGGED>
 __device__ __forceinline__ void store_row(const Mat &m, size_t row, const RowLane &l,
                                           const Chunk<TYPE> &c) {
+    const size_t off = row * m.stride + l.col;
     if (!RAGGED || l.first == 0) {
-        store_chunk<TYPE, false>(m, row, l.col, 8, c);
+        store_chunk<TYPE, false>(m, off, 8, c);
         return;
     }
 #pragma unroll
     for (uint32_t e = 1; e < 8; ++e)
         if (e >= l.first) {
             if constexpr (TYPE == kBf16)
-                out_at<uint16_t>(m, row, l.col)[e] = (uint16_t)(c.w[e / 2] >> (16 * (e % 2)));
+                reinterpret_cast<uint16_t *>(m.data)[off + e] =
+                    (uint16_t)(c.w[e / 2] >> (16 * (e % 2)));
             else
-                out_at<float>(m, row, l.col)[e] = e < 4 ? c.lo[e] : c.hi[e - 4];
+                reinterpret_cast<float *>(m.data)[off + e] = e < 4 ? c.lo[e] : c.hi[e - 4];
         }
 }
 
@@ -141,7 +136,7 @@ __device__ __forceinline__ void save_row(const Mat &m, size_t row, const RowLane
     if (!l.in)
         return;
     const u32x2 w = act_codes(x, exp);
-    uint8_t *p = out_at<uint8_t>(m, row, l.col);
+    uint8_t *p = reinterpret_cast<uint8_t *>(m.data) + row * m.stride + l.col;
     if (!RAGGED || l.first == 0) {
         st_nt_at<u32x2, 1>(p, w);
     } else {
@@ -181,85 +176,104 @@ __device__ __forceinline__ void norm_input(const NormForwardArgs &a, const Chunk
     }
 }
 
-// R rows a turn, blockDim.x lanes a row; the next turn's rows are on their way
-// while this turn's are summed.
-template <int TYPE, int R, bool RAGGED>
+// 1 / sqrt(v), within an ulp; v below the normal numbers is scaled up first.
+__device__ __forceinline__ float inverse_root(float v) {
+    const bool tiny = v < 0x1p-96f;
+    return __builtin_amdgcn_rsqf(tiny ? v * 0x1p64f : v) * (tiny ? 0x1p32f : 1.0f);
+}
+
+// One row a turn, V chunks a lane, the i-th `threads` lanes after the one
+// before.  With V == 1 the next row is on its way while this one's sums are made
+// and gamma and beta stay in registers; two chunks a lane leave no registers for
+// either.
+template <int TYPE, int V, bool RAGGED>
 __global__ __launch_bounds__(kMaxThreads) void norm_forward_kernel(NormForwardArgs a) {
-    __shared__ GroupSum<R> scratch;
+    __shared__ GroupSum<1> scratch;
     const uint32_t blocks = (a.cols + kActBlock - 1) / kActBlock;
     const uint32_t waves = blockDim.x / kWave;
-    const RowLane l = row_lane<RAGGED>(threadIdx.x, a.cols);
     const float per = 1.0f / (float)a.cols;
     uint32_t turn = 0;
+    RowLane l[V];
     float gamma[8], beta[8];
-    load_param(a.gamma, a.param_type, l.col, l.in ? 8 : 0, gamma);
-    load_param(a.beta, a.param_type, l.col, l.in ? 8 : 0, beta);
-    Chunk<TYPE> cx[R] = {}, cr[R] = {};
-    // rows past the last are the last again
-    auto fetch = [&](size_t row0) {
-        if (l.in) {
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const size_t row = row0 + r < a.rows ? row0 + r : a.rows - 1;
-                cx[r] = load_row<TYPE>(a.x, row, l, blocks);
-                if (a.residual.data)
-                    cr[r] = load_row<TYPE>(a.residual, row, l, blocks);
-            }
-        }
+    auto params = [&](int v) {
+        load_param(a.gamma, a.param_type, l[v].col, l[v].in ? 8 : 0, gamma);
+        load_param(a.beta, a.param_type, l[v].col, l[v].in ? 8 : 0, beta);
     };
-    const size_t step = (size_t)gridDim.x * R;
-    fetch((size_t)blockIdx.x * R);
-    for (size_t row0 = (size_t)blockIdx.x * R; row0 < a.rows; row0 += step) {
-        float x[R][8], sum[R], mean[R];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            norm_input<TYPE>(a, cx[r], cr[r], x[r], [&](const Chunk<TYPE> &t) {
-                if (l.in && row0 + r < a.rows)
-                    store_row<TYPE, RAGGED>(a.total, row0 + r, l, t);
+    for (int v = 0; v < V; ++v)
+        l[v] = row_lane<RAGGED>(v * blockDim.x + threadIdx.x, a.cols);
+    if constexpr (V == 1)
+        params(0);
+    Chunk<TYPE> cx[V] = {}, cr[V] = {};
+    auto fetch = [&](size_t row) {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (l[v].in) {
+                cx[v] = load_row<TYPE>(a.x, row, l[v], blocks);
+                if (a.residual.data)
+                    cr[v] = load_row<TYPE>(a.residual, row, l[v], blocks);
+            }
+    };
+    fetch(blockIdx.x);
+    for (size_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        float x[V][8], sum[1] = {0.0f};
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            norm_input<TYPE>(a, cx[v], cr[v], x[v], [&](const Chunk<TYPE> &t) {
+                if (l[v].in)
+                    store_row<TYPE, RAGGED>(a.total, row, l[v], t);
             });
-            clear_others<RAGGED>(x[r], l);
-            sum[r] = 0.0f;
+            clear_others<RAGGED>(x[v], l[v]);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                sum[r] += x[r][e];
+                sum[0] += x[v][e];
         }
-        if (row0 + step < a.rows)
-            fetch(row0 + step);
+        if (V == 1 && row + gridDim.x < a.rows)
+            fetch(row + gridDim.x);
         group_sum(sum, scratch, turn, 0, waves);
+        const float mean = sum[0] * per;
+        sum[0] = 0.0f;
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            mean[r] = sum[r] * per;
-            sum[r] = 0.0f;
+        for (int v = 0; v < V; ++v) {
+            float square = 0.0f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float d = x[r][e] - mean[r];
-                sum[r] += !RAGGED || (uint32_t)e >= l.first ? d * d : 0.0f;
+                const float d = x[v][e] - mean;
+                square += !RAGGED || (uint32_t)e >= l[v].first ? d * d : 0.0f;
             }
-            sum[r] = l.in ? sum[r] : 0.0f;
+            sum[0] += l[v].in ? square : 0.0f;
         }
         group_sum(sum, scratch, turn, 0, waves);
+        const float rstd = inverse_root(sum[0] * per + a.eps);
+        if (threadIdx.x == 0) {
+            if (a.mean)
+                a.mean[row] = mean;
+            if (a.rstd)
+                a.rstd[row] = rstd;
+        }
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const size_t row = row0 + r;
-            if (row >= a.rows)
-                break;
-            const float rstd = 1.0f / __builtin_sqrtf(sum[r] * per + a.eps);
-            if (threadIdx.x == 0) {
-                if (a.mean)
-                    a.mean[row] = mean[r];
-                if (a.rstd)
-                    a.rstd[row] = rstd;
-            }
+        for (int v = 0; v < V; ++v) {
             float y[8];
+            if constexpr (V > 1)
+                params(v);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                y[e] = __builtin_fmaf((x[r][e] - mean[r]) * rstd, gamma[e], beta[e]);
-            if (l.in)
-                store_row<TYPE, RAGGED>(a.y, row, l, make_chunk<TYPE>(y));
+                y[e] = __builtin_fmaf((x[v][e] - mean) * rstd, gamma[e], beta[e]);
+            if (l[v].in)
+                store_row<TYPE, RAGGED>(a.y, row, l[v], make_chunk<TYPE>(y));
             if (a.saved.data)
-                save_row<RAGGED>(a.saved, row, l, blocks, x[r]);
+                save_row<RAGGED>(a.saved, row, l[v], blocks, x[v]);
         }
+        if (V > 1 && row + gridDim.x < a.rows)
+            fetch(row + gridDim.x);
     }
+}
+
+// Elements col .. col + 7 of a row, `valid` of them inside it.
+template <int TYPE>
+__device__ __forceinline__ Chunk<TYPE> load_part(const Mat &m, size_t row, uint32_t col,
+                                                 uint32_t valid, uint32_t blocks) {
+    return load_chunk<TYPE>(m, row * m.stride + col, valid, row * blocks + col / kActBlock);
 }
 
 // Rows too long for registers: three passes over each.
@@ -279,14 +293,14 @@ __global__ __launch_bounds__(kMaxThreads) void norm_forward_long_kernel(NormForw
                 const uint32_t valid = valid_at(col, a.cols);
                 Chunk<TYPE> cx = {}, cr = {};
                 if (valid) {
-                    cx = load_chunk<TYPE>(a.x, row, col, valid, blocks);
+                    cx = load_part<TYPE>(a.x, row, col, valid, blocks);
                     if (a.residual.data)
-                        cr = load_chunk<TYPE>(a.residual, row, col, valid, blocks);
+                        cr = load_part<TYPE>(a.residual, row, col, valid, blocks);
                 }
                 float x[8];
                 norm_input<TYPE>(a, cx, cr, x, [&](const Chunk<TYPE> &t) {
                     if (pass == 2 && valid)
-                        store_chunk<TYPE>(a.total, row, col, valid, t);
+                        store_chunk<TYPE>(a.total, row * a.total.stride + col, valid, t);
                 });
                 if (pass < 2) {
 #pragma unroll
@@ -302,9 +316,10 @@ __global__ __launch_bounds__(kMaxThreads) void norm_forward_long_kernel(NormForw
                     for (int e = 0; e < 8; ++e)
                         y[e] = __builtin_fmaf((x[e] - mean) * rstd, gamma[e], beta[e]);
                     if (valid)
-                        store_chunk<TYPE>(a.y, row, col, valid, make_chunk<TYPE>(y));
+                        store_chunk<TYPE>(a.y, row * a.y.stride + col, valid, make_chunk<TYPE>(y));
                     if (a.saved.data)
-                        save_chunk(a.saved, row, col, valid, blocks, x);
+                        save_chunk(a.saved, row * a.saved.stride + col, valid,
+                                   row * blocks + col / kActBlock, x);
                 }
             }
             if (pass == 2)
@@ -313,7 +328,7 @@ __global__ __launch_bounds__(kMaxThreads) void norm_forward_long_kernel(NormForw
             if (pass == 0)
                 mean = sum[0] / (float)a.cols;
             else
-                rstd = 1.0f / __builtin_sqrtf(sum[0] / (float)a.cols + a.eps);
+                rstd = inverse_root(sum[0] / (float)a.cols + a.eps);
         }
         if (threadIdx.x == 0) {
             if (a.mean)
@@ -337,8 +352,6 @@ struct RowShape {
     uint32_t grid;     // its workgroups, pairs of arrays in the workspace
 };
 
-constexpr uint32_t kRowsAtOnce = 1;  // rows of a team in a turn
-
 RowShape row_shape(size_t rows, size_t cols) {
     RowShape s = {0, 0, 0};
     if (cols > kMostRegCols || cols < 8)
@@ -346,16 +359,18 @@ RowShape row_shape(size_t rows, size_t cols) {
     const size_t chunks = (cols + 7) / 8;
     s.threads = (uint32_t)((chunks + kWave - 1) / kWave * kWave);
     s.teams = kMaxThreads / s.threads;
-    const size_t groups = (rows + s.teams * kRowsAtOnce - 1) / (s.teams * kRowsAtOnce);
+    const size_t groups = (rows + s.teams - 1) / s.teams;
     s.grid = (uint32_t)(groups < kCus ? groups : kCus);
     return s;
 }
 
-template <int TYPE, int X, int R, bool AGAIN, bool RAGGED>
+// One row of each team a turn; the next turn's are on their way while this one's
+// are summed.
+template <int TYPE, int X, bool AGAIN, bool RAGGED>
 __global__ __launch_bounds__(kMaxThreads) void norm_backward_kernel(NormBackwardArgs a,
                                                                     uint32_t threads,
                                                                     uint32_t teams) {
-    __shared__ GroupSum<2 * R> scratch;
+    __shared__ GroupSum<2> scratch;
     // gamma (and beta) in fp32, then, where a workgroup has several teams, the
     // join of their sums
     extern __shared__ float shared[];
@@ -370,8 +385,8 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward_kernel(NormBackward
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         dg[e] = db[e] = 0.0f;
-    // gamma and beta as two halves of four features a lane, so that neighbouring
-    // lanes read neighbouring 16 bytes
+    // as two halves of four features a lane, so that neighbouring lanes read
+    // neighbouring 16 bytes
     f32x4 *const params = reinterpret_cast<f32x4 *>(shared) + lane;
     auto param = [&](int which, float (&v)[8]) {
 #pragma unroll
@@ -392,91 +407,73 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward_kernel(NormBackward
         }
     }
     __syncthreads();
-    // the next turn's rows as loaded
-    Chunk<TYPE> nd[R] = {}, nr[R] = {};
-    Chunk<X> nx[R] = {};
-    float mean[R], rstd[R];
-    // Rows past the last are zeros, and so are their means and factors: they add
-    // nothing to any sum.
-    auto fetch = [&](size_t row0) {
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            if (row0 + r < a.rows) {
-                if (l.in) {
-                    nd[r] = load_row<TYPE>(a.dy, row0 + r, l, blocks);
-                    nx[r] = load_row<X>(a.x, row0 + r, l, blocks);
-                    if (a.dresidual.data)
-                        nr[r] = load_row<TYPE>(a.dresidual, row0 + r, l, blocks);
-                }
-                mean[r] = a.mean[row0 + r];
-                rstd[r] = a.rstd[row0 + r];
-            } else {
-                nd[r] = Chunk<TYPE>{};
-                nx[r] = Chunk<X>{};
-                mean[r] = rstd[r] = 0.0f;
+    Chunk<TYPE> nd = {}, nr = {};
+    Chunk<X> nx = {};
+    float stat[2] = {0.0f, 0.0f};  // the next row's mean and factor
+    // A row past the last is zeros, and so are its mean and factor: it adds nothing
+    // to any sum.
+    auto fetch = [&](size_t row) {
+        if (row < a.rows) {
+            if (l.in) {
+                nd = load_row<TYPE>(a.dy, row, l, blocks);
+                nx = load_row<X>(a.x, row, l, blocks);
+                if (a.dresidual.data)
+                    nr = load_row<TYPE>(a.dresidual, row, l, blocks);
             }
+            stat[0] = a.mean[row];
+            stat[1] = a.rstd[row];
+        } else {
+            nd = Chunk<TYPE>{};
+            nx = Chunk<X>{};
+            stat[0] = stat[1] = 0.0f;
         }
     };
     // every team takes as many turns, so that all meet at the barriers
-    const size_t step = (size_t)gridDim.x * teams * R;
-    const size_t mine = (size_t)team * R;
-    fetch((size_t)blockIdx.x * teams * R + mine);
-    for (size_t base = (size_t)blockIdx.x * teams * R; base < a.rows; base += step) {
-        const size_t row0 = base + mine;
-        Chunk<TYPE> cr[R];
-        float s[2 * R], g[R][8], h[R][8], scale[R];
+    const size_t step = (size_t)gridDim.x * teams;
+    fetch((size_t)blockIdx.x * teams + team);
+    for (size_t base = (size_t)blockIdx.x * teams; base < a.rows; base += step) {
+        const size_t row = base + team;
+        const Chunk<TYPE> cr = nr;
+        const float mean = stat[0], scale = stat[1];
+        float s[2] = {0.0f, 0.0f}, d[8], g[8], h[8];
+        chunk_values(nd, d);
+        clear_others<RAGGED>(d, l);
+        chunk_values(nx, h);
+        param(0, g);
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            float d[8];
-            chunk_values(nd[r], d);
-            clear_others<RAGGED>(d, l);
-            chunk_values(nx[r], h[r]);
-            param(0, g[r]);
-            scale[r] = rstd[r];
-            cr[r] = nr[r];
-            s[2 * r] = s[2 * r + 1] = 0.0f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                h[r][e] = (h[r][e] - mean[r]) * scale[r];
-                dg[e] = __builtin_fmaf(d[e], h[r][e], dg[e]);
-                db[e] += d[e];
-                g[r][e] *= d[e];
-                s[2 * r] += g[r][e];
-                s[2 * r + 1] = __builtin_fmaf(g[r][e], h[r][e], s[2 * r + 1]);
-            }
+        for (int e = 0; e < 8; ++e) {
+            h[e] = (h[e] - mean) * scale;
+            dg[e] = __builtin_fmaf(d[e], h[e], dg[e]);
+            db[e] += d[e];
+            g[e] *= d[e];
+            s[0] += g[e];
+            s[1] = __builtin_fmaf(g[e], h[e], s[1]);
         }
         if (base + step < a.rows)
-            fetch(row0 + step);
+            fetch(row + step);
         group_sum(s, scratch, turn, wave0, waves);
-        if (!l.in)
+        if (!l.in || row >= a.rows)
             continue;
+        const float c1 = s[0] * per, c2 = s[1] * per;
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const size_t row = row0 + r;
-            if (row >= a.rows)
-                break;
-            const float c1 = s[2 * r] * per, c2 = s[2 * r + 1] * per;
-            float d[8];
+        for (int e = 0; e < 8; ++e)
+            d[e] = scale * __builtin_fmaf(-h[e], c2, g[e] - c1);
+        if (a.dresidual.data) {
+            float past[8];
+            chunk_values(cr, past);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                d[e] = scale[r] * __builtin_fmaf(-h[r][e], c2, g[r][e] - c1);
-            if (a.dresidual.data) {
-                float past[8];
-                chunk_values(cr[r], past);
+                d[e] += past[e];
+        }
+        store_row<TYPE, RAGGED>(a.dx, row, l, make_chunk<TYPE>(d));
+        if constexpr (AGAIN) {
+            float w[8], y[8];
+            param(0, w);
+            param(1, y);
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    d[e] += past[e];
-            }
-            store_row<TYPE, RAGGED>(a.dx, row, l, make_chunk<TYPE>(d));
-            if constexpr (AGAIN) {
-                float w[8], y[8];
-                param(0, w);
-                param(1, y);
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    y[e] = __builtin_fmaf(h[r][e], w[e], y[e]);
-                store_row<TYPE, RAGGED>(a.y, row, l, make_chunk<TYPE>(y));
-            }
+            for (int e = 0; e < 8; ++e)
+                y[e] = __builtin_fmaf(h[e], w[e], y[e]);
+            store_row<TYPE, RAGGED>(a.y, row, l, make_chunk<TYPE>(y));
         }
     }
     if (!a.partials)
@@ -524,8 +521,8 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward_long_sums(NormBackw
             if (!valid)
                 continue;
             float d[8], h[8], gamma[8];
-            chunk_values(load_chunk<TYPE>(a.dy, row, col, valid, blocks), d);
-            chunk_values(load_chunk<X>(a.x, row, col, valid, blocks), h);
+            chunk_values(load_part<TYPE>(a.dy, row, col, valid, blocks), d);
+            chunk_values(load_part<X>(a.x, row, col, valid, blocks), h);
             load_param(a.gamma, a.param_type, col, valid, gamma);
 #pragma unroll
             for (uint32_t e = 0; e < 8; ++e) {
@@ -557,14 +554,24 @@ __global__ __launch_bounds__(kStripThreads) void norm_backward_long_kernel(NormB
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         dg[e] = db[e] = 0.0f;
+    Chunk<TYPE> nd, nr = {};
+    Chunk<X> nx;
+    auto fetch = [&](size_t row) {
+        nd = load_part<TYPE>(a.dy, row, col, valid, blocks);
+        nx = load_part<X>(a.x, row, col, valid, blocks);
+        if (a.dresidual.data)
+            nr = load_part<TYPE>(a.dresidual, row, col, valid, blocks);
+    };
+    fetch(blockIdx.y);
     for (size_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
         const float mean = a.mean[row], rstd = a.rstd[row];
         const float c1 = a.partials[2 * row], c2 = a.partials[2 * row + 1];
         float d[8], h[8], y[8], past[8];
-        chunk_values(load_chunk<TYPE>(a.dy, row, col, valid, blocks), d);
-        chunk_values(load_chunk<X>(a.x, row, col, valid, blocks), h);
-        if (a.dresidual.data)
-            chunk_values(load_chunk<TYPE>(a.dresidual, row, col, valid, blocks), past);
+        chunk_values(nd, d);
+        chunk_values(nx, h);
+        chunk_values(nr, past);
+        if (row + gridDim.y < a.rows)
+            fetch(row + gridDim.y);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             h[e] = (h[e] - mean) * rstd;
@@ -575,9 +582,9 @@ __global__ __launch_bounds__(kStripThreads) void norm_backward_long_kernel(NormB
             if (a.dresidual.data)
                 d[e] += past[e];
         }
-        store_chunk<TYPE>(a.dx, row, col, valid, make_chunk<TYPE>(d));
+        store_chunk<TYPE>(a.dx, row * a.dx.stride + col, valid, make_chunk<TYPE>(d));
         if (a.y.data)
-            store_chunk<TYPE>(a.y, row, col, valid, make_chunk<TYPE>(y));
+            store_chunk<TYPE>(a.y, row * a.y.stride + col, valid, make_chunk<TYPE>(y));
     }
     if (!a.dgamma && !a.dbeta)
         return;
@@ -663,10 +670,10 @@ void start_backward(const NormBackwardArgs &a, const RowShape &s, hipStream_t st
     const size_t lds = 2 * sizeof(float) * s.threads * 8;
     const dim3 grid(s.grid), threads(s.threads * s.teams);
     if (a.cols % 8)
-        hipLaunchKernelGGL((norm_backward_kernel<TYPE, X, kRowsAtOnce, AGAIN, true>), grid, threads,
+        hipLaunchKernelGGL((norm_backward_kernel<TYPE, X, AGAIN, true>), grid, threads,
                            lds, stream, a, s.threads, s.teams);
     else
-        hipLaunchKernelGGL((norm_backward_kernel<TYPE, X, kRowsAtOnce, AGAIN, false>), grid,
+        hipLaunchKernelGGL((norm_backward_kernel<TYPE, X, AGAIN, false>), grid,
                            threads, lds, stream, a, s.threads, s.teams);
 }
 
@@ -690,30 +697,35 @@ void start_backward(const NormBackwardArgs &a, const RowShape &s, hipStream_t st
 
 }  // namespace
 
+namespace {
+
+template <int TYPE, int V>
+void start_forward(const NormForwardArgs &a, hipStream_t stream) {
+    const size_t lanes = ((size_t)a.cols + 8 * V - 1) / (8 * V);
+    const uint32_t threads = (uint32_t)((lanes + kWave - 1) / kWave * kWave);
+    // the lanes that the GPU holds at once: 2048 a CU up to 64 registers
+    const size_t fit = (size_t)kCus * ((V == 1 ? 2048 : 1024) / threads);
+    const dim3 grid((unsigned)(a.rows < fit ? a.rows : fit));
+    if (a.cols % 8)
+        hipLaunchKernelGGL((norm_forward_kernel<TYPE, V, true>), grid, dim3(threads), 0, stream, a);
+    else
+        hipLaunchKernelGGL((norm_forward_kernel<TYPE, V, false>), grid, dim3(threads), 0, stream,
+                           a);
+}
+
+}  // namespace
+
 hipError_t launch_norm_forward(const NormForwardArgs &a, int type, hipStream_t stream) {
-    const uint32_t threads = row_shape(a.rows, a.cols).threads;
     return with_type(type, [&](auto t) {
         constexpr int T = decltype(t)::value;
-        if (!threads) {
+        if (a.cols < 8 || a.cols > 2 * kMostRegCols)
             hipLaunchKernelGGL((norm_forward_long_kernel<T>),
                                dim3((unsigned)(a.rows < 2 * kCus ? a.rows : 2 * kCus)),
                                dim3(kMaxThreads), 0, stream, a);
-            return;
-        }
-        // workgroups that the GPU holds at once, at the 128 registers a lane that
-        // workgroups of 1024 leave; two rows a turn where there are rows for all
-        const size_t fit = (size_t)kCus * (1024 / threads);
-        const dim3 grid((unsigned)(a.rows < fit ? a.rows : fit));
-        if (a.cols % 8 && a.rows < 2 * fit)
-            hipLaunchKernelGGL((norm_forward_kernel<T, 1, true>), grid, dim3(threads), 0, stream, a);
-        else if (a.cols % 8)
-            hipLaunchKernelGGL((norm_forward_kernel<T, 2, true>), grid, dim3(threads), 0, stream, a);
-        else if (a.rows < 2 * fit)
-            hipLaunchKernelGGL((norm_forward_kernel<T, 1, false>), grid, dim3(threads), 0, stream,
-                               a);
+        else if (a.cols <= kMostRegCols)
+            start_forward<T, 1>(a, stream);
         else
-            hipLaunchKernelGGL((norm_forward_kernel<T, 2, false>), grid, dim3(threads), 0, stream,
-                               a);
+            start_forward<T, 2>(a, stream);
     });
 }
 

@@ -27,32 +27,30 @@ struct Chunk<kI8> {
     uint32_t exp;
 };
 
-// A vector at an address aligned to A bytes, of memory that is read again.
+// A vector at an address aligned to A bytes, as an ordinary access.
 template <class V, int A>
 __device__ __forceinline__ V ld_at(const void *p) {
     typedef V U __attribute__((aligned(A)));
     return *reinterpret_cast<const U *>(p);
 }
-
-template <class E>
-__device__ __forceinline__ const E *at(const Mat &m, size_t row, uint32_t col) {
-    return reinterpret_cast<const E *>(m.data) + row * m.stride + col;
-}
-template <class E>
-__device__ __forceinline__ E *out_at(const Mat &m, size_t row, uint32_t col) {
-    return reinterpret_cast<E *>(m.data) + row * m.stride + col;
+template <class V, int A>
+__device__ __forceinline__ void st_at(void *p, V v) {
+    typedef V U __attribute__((aligned(A)));
+    *reinterpret_cast<U *>(p) = v;
 }
 
-// Elements col .. col+7 of a row with `valid` >= 1 of them inside it (those
-// past them read as the row's last).  A row's last, partial chunk takes single
-// loads at clamped columns, which do not wait for each other; RAGGED false:
-// there is none, `valid` is 8.
+// Eight elements at p, `valid` >= 1 of them inside the row (those past them read
+// as the row's last).  A row's last, partial chunk takes single loads at clamped
+// places, which do not wait for each other; RAGGED false: there is none, `valid`
+// is 8.  Codes are read as ordinary, temporal loads: 8 bytes a lane, they left
+// half of each line's fetch behind as streaming ones (8192x8192 read back: 34.8
+// us, 29.4 so).
 template <int TYPE, bool RAGGED = true>
-__device__ __forceinline__ Chunk<TYPE> load_chunk(const Mat &m, size_t row, uint32_t col,
-                                                  uint32_t valid, uint32_t blocks) {
+__device__ __forceinline__ Chunk<TYPE> load_chunk(const Mat &m, size_t off, uint32_t valid,
+                                                  size_t block) {
     Chunk<TYPE> c;
     if constexpr (TYPE == kBf16) {
-        const uint16_t *p = at<uint16_t>(m, row, col);
+        const uint16_t *p = reinterpret_cast<const uint16_t *>(m.data) + off;
         if (!RAGGED || valid >= 8) {
             c.w = ld_nt_at<u32x4, 2>(p);
         } else {
@@ -62,7 +60,7 @@ __device__ __forceinline__ Chunk<TYPE> load_chunk(const Mat &m, size_t row, uint
                          ((uint32_t)p[clamped(2 * e + 1, valid)] << 16);
         }
     } else if constexpr (TYPE == kF32) {
-        const float *p = at<float>(m, row, col);
+        const float *p = reinterpret_cast<const float *>(m.data) + off;
         if (!RAGGED || valid >= 8) {
             c.lo = ld_nt_at<f32x4, 4>(p);
             c.hi = ld_nt_at<f32x4, 4>(p + 4);
@@ -74,16 +72,16 @@ __device__ __forceinline__ Chunk<TYPE> load_chunk(const Mat &m, size_t row, uint
             }
         }
     } else {
-        const uint8_t *p = at<uint8_t>(m, row, col);
+        const uint8_t *p = reinterpret_cast<const uint8_t *>(m.data) + off;
         if (!RAGGED || valid >= 8) {
-            c.codes = ld_nt_at<u32x2, 1>(p);
+            c.codes = ld_at<u32x2, 1>(p);
         } else {
             c.codes = u32x2{0, 0};
 #pragma unroll
             for (uint32_t e = 0; e < 8; ++e)
                 c.codes[e / 4] |= (uint32_t)p[clamped(e, valid)] << (8 * (e % 4));
         }
-        c.exp = m.exps[row * blocks + col / kActBlock];
+        c.exp = m.exps[block];
     }
     return c;
 }
@@ -147,12 +145,15 @@ __device__ __forceinline__ Chunk<TYPE> make_chunk(const float (&x)[8]) {
     return c;
 }
 
-// Stores the first `valid` >= 1 elements of the chunk.
+// Stores the first `valid` >= 1 elements of the chunk.  fp32 is stored as
+// ordinary, temporal: a lane's two halves are 16 bytes each, and streaming stores
+// of every other 16 bytes did not meet in the L2 (a checkpoint read back as
+// 8192x8192 fp32: 91 us, 69 so).
 template <int TYPE, bool RAGGED = true>
-__device__ __forceinline__ void store_chunk(const Mat &m, size_t row, uint32_t col, uint32_t valid,
+__device__ __forceinline__ void store_chunk(const Mat &m, size_t off, uint32_t valid,
                                             const Chunk<TYPE> &c) {
     if constexpr (TYPE == kBf16) {
-        uint16_t *p = out_at<uint16_t>(m, row, col);
+        uint16_t *p = reinterpret_cast<uint16_t *>(m.data) + off;
         if (!RAGGED || valid >= 8) {
             st_nt_at<u32x4, 2>(p, c.w);
         } else {
@@ -162,10 +163,10 @@ __device__ __forceinline__ void store_chunk(const Mat &m, size_t row, uint32_t c
                     p[e] = (uint16_t)(c.w[e / 2] >> (16 * (e % 2)));
         }
     } else {
-        float *p = out_at<float>(m, row, col);
+        float *p = reinterpret_cast<float *>(m.data) + off;
         if (!RAGGED || valid >= 8) {
-            st_nt_at<f32x4, 4>(p, c.lo);
-            st_nt_at<f32x4, 4>(p + 4, c.hi);
+            st_at<f32x4, 4>(p, c.lo);
+            st_at<f32x4, 4>(p + 4, c.hi);
         } else {
 #pragma unroll
             for (uint32_t e = 0; e < 8; ++e)
@@ -259,12 +260,12 @@ __device__ __forceinline__ u32x2 act_codes(const float (&x)[8], uint32_t exp) {
 // Writes the checkpoint of the elements that the 8 lanes of a block hold.  All
 // 8 lanes take part, with `valid` 0 where a lane is past the row's end.
 template <bool RAGGED = true>
-__device__ __forceinline__ void save_chunk(const Mat &m, size_t row, uint32_t col, uint32_t valid,
-                                           uint32_t blocks, const float (&x)[8]) {
-    const uint32_t exp = act_exp(max8(max_bits(x, valid)));
+__device__ __forceinline__ void save_chunk(const Mat &m, size_t off, uint32_t valid, size_t block,
+                                           const float (&x)[8]) {
+    const uint32_t exp = act_exp(max8(max_bits(x, RAGGED ? valid : 8)));
     if (valid) {
         const u32x2 w = act_codes(x, exp);
-        uint8_t *p = out_at<uint8_t>(m, row, col);
+        uint8_t *p = reinterpret_cast<uint8_t *>(m.data) + off;
         if (!RAGGED || valid >= 8) {
             st_nt_at<u32x2, 1>(p, w);
         } else {
@@ -273,8 +274,8 @@ __device__ __forceinline__ void save_chunk(const Mat &m, size_t row, uint32_t co
                 if (e < valid)
                     p[e] = (uint8_t)(w[e / 4] >> (8 * (e % 4)));
         }
-        if ((col & (kActBlock - 1)) == 0)
-            m.exps[row * blocks + col / kActBlock] = (uint8_t)exp;
+        if ((threadIdx.x & 7) == 0)
+            m.exps[block] = (uint8_t)exp;
     }
 }
 
