@@ -20,15 +20,21 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr uint32_t kStep = 64;  // tokens a turn
+// Elements between tokens up to which a turn's offsets (64 tokens of 2 bytes an
+// element) are 32 bits; tokens further apart are fetched one by one.
+constexpr size_t kNear = (size_t)1 << 24;
 
 struct WeightGradArgs {
     Mat dy, x;
-    float *out;         // dw, or the workspace's [splits][n][k]
-    size_t out_stride;  // between rows
-    size_t out_split;   // between splits
+    float *dw;
+    size_t dw_stride;
+    float *parts;  // the workspace: [splits][tail tiles][tile][tile]
     size_t rows, split_rows;
     uint32_t n, k, tiles_n, tiles_k;
+    uint32_t whole;   // tiles whose tokens one workgroup takes all
+    uint32_t splits;  // of the tokens of the tiles after those
     int accumulate;
+    int near;  // a turn's tokens lie within 32-bit offsets of each other
 };
 
 // 4 tokens by 8 features as fetched.
@@ -43,11 +49,13 @@ struct Piece {
 // stored.
 template <int TYPE>
 struct Operand {
-    const uint8_t *data;  // of token 0, the same in all lanes
+    const uint8_t *data;  // of token 0
     const uint8_t *exps;
     size_t pitch;         // bytes between tokens
     uint32_t blocks;      // exponents between tokens
-    uint32_t at, exp_at;  // the lane's bytes and exponents past the turn's first token
+    uint32_t col;         // the lane's bytes into a token
+    uint32_t at, exp_at;  // its bytes and exponents past a turn's first token
+    uint32_t block;       // its exponent's place in a token
     uint32_t valid;       // elements of its chunk inside the row
     uint32_t margin;      // tokens before the matrix's end whose chunks may pass it
 };
@@ -63,75 +71,75 @@ __device__ __forceinline__ Operand<TYPE> operand(const Mat &m, uint32_t cols, ui
     o.exps = m.exps;
     o.pitch = m.stride * kSize;
     o.blocks = (cols + kActBlock - 1) / kActBlock;
-    o.at = token * (uint32_t)o.pitch + col * kSize;
-    o.exp_at = token * o.blocks + col / kActBlock;
+    o.col = col * kSize;
+    o.block = col / kActBlock;
+    o.at = token * (uint32_t)o.pitch + o.col;
+    o.exp_at = token * o.blocks + o.block;
     o.valid = cols - col < 8 ? cols - col : 8;
     // the last chunk ends last + 8 - cols elements past its row
     o.margin = cols % 8 ? (uint32_t)((last + 8 - cols + m.stride - 1) / m.stride) : 0;
     return o;
 }
 
-// Memory at an address that is the same in all lanes, told to be global memory
-// and kept in scalar registers: loads add the lane's 32-bit offset themselves.
-#define ZPP_GLOBAL __attribute__((address_space(1)))
-typedef const ZPP_GLOBAL uint8_t *GlobalBytes;
-__device__ __forceinline__ GlobalBytes uniform(const uint8_t *p) {
-    const uint64_t u = reinterpret_cast<uint64_t>(p);
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)u);
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(u >> 32));
-    return reinterpret_cast<GlobalBytes>((uint64_t)hi << 32 | lo);
-}
-template <class V, int A>
-__device__ __forceinline__ V ld_uniform(const uint8_t *base, uint32_t offset) {
-    typedef V U __attribute__((aligned(A)));
-    return *reinterpret_cast<const ZPP_GLOBAL U *>(uniform(base) + offset);
-}
-
-__device__ __forceinline__ void fetch_chunk(Chunk<kBf16> &c, const Operand<kBf16> &o, size_t token) {
-    c.w = ld_at<u32x4, 2>(o.data + token * o.pitch + o.at);
-}
-__device__ __forceinline__ void fetch_chunk(Chunk<kI8> &c, const Operand<kI8> &o, size_t token) {
-    c.codes = ld_uniform<u32x2, 1>(o.data + token * o.pitch, o.at);
-    c.exp = ld_uniform<uint8_t, 1>(o.exps + token * o.blocks, o.exp_at);
+// Memory from an address that is the same in all lanes: the address and the
+// distance between tokens stay in scalar registers, and a lane adds its 32 bits.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t memory_at(const uint8_t *p) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(p), 0, -1, 0x00027000);
 }
 
 // A turn whose tokens all lie `margin` and more before the matrix's end: whole
 // chunks, which end inside the matrix.
-template <int TYPE>
-__device__ __forceinline__ void fetch(Piece<TYPE> &p, const Operand<TYPE> &o, size_t token) {
+__device__ __forceinline__ void fetch(Piece<kBf16> &p, const Operand<kBf16> &o, size_t token) {
+    const __amdgpu_buffer_rsrc_t m = memory_at(o.data + token * o.pitch);
 #pragma unroll
     for (uint32_t i = 0; i < 4; ++i)
-        fetch_chunk(p.t[i], o, token + i);
+        p.t[i].w = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                                 m, o.at, i * (uint32_t)o.pitch, 0));
+}
+__device__ __forceinline__ void fetch(Piece<kI8> &p, const Operand<kI8> &o, size_t token) {
+    const __amdgpu_buffer_rsrc_t m = memory_at(o.data + token * o.pitch);
+    const __amdgpu_buffer_rsrc_t e = memory_at(o.exps + token * o.blocks);
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) {
+        p.t[i].codes = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(
+                                                     m, o.at, i * (uint32_t)o.pitch, 0));
+        p.t[i].exp = __builtin_amdgcn_raw_buffer_load_b8(e, o.exp_at, i * o.blocks, 0);
+    }
 }
 
-// A row's last elements where a whole chunk would pass the matrix's end.
-__device__ __forceinline__ void fetch_part(Chunk<kBf16> &c, const Operand<kBf16> &o, size_t token) {
-    const uint16_t *p = reinterpret_cast<const uint16_t *>(o.data + token * o.pitch + o.at);
+// A token's chunk by itself: whole, or, where that would pass the matrix's end,
+// its `valid` elements one by one.
+__device__ __forceinline__ void fetch_token(Chunk<kBf16> &c, const Operand<kBf16> &o, size_t token,
+                                            bool all) {
+    const uint16_t *p = reinterpret_cast<const uint16_t *>(o.data + token * o.pitch + o.col);
+    if (all) {
+        c.w = ld_at<u32x4, 2>(p);
+        return;
+    }
     for (uint32_t e = 0; e < o.valid; ++e)
         c.w[e / 2] |= (uint32_t)p[e] << (16 * (e % 2));
 }
-__device__ __forceinline__ void fetch_part(Chunk<kI8> &c, const Operand<kI8> &o, size_t token) {
-    const uint8_t *p = o.data + token * o.pitch + o.at;
+__device__ __forceinline__ void fetch_token(Chunk<kI8> &c, const Operand<kI8> &o, size_t token,
+                                            bool all) {
+    const uint8_t *p = o.data + token * o.pitch + o.col;
+    c.exp = o.exps[token * o.blocks + o.block];
+    if (all) {
+        c.codes = ld_at<u32x2, 1>(p);
+        return;
+    }
     for (uint32_t e = 0; e < o.valid; ++e)
         c.codes[e / 4] |= (uint32_t)p[e] << (8 * (e % 4));
-    c.exp = (o.exps + token * o.blocks)[o.exp_at];
 }
 
-// A turn at the end: tokens from `end` on are zeros.  `mine`: the lane's first
-// token in the turn (which `at` holds as well).
+// A turn at the end: tokens from `end` on are zeros.  `token`: the lane's first.
 template <int TYPE>
 __device__ __forceinline__ void fetch_end(Piece<TYPE> &p, const Operand<TYPE> &o, size_t token,
-                                          uint32_t mine, size_t end, size_t rows) {
+                                          size_t end, size_t rows) {
 #pragma unroll
     for (uint32_t i = 0; i < 4; ++i) {
         p.t[i] = Chunk<TYPE>{};
-        const size_t t = token + mine + i;
-        if (t < end) {
-            if (t + o.margin < rows || o.valid == 8)
-                fetch_chunk(p.t[i], o, token + i);
-            else
-                fetch_part(p.t[i], o, token + i);
-        }
+        if (token + i < end)
+            fetch_token(p.t[i], o, token + i, o.valid == 8 || token + i + o.margin < rows);
     }
 }
 
@@ -196,15 +204,18 @@ __device__ __forceinline__ void put_half(uint8_t *tile, const Piece<TYPE> &p, ui
             turned(p, e, scale);
 }
 
-// Workgroup w's tile.  The dispatcher deals workgroups to the 8 XCDs in turn;
-// each XCD takes a run of consecutive tiles, ordered in bands of kBand tile rows,
-// so that the 32 tiles an XCD works on at a time share few rows and columns in
-// its L2.
+// The dispatcher deals workgroups to the 8 XCDs in turn; each XCD takes a run of
+// consecutive places of the `count` in a launch.
+__device__ __forceinline__ uint32_t xcd_run(uint32_t w, uint32_t count) {
+    const uint32_t xcd = w % 8, q = count / 8, r = count % 8;
+    return xcd * q + (xcd < r ? xcd : r) + w / 8;
+}
+
+// Tile t.  Tiles are ordered in bands of kBand tile rows, so that the 32 that an
+// XCD works on at a time share few rows and columns in its L2.
 constexpr uint32_t kBand = 8;
-__device__ __forceinline__ void tile_of_group(uint32_t w, uint32_t tiles_n, uint32_t tiles_k,
-                                              uint32_t &tile_n, uint32_t &tile_k) {
-    const uint32_t total = tiles_n * tiles_k, xcd = w % 8, q = total / 8, r = total % 8;
-    const uint32_t t = xcd * q + (xcd < r ? xcd : r) + w / 8;
+__device__ __forceinline__ void tile_at(uint32_t t, uint32_t tiles_n, uint32_t tiles_k,
+                                        uint32_t &tile_n, uint32_t &tile_k) {
     const uint32_t band = t / (kBand * tiles_k), first = band * kBand;
     const uint32_t high = tiles_n - first < kBand ? tiles_n - first : kBand;
     const uint32_t at = t - first * tiles_k;
@@ -221,11 +232,22 @@ __global__ __launch_bounds__(WAVES_N *WAVES_K *kWave) void weight_grad_kernel(We
     constexpr uint32_t kApart = kStep / kPieces;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];  // [2 turns][2 operands][kBytes]
     const uint32_t tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-    uint32_t tile_n, tile_k;
-    tile_of_group(blockIdx.x, a.tiles_n, a.tiles_k, tile_n, tile_k);
+    // the whole tiles first, then the splits of the tail's, split by split
+    const bool whole = blockIdx.x < a.whole;
+    const uint32_t tail = a.tiles_n * a.tiles_k - a.whole;
+    uint32_t tile, split = 0, tile_n, tile_k;
+    if (whole) {
+        tile = xcd_run(blockIdx.x, a.whole);
+    } else {
+        const uint32_t at = xcd_run(blockIdx.x - a.whole, tail * a.splits);
+        split = at / tail;
+        tile = a.whole + at % tail;
+    }
+    tile_at(tile, a.tiles_n, a.tiles_k, tile_n, tile_k);
     const uint32_t n0 = tile_n * TILE, k0 = tile_k * TILE;
-    const size_t begin = (size_t)blockIdx.y * a.split_rows;
-    const size_t end = begin + a.split_rows < a.rows ? begin + a.split_rows : a.rows;
+    const size_t tokens = whole ? a.rows : a.split_rows;
+    const size_t begin = split * tokens;
+    const size_t end = begin + tokens < a.rows ? begin + tokens : a.rows;
 
     // the lane's piece: neighbouring lanes take the two halves of a unit
     const uint32_t chunk = chunk_of<TILE>(tid / 2 % kChunks), group = tid % 2 + 2 * (tid / (2 * kChunks));
@@ -278,28 +300,52 @@ __global__ __launch_bounds__(WAVES_N *WAVES_K *kWave) void weight_grad_kernel(We
         put_x(buffer, low);
         put_x(buffer, high);
     };
-    bf16x8 fd[2][MN], fx[2][MK];
-    auto read = [&](uint32_t buffer, uint32_t kk, auto set) {
+    bf16x8 fd[MN], fx[2][MK];
+    auto read_x = [&](uint32_t buffer, uint32_t kk, auto set) {
         constexpr int S = decltype(set)::value;
-        const uint8_t *from = lds + buffer * (2 * kBytes);
-        const uint32_t unit = kk * 2 + lane / 32;
+        const uint8_t *from = lds + buffer * (2 * kBytes) + kBytes;
 #pragma unroll
         for (int j = 0; j < MK; ++j)
             fx[S][j] = *reinterpret_cast<const bf16x8 *>(
-                from + kBytes + unit_at<TILE>(wk + j * 32 + lane % 32, unit));
-#pragma unroll
-        for (int i = 0; i < MN; ++i)
-            fd[S][i] = *reinterpret_cast<const bf16x8 *>(
-                from + unit_at<TILE>(wn + i * 32 + lane % 32, unit));
+                from + unit_at<TILE>(wk + j * 32 + lane % 32, kk * 2 + lane / 32));
     };
-    auto multiply = [&](auto set) {
-        constexpr int S = decltype(set)::value;
+    auto read_dy = [&](uint32_t buffer, uint32_t kk, int i) {
+        const uint8_t *from = lds + buffer * (2 * kBytes);
+        fd[i] = *reinterpret_cast<const bf16x8 *>(
+            from + unit_at<TILE>(wn + i * 32 + lane % 32, kk * 2 + lane / 32));
+    };
+    auto read = [&](uint32_t buffer, uint32_t kk, auto set) {
+        read_x(buffer, kk, set);
 #pragma unroll
         for (int i = 0; i < MN; ++i)
+            read_dy(buffer, kk, i);
+    };
+    // The products of one step, and after the last one of each of dy's fragments
+    // its read for step kk of `buffer` into the same registers (two sets of them
+    // left no registers: 8192^3 947 us, 925 so).  A wave at its products goes before
+    // one that lays tokens into LDS: 925 -> 906 us; with codes, whose conversion
+    // then waits too long, 973 -> 1006, so not there.
+    auto multiply = [&](auto set, uint32_t buffer, int kk) {
+        constexpr int S = decltype(set)::value;
+        if (kk >= 0) {
+            if constexpr (S == 0)
+                read_x(buffer, kk, high);
+            else
+                read_x(buffer, kk, low);
+        }
+        if constexpr (X == kBf16)
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int i = 0; i < MN; ++i) {
 #pragma unroll
             for (int j = 0; j < MK; ++j)
                 acc[i][j] =
-                    __builtin_amdgcn_mfma_f32_32x32x16_bf16(fd[S][i], fx[S][j], acc[i][j], 0, 0, 0);
+                    __builtin_amdgcn_mfma_f32_32x32x16_bf16(fd[i], fx[S][j], acc[i][j], 0, 0, 0);
+            if (kk >= 0)
+                read_dy(buffer, kk, i);
+        }
+        if constexpr (X == kBf16)
+            __builtin_amdgcn_s_setprio(0);
     };
     auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
 
@@ -309,7 +355,7 @@ __global__ __launch_bounds__(WAVES_N *WAVES_K *kWave) void weight_grad_kernel(We
     // products; the barrier stands before the last step, whose products then cover
     // the other buffer's first reads.
     const uint32_t margin = od.margin > ox.margin ? od.margin : ox.margin;
-    size_t turns = (end - begin) / kStep;
+    size_t turns = a.near ? (end - begin) / kStep : 0;
     if (turns && begin + turns * kStep + margin > a.rows)
         --turns;
     uint32_t buffer = 0;
@@ -325,40 +371,33 @@ __global__ __launch_bounds__(WAVES_N *WAVES_K *kWave) void weight_grad_kernel(We
         for (size_t token = begin; token < last; token += kStep) {
             const size_t next = token + 2 * kStep < last ? token + 2 * kStep : last;
             fence();
-            read(buffer, 1, high);
             put_x(buffer ^ 1, low);
-            multiply(low);
+            multiply(low, buffer, 1);
             fence();
-            read(buffer, 2, low);
             put_x(buffer ^ 1, high);
             get_x(next);
-            multiply(high);
+            multiply(high, buffer, 2);
             fence();
-            read(buffer, 3, high);
             put_dy(buffer ^ 1, low);
             put_dy(buffer ^ 1, high);
             get_dy(next);
-            multiply(low);
+            multiply(low, buffer, 3);
             fence();
             __syncthreads();
             buffer ^= 1;
-            read(buffer, 0, low);
-            multiply(high);
+            multiply(high, buffer, 0);
         }
-        read(buffer, 1, high);
-        multiply(low);
-        read(buffer, 2, low);
-        multiply(high);
-        read(buffer, 3, high);
-        multiply(low);
-        multiply(high);
+        multiply(low, buffer, 1);
+        multiply(high, buffer, 2);
+        multiply(low, buffer, 3);
+        multiply(high, buffer, -1);
         buffer ^= 1;
     }
     for (size_t token = begin + turns * kStep; token < end; token += kStep) {
 #pragma unroll
         for (uint32_t p = 0; p < kPieces; ++p) {
-            fetch_end(pd[p], od, token + p * kApart, group * 4, end, a.rows);
-            fetch_end(px[p], ox, token + p * kApart, group * 4, end, a.rows);
+            fetch_end(pd[p], od, token + p * kApart + group * 4, end, a.rows);
+            fetch_end(px[p], ox, token + p * kApart + group * 4, end, a.rows);
         }
         // the other buffer's readers are past the last barrier
         put(buffer);
@@ -366,88 +405,120 @@ __global__ __launch_bounds__(WAVES_N *WAVES_K *kWave) void weight_grad_kernel(We
 #pragma unroll 1
         for (uint32_t kk = 0; kk < kStep / 16; ++kk) {
             read(buffer, kk, low);
-            multiply(low);
+            multiply(low, buffer, -1);
         }
         buffer ^= 1;
     }
 
     // lane l holds column l % 32 and, in register r, row 8 (r / 4) + 4 (l / 32) + r % 4
-    float *out = a.out + (size_t)blockIdx.y * a.out_split;
+    const bool direct = whole || a.splits == 1;
+    float *out = a.dw + n0 * a.dw_stride + k0;
+    size_t stride = a.dw_stride;
+    if (!direct) {
+        out = a.parts + ((size_t)split * tail + (tile - a.whole)) * (TILE * TILE);
+        stride = TILE;
+    }
+    const bool add = direct && a.accumulate;
 #pragma unroll
     for (int j = 0; j < MK; ++j) {
-        const uint32_t col = k0 + wk + j * 32 + lane % 32;
-        if (col >= a.k)
+        const uint32_t col = wk + j * 32 + lane % 32;
+        if (k0 + col >= a.k)
             continue;
 #pragma unroll
         for (int i = 0; i < MN; ++i)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const uint32_t row = n0 + wn + i * 32 + 8 * (r / 4) + 4 * (lane / 32) + r % 4;
-                if (row < a.n) {
-                    float *p = out + (size_t)row * a.out_stride + col;
-                    *p = a.accumulate ? *p + acc[i][j][r] : acc[i][j][r];
+                const uint32_t row = wn + i * 32 + 8 * (r / 4) + 4 * (lane / 32) + r % 4;
+                if (n0 + row < a.n) {
+                    float *p = out + row * stride + col;
+                    *p = add ? *p + acc[i][j][r] : acc[i][j][r];
                 }
             }
     }
 }
 
-// dw (+)= the splits' sums, in order; also writes zeros where there is nothing
-// to sum.
-__global__ __launch_bounds__(256) void weight_grad_join(const float *parts, uint32_t splits,
-                                                        uint32_t n, uint32_t k, float *dw,
-                                                        size_t stride, int accumulate) {
+// dw (+)= the tail tiles' splits, in order: a workgroup takes 4 rows of a tile,
+// lanes neighbouring columns.
+constexpr uint32_t kJoinRows = 4;
+template <int TILE>
+__global__ __launch_bounds__(TILE) void weight_grad_join(WeightGradArgs a) {
+    const uint32_t tail = a.tiles_n * a.tiles_k - a.whole;
+    const uint32_t t = blockIdx.x / (TILE / kJoinRows), row = blockIdx.x % (TILE / kJoinRows) * kJoinRows;
+    uint32_t tile_n, tile_k;
+    tile_at(a.whole + t, a.tiles_n, a.tiles_k, tile_n, tile_k);
+    const uint32_t n0 = tile_n * TILE + row, col = tile_k * TILE + threadIdx.x;
+    if (n0 >= a.n || col >= a.k)
+        return;
+    const float *p = a.parts + (size_t)t * (TILE * TILE) + row * TILE + threadIdx.x;
+    // rows past the last are the last again, and not stored
+    const uint32_t rows = a.n - n0 < kJoinRows ? a.n - n0 : kJoinRows;
+    float sum[kJoinRows] = {};
+    for (uint32_t s = 0; s < a.splits; ++s, p += (size_t)tail * (TILE * TILE)) {
+#pragma unroll
+        for (uint32_t r = 0; r < kJoinRows; ++r)
+            sum[r] += p[(r < rows ? r : rows - 1) * TILE];
+    }
+#pragma unroll
+    for (uint32_t r = 0; r < kJoinRows; ++r)
+        if (r < rows) {
+            float *out = a.dw + (size_t)(n0 + r) * a.dw_stride + col;
+            *out = a.accumulate ? *out + sum[r] : sum[r];
+        }
+}
+
+// The gradient of no tokens.
+__global__ __launch_bounds__(256) void weight_grad_zero(float *dw, uint32_t n, uint32_t k,
+                                                        size_t stride) {
     const size_t total = (size_t)n * k;
     for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < total;
-         i += (size_t)gridDim.x * 256) {
-        float sum = 0.0f;
-        for (uint32_t s = 0; s < splits; ++s)
-            sum += parts[s * total + i];
-        float *p = dw + i / k * stride + i % k;
-        *p = accumulate ? *p + sum : sum;
-    }
+         i += (size_t)gridDim.x * 256)
+        dw[i / k * stride + i % k] = 0.0f;
 }
 
 constexpr size_t kMostSplits = 64;
 
 struct GradShape {
     uint32_t tile, splits;
-    size_t split_rows;
+    size_t tiles, whole, split_rows;
+    size_t parts() const { return splits > 1 ? splits * (tiles - whole) * tile * tile : 0; }
 };
 
-// Tile and number of splits of the tokens with the smallest expected time: the
-// rounds that the workgroups take over the CUs (two of tile 128 fit a CU, one of
-// tile 256), each as long as its turns and a fixed part, and with splits the
-// traffic of their partial results.  The constants, in us, are what bf16 and
-// checkpoints (a tenth more) measure.  Tile 128 against 256, without splits:
-// 4096x18176x4544 841 / 626, 2048x4096x4096 89 / 72, 4096x2048x2048 55 / 96,
-// 300x2048x2048 13 / 20.  Splits of tile 128, 1 / 4 / 16: 8192x1024x1024 91 / 38 /
-// 52, 8192x256x256 86 / 30 / 19, 1000x1000x1000 18 / 20 / 35.
+// Tile, and into how many splits of the tokens, with the smallest expected time.
+// Workgroups run in rounds over the CUs (two of tile 128 fit a CU, one of tile
+// 256): as many whole rounds of tiles as there are take their tokens undivided, or
+// none does where the tiles are few; the rest are split, which shortens the last
+// round and costs the traffic of the partial results.  A round is as long as its
+// turns and a fixed part; the constants, in us, are what bf16 and checkpoints (a
+// tenth more) measure.  Tile 128 against 256, nothing split: 4096x18176x4544 841 /
+// 626, 2048x4096x4096 89 / 72, 4096x2048x2048 55 / 96, 300x2048x2048 13 / 20.
+// Splits of tile 128, 1 / 4 / 16: 8192x1024x1024 91 / 38 / 52, 8192x256x256 86 /
+// 30 / 19, 1000x1000x1000 18 / 20 / 35.
 GradShape grad_shape(size_t rows, size_t n, size_t k) {
     const size_t turns = (rows + kStep - 1) / kStep;
-    GradShape best = {128, 1, turns * kStep};
+    GradShape best = {};
     double least = 1e30;
     for (const uint32_t tile : {128u, 256u}) {
         const size_t tiles = ((n + tile - 1) / tile) * ((k + tile - 1) / tile);
+        const size_t slots = tile == 256 ? kCus : 2 * kCus;
+        const auto round = [&](double per, double groups) {
+            return tile == 256        ? 1.95 * per + 6.0
+                   : groups <= kCus ? 0.7 * per + 3.0
+                                    : 1.31 * per + 4.0;
+        };
         for (size_t splits = 1; splits <= kMostSplits && splits <= turns; ++splits) {
             const size_t per = (turns + splits - 1) / splits;
             if ((turns + per - 1) / per != splits)
                 continue;  // the same as a smaller number
-            const double groups = (double)tiles * (double)splits;
-            double each, time = 5.0;
-            if (tile == 256) {
-                each = 1.95 * (double)per + 6.0;
-                time += ceil(groups / kCus) * each;
-            } else if (groups <= kCus) {
-                time += 0.7 * (double)per + 3.0;
-            } else {
-                each = 1.31 * (double)per + 4.0;
-                time += ceil(groups / (2 * kCus)) * each;
-            }
-            if (splits > 1)
-                time += 3.0 + 2.0 * (double)splits * (double)n * (double)k * 4.0 / 4.8e6;
+            const size_t whole = splits == 1 ? tiles : tiles / slots * slots;
+            const double rest = (double)(tiles - whole) * (double)splits;
+            double time = 5.0 + ceil((double)whole / (double)slots) *
+                                    round((double)turns, (double)whole);
+            if (rest > 0)
+                time += ceil(rest / (double)slots) * round((double)per, rest) + 3.0 +
+                        2.0 * rest * tile * tile * 4.0 / 4.8e6;
             if (time < least) {
                 least = time;
-                best = {tile, (uint32_t)splits, per * kStep};
+                best = {tile, (uint32_t)splits, tiles, whole, per * kStep};
             }
         }
     }
@@ -455,7 +526,7 @@ GradShape grad_shape(size_t rows, size_t n, size_t k) {
 }
 
 template <int X, int TILE, int WAVES_N, int WAVES_K>
-hipError_t start(const WeightGradArgs &a, uint32_t splits, hipStream_t stream) {
+hipError_t start(const WeightGradArgs &a, const GradShape &s, hipStream_t stream) {
     constexpr size_t kLds = 2 * 2 * TILE * kStep * 2;
     const void *kernel =
         reinterpret_cast<const void *>(weight_grad_kernel<X, TILE, WAVES_N, WAVES_K>);
@@ -464,63 +535,58 @@ hipError_t start(const WeightGradArgs &a, uint32_t splits, hipStream_t stream) {
         hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
     if (allowed != hipSuccess)
         return allowed;
-    hipLaunchKernelGGL((weight_grad_kernel<X, TILE, WAVES_N, WAVES_K>),
-                       dim3(a.tiles_n * a.tiles_k, splits), dim3(WAVES_N * WAVES_K * kWave), kLds,
-                       stream, a);
+    const size_t tail = s.tiles - s.whole, groups = s.whole + tail * s.splits;
+    hipLaunchKernelGGL((weight_grad_kernel<X, TILE, WAVES_N, WAVES_K>), dim3((unsigned)groups),
+                       dim3(WAVES_N * WAVES_K * kWave), kLds, stream, a);
+    if (s.splits > 1 && tail)
+        hipLaunchKernelGGL((weight_grad_join<TILE>), dim3((unsigned)(tail * (TILE / kJoinRows))),
+                           dim3(TILE), 0, stream, a);
     return hipGetLastError();
 }
 
 template <int X>
 hipError_t start(const WeightGradArgs &a, const GradShape &s, hipStream_t stream) {
-    return s.tile == 256 ? start<X, 256, 2, 4>(a, s.splits, stream)
-                         : start<X, 128, 2, 2>(a, s.splits, stream);
+    return s.tile == 256 ? start<X, 256, 2, 4>(a, s, stream) : start<X, 128, 2, 2>(a, s, stream);
 }
 
 }  // namespace
 
 size_t weight_grad_workspace(size_t rows, size_t n, size_t k) {
-    const GradShape s = grad_shape(rows, n, k);
-    return s.splits > 1 ? s.splits * n * k * sizeof(float) : 0;
+    return grad_shape(rows, n, k).parts() * sizeof(float);
 }
 
 hipError_t launch_weight_grad(const Mat &dy, const Mat &x, int x_type, size_t rows, size_t n,
                               size_t k, const Mat &dw, int accumulate, void *workspace,
                               hipStream_t stream) {
-    const size_t total = n * k;
-    const unsigned join_grid = (unsigned)(total / 256 < 8 * kCus ? total / 256 + 1 : 8 * kCus);
-    float *out = reinterpret_cast<float *>(dw.data);
+    WeightGradArgs a = {};
+    a.dy = dy;
+    a.x = x;
+    a.dw = reinterpret_cast<float *>(dw.data);
+    a.dw_stride = dw.stride;
+    a.n = (uint32_t)n;
+    a.k = (uint32_t)k;
     if (rows == 0) {
-        if (!accumulate)
-            hipLaunchKernelGGL(weight_grad_join, dim3(join_grid), dim3(256), 0, stream, nullptr, 0u,
-                               (uint32_t)n, (uint32_t)k, out, dw.stride, 0);
+        if (!accumulate) {
+            const size_t groups = (n * k + 255) / 256;
+            hipLaunchKernelGGL(weight_grad_zero, dim3((unsigned)(groups < 8 * kCus ? groups : 8 * kCus)),
+                               dim3(256), 0, stream, a.dw, a.n, a.k, a.dw_stride);
+        }
         return hipGetLastError();
     }
     const GradShape s = grad_shape(rows, n, k);
     // a grid has 2^32 - 1 work-items at most
-    if (((n + s.tile - 1) / s.tile) * ((k + s.tile - 1) / s.tile) > UINT32_MAX / 512 / s.splits)
+    if (s.tiles > UINT32_MAX / 512 / s.splits)
         return hipErrorInvalidConfiguration;
-    WeightGradArgs a;
-    a.dy = dy;
-    a.x = x;
-    a.out = s.splits > 1 ? reinterpret_cast<float *>(workspace) : out;
-    a.out_stride = s.splits > 1 ? k : dw.stride;
-    a.out_split = total;
+    a.parts = reinterpret_cast<float *>(workspace);
     a.rows = rows;
     a.split_rows = s.split_rows;
-    a.n = (uint32_t)n;
-    a.k = (uint32_t)k;
     a.tiles_n = (uint32_t)((n + s.tile - 1) / s.tile);
     a.tiles_k = (uint32_t)((k + s.tile - 1) / s.tile);
-    a.accumulate = s.splits > 1 ? 0 : accumulate;
-    const hipError_t e =
-        x_type == kI8 ? start<kI8>(a, s, stream) : start<kBf16>(a, s, stream);
-    if (e != hipSuccess)
-        return e;
-    if (s.splits > 1)
-        hipLaunchKernelGGL(weight_grad_join, dim3(join_grid), dim3(256), 0, stream,
-                           reinterpret_cast<const float *>(workspace), s.splits, (uint32_t)n,
-                           (uint32_t)k, out, dw.stride, accumulate);
-    return hipGetLastError();
+    a.whole = (uint32_t)s.whole;
+    a.splits = s.splits;
+    a.accumulate = accumulate;
+    a.near = dy.stride <= kNear && x.stride <= kNear && k <= kNear;
+    return x_type == kI8 ? start<kI8>(a, s, stream) : start<kBf16>(a, s, stream);
 }
 
 }  // namespace zpp

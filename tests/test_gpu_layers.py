@@ -535,3 +535,70 @@ def test_offsets_past_32_bits(zpp):
     zpp.gelu_forward(near, far)
     zpp.gelu_forward(near, out)
     assert same(far, out)
+
+
+# Rows of two chunks a lane in the norm's forward pass, ragged and not, the last
+# length in registers and the first beyond
+@TYPES
+@pytest.mark.parametrize("rows,cols", [(3, 9001), (600, 16384), (2, 16383), (2, 16385), (4, 5)])
+def test_norm_of_long_and_of_tiny_rows(zpp, rows, cols, dtype):
+    eps = 1e-5
+    x, r = ref.values(rows, cols, 1, dtype, 3, 1), ref.values(rows, cols, 2, dtype)
+    gamma, beta = norm_params(cols, dtype, 3)
+    y, total = ref.matrix(rows, cols, dtype, 1), ref.matrix(rows, cols, dtype)
+    mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    saved = zpp.empty_checkpoint(rows, cols)
+    zpp.layer_norm_forward(x, gamma, beta, y, mean, rstd, eps=eps, residual=r, total=total,
+                           saved=saved)
+    want, bound = ref.norm_forward(total.double(), gamma.double(), beta.double(), eps, dtype)
+    for got, w, b, what in zip((y, mean, rstd), want, bound, ("y", "mean", "rstd")):
+        ref.check(got, w, b, what)
+    codes, exps = ref.encode(total.float().cpu().numpy())
+    assert np.array_equal(saved[0].cpu().numpy(), codes)
+    assert np.array_equal(saved[1].cpu().numpy(), exps)
+    dy = ref.values(rows, cols, 4, dtype, std=1e-3)
+    xs = torch.from_numpy(ref.decode(codes, exps)).cuda()
+    want, bound = ref.norm_backward(dy.double(), xs, gamma.double(), beta.double(), mean.double(),
+                                    rstd.double(), None, dtype)
+    dx, dg, db = ref.matrix(rows, cols, dtype), torch.empty(cols, device="cuda"), \
+        torch.empty(cols, device="cuda")
+    ws = torch.empty(zpp.layer_norm_backward_workspace(rows, cols), dtype=torch.uint8,
+                     device="cuda")
+    zpp.layer_norm_backward(dy, saved, gamma, mean, rstd, dx, dg, db, ws)
+    for got, w, b, what in zip((dx, dg, db), want, bound, ("dx", "dgamma", "dbeta")):
+        ref.check(got, w, b, what)
+
+
+# Sizes for each way the weight gradient divides its work: tiles of 256 whole,
+# a last round split over the tokens, few tiles split, at a multiple of the
+# turn of 64 tokens and off it
+@pytest.mark.parametrize("from_saved", [False, True], ids=["bf16", "i8"])
+@pytest.mark.parametrize("rows,n,k", [(256, 4100, 4096), (641, 4672, 4544), (320, 4096, 4608),
+                                      (2047, 300, 520), (4096, 256, 256)])
+def test_weight_grad_divisions(zpp, rows, n, k, from_saved):
+    dy, x = ref.values(rows, n, 1, BF16, std=1e-3), ref.values(rows, k, 2, BF16)
+    saved = zpp.empty_checkpoint(rows, k)
+    zpp.checkpoint_save(x, saved)
+    xs = x.float()
+    if from_saved:
+        xs = torch.empty_like(xs)
+        zpp.checkpoint_load(saved, xs)
+    want, bound = ref.weight_grad(dy.double(), xs.double())
+    dw = run_grad(zpp, dy, saved if from_saved else x, n, k)
+    ref.check(dw, want, bound, "dw")
+    assert same(dw, run_grad(zpp, dy, saved if from_saved else x, n, k))
+    ws = torch.empty(zpp.weight_grad_workspace(rows, n, k), dtype=torch.uint8, device="cuda")
+    twice = dw.clone()
+    zpp.weight_grad(dy, saved if from_saved else x, twice, ws, accumulate=True)
+    ref.check(twice, 2 * want, 2 * bound + 2 * ref.U * want.abs(), "dw added to")
+
+
+def test_weight_grad_of_tokens_far_apart(zpp):
+    """Tokens further apart than a turn's 32-bit offsets reach, more than one turn
+    of them."""
+    rows, n, k, apart = 70, 40, 72, (1 << 24) + 8
+    buf = torch.empty(69 * apart + n, dtype=BF16, device="cuda")
+    dy = buf.as_strided((rows, n), (apart, 1))
+    near, x = ref.values(rows, n, 1, BF16), ref.values(rows, k, 2, BF16)
+    dy.copy_(near)
+    assert same(run_grad(zpp, dy, x, n, k), run_grad(zpp, near, x, n, k))
