@@ -90,6 +90,8 @@ def build_marshal(verbose=False):
            "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
            *[x for d in cpp_extension.include_paths() for x in ("-isystem", d)],
            "-isystem", sysconfig.get_paths()["include"],
+           "-D__HIP_PLATFORM_AMD__", "-I", INCLUDE,
+           "-isystem", os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include"),
            os.path.join(CSRC, MARSHAL_SOURCE), "-o", tmp,
            "-L" + torch_lib, "-ltorch_python", "-ltorch_cpu", "-lc10"]
     if verbose:

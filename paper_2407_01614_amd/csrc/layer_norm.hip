@@ -202,8 +202,6 @@ __global__ __launch_bounds__(kMaxThreads) void norm_forward_kernel(NormForwardAr
 #pragma unroll
     for (int v = 0; v < V; ++v)
         l[v] = row_lane<RAGGED>(v * blockDim.x + threadIdx.x, a.cols);
-    if constexpr (V == 1)
-        params(0);
     Chunk<TYPE> cx[V] = {}, cr[V] = {};
     auto fetch = [&](size_t row) {
 #pragma unroll
@@ -215,6 +213,8 @@ __global__ __launch_bounds__(kMaxThreads) void norm_forward_kernel(NormForwardAr
             }
     };
     fetch(blockIdx.x);
+    if constexpr (V == 1)
+        params(0);
     for (size_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         float x[V][8], sum[1] = {0.0f};
 #pragma unroll
@@ -397,16 +397,6 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward_kernel(NormBackward
                 v[4 * half + e] = p[e];
         }
     };
-    if (team == 0) {
-#pragma unroll
-        for (int which = 0; which < (AGAIN ? 2 : 1); ++which) {
-            float v[8];
-            load_param(which ? a.beta : a.gamma, a.param_type, l.col, l.in ? 8 : 0, v);
-            params[2 * which * threads] = f32x4{v[0], v[1], v[2], v[3]};
-            params[(2 * which + 1) * threads] = f32x4{v[4], v[5], v[6], v[7]};
-        }
-    }
-    __syncthreads();
     Chunk<TYPE> nd = {}, nr = {};
     Chunk<X> nx = {};
     float stat[2] = {0.0f, 0.0f};  // the next row's mean and factor
@@ -431,6 +421,16 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward_kernel(NormBackward
     // every team takes as many turns, so that all meet at the barriers
     const size_t step = (size_t)gridDim.x * teams;
     fetch((size_t)blockIdx.x * teams + team);
+    if (team == 0) {
+#pragma unroll
+        for (int which = 0; which < (AGAIN ? 2 : 1); ++which) {
+            float v[8];
+            load_param(which ? a.beta : a.gamma, a.param_type, l.col, l.in ? 8 : 0, v);
+            params[2 * which * threads] = f32x4{v[0], v[1], v[2], v[3]};
+            params[(2 * which + 1) * threads] = f32x4{v[4], v[5], v[6], v[7]};
+        }
+    }
+    __syncthreads();
     for (size_t base = (size_t)blockIdx.x * teams; base < a.rows; base += step) {
         const size_t row = base + team;
         const Chunk<TYPE> cr = nr;
@@ -478,27 +478,32 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward_kernel(NormBackward
     }
     if (!a.partials)
         return;
-    // The teams' sums, one team after the other, then the workgroup's pair; the
-    // join's memory is gamma's, which all are done with.  Both are laid out as
-    // gamma is, [2][2 halves][threads][4].
-    f32x4 v[4] = {{dg[0], dg[1], dg[2], dg[3]},
-                  {dg[4], dg[5], dg[6], dg[7]},
-                  {db[0], db[1], db[2], db[3]},
-                  {db[4], db[5], db[6], db[7]}};
-    for (uint32_t t = 0; t < teams; ++t) {
-        if (teams > 1)
-            __syncthreads();
-        if (team != t)
-            continue;
+    // The workgroup's pair, laid out as gamma is, [2][2 halves][threads][4]: the
+    // teams' sums of one array at a time side by side in LDS, where gamma was, and
+    // added in the teams' order.
+    const f32x4 v[4] = {{dg[0], dg[1], dg[2], dg[3]},
+                        {dg[4], dg[5], dg[6], dg[7]},
+                        {db[0], db[1], db[2], db[3]},
+                        {db[4], db[5], db[6], db[7]}};
+    f32x4 *const out = reinterpret_cast<f32x4 *>(a.partials) + (size_t)blockIdx.x * 4 * threads;
+    if (teams == 1) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (t > 0)
-                v[i] += params[i * threads];
-            if (t + 1 < teams)
-                params[i * threads] = v[i];
-            else
-                reinterpret_cast<f32x4 *>(a.partials)[((size_t)blockIdx.x * 4 + i) * threads + lane] =
-                    v[i];
+        for (int i = 0; i < 4; ++i)
+            out[i * threads + lane] = v[i];
+        return;
+    }
+    f32x4 *const sums = reinterpret_cast<f32x4 *>(shared);  // [2 halves][teams][threads]
+#pragma unroll
+    for (uint32_t which = 0; which < 2; ++which) {
+        __syncthreads();
+        sums[team * threads + lane] = v[2 * which];
+        sums[(teams + team) * threads + lane] = v[2 * which + 1];
+        __syncthreads();
+        if (team < 2) {
+            f32x4 sum = sums[team * teams * threads + lane];
+            for (uint32_t t = 1; t < teams; ++t)
+                sum += sums[(team * teams + t) * threads + lane];
+            out[(2 * which + team) * threads + lane] = sum;
         }
     }
 }
@@ -667,7 +672,8 @@ uint32_t long_row_groups(size_t rows, size_t cols) {
 
 template <int TYPE, int X, bool AGAIN>
 void start_backward(const NormBackwardArgs &a, const RowShape &s, hipStream_t stream) {
-    const size_t lds = 2 * sizeof(float) * s.threads * 8;
+    const size_t params = 2 * 2 * sizeof(f32x4), sums = s.teams > 1 ? 2 * sizeof(f32x4) * s.teams : 0;
+    const size_t lds = s.threads * (params > sums ? params : sums);
     const dim3 grid(s.grid), threads(s.threads * s.teams);
     if (a.cols % 8)
         hipLaunchKernelGGL((norm_backward_kernel<TYPE, X, AGAIN, true>), grid, threads,

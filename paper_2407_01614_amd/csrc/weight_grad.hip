@@ -359,17 +359,27 @@ __global__ __launch_bounds__(WAVES_N *WAVES_K *kWave) void weight_grad_kernel(We
     if (turns && begin + turns * kStep + margin > a.rows)
         --turns;
     uint32_t buffer = 0;
+    size_t token = begin + turns * kStep;  // of the turns at the end, fetched apart
+    auto get_end = [&] {
+#pragma unroll
+        for (uint32_t p = 0; p < kPieces; ++p) {
+            fetch_end(pd[p], od, token + p * kApart + group * 4, end, a.rows);
+            fetch_end(px[p], ox, token + p * kApart + group * 4, end, a.rows);
+        }
+    };
     if (turns) {
         const size_t last = begin + (turns - 1) * kStep;
         get_x(begin);
         get_dy(begin);
         put(0);
-        get_x(begin + kStep < last ? begin + kStep : last);
-        get_dy(begin + kStep < last ? begin + kStep : last);
+        if (turns > 1) {
+            get_x(begin + kStep);
+            get_dy(begin + kStep);
+        }
         __syncthreads();
         read(0, 0, low);
-        for (size_t token = begin; token < last; token += kStep) {
-            const size_t next = token + 2 * kStep < last ? token + 2 * kStep : last;
+        for (size_t at = begin; at < last; at += kStep) {
+            const size_t next = at + 2 * kStep < last ? at + 2 * kStep : last;
             fence();
             put_x(buffer ^ 1, low);
             multiply(low, buffer, 1);
@@ -387,21 +397,23 @@ __global__ __launch_bounds__(WAVES_N *WAVES_K *kWave) void weight_grad_kernel(We
             buffer ^= 1;
             multiply(high, buffer, 0);
         }
+        if (token < end)
+            get_end();
         multiply(low, buffer, 1);
         multiply(high, buffer, 2);
         multiply(low, buffer, 3);
         multiply(high, buffer, -1);
         buffer ^= 1;
+    } else if (token < end) {
+        get_end();
     }
-    for (size_t token = begin + turns * kStep; token < end; token += kStep) {
-#pragma unroll
-        for (uint32_t p = 0; p < kPieces; ++p) {
-            fetch_end(pd[p], od, token + p * kApart + group * 4, end, a.rows);
-            fetch_end(px[p], ox, token + p * kApart + group * 4, end, a.rows);
-        }
+    while (token < end) {
         // the other buffer's readers are past the last barrier
         put(buffer);
         __syncthreads();
+        token += kStep;
+        if (token < end)
+            get_end();
 #pragma unroll 1
         for (uint32_t kk = 0; kk < kStep / 16; ++kk) {
             read(buffer, kk, low);
@@ -503,7 +515,7 @@ GradShape grad_shape(size_t rows, size_t n, size_t k) {
         const auto round = [&](double per, double groups) {
             return tile == 256        ? 1.95 * per + 6.0
                    : groups <= kCus ? 0.7 * per + 3.0
-                                    : 1.31 * per + 4.0;
+                                    : 1.31 * per + 3.5;
         };
         for (size_t splits = 1; splits <= kMostSplits && splits <= turns; ++splits) {
             const size_t per = (turns + splits - 1) / splits;

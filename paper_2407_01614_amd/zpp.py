@@ -669,9 +669,6 @@ def _matrix(m, mask, rows, cols, name):
 def _matrices(names, *args):
     """The zpp_matrix of each object in args = (object, mask, rows, cols, ...),
     in order; an optional one's None stays None."""
-    found = _marshal.matrices(_device(), ACT_BLOCK, *args)
-    if found is not None:
-        return found
     return tuple(_matrix(*a, name) for name, a in
                  zip(names, zip(args[::4], args[1::4], args[2::4], args[3::4])))
 
@@ -686,6 +683,29 @@ def _params(gamma, beta, cols):
     return g, b, kind
 
 
+def _fn(name):
+    return ctypes.cast(getattr(_lib, name), _P).value
+
+
+# Addresses of the entry points, for the calls that `_marshal` makes itself.
+_FN = {name: _fn("zpp_" + name) for name in (
+    "checkpoint_save", "checkpoint_load", "layer_norm_forward", "layer_norm_backward",
+    "layer_norm_backward_workspace", "gelu_forward", "gelu_backward", "weight_grad",
+    "weight_grad_workspace")}
+
+
+def _where(name, stream, wait_before, done_after):
+    """The first arguments of a native call: entry point, device, stream, events."""
+    device = _device()
+    if device < 0:
+        handle = 0  # no tensor is on it: the checks say so
+    elif stream is None:
+        handle = torch._C._cuda_getCurrentRawStream(device)
+    else:
+        handle = stream_handle(stream)
+    return _FN[name], device, handle, _event_handle(wait_before), _event_handle(done_after)
+
+
 def _workspace(t, need, name):
     """Address and size of a call's workspace; None where none is needed."""
     if t is None and not need:
@@ -698,19 +718,25 @@ def _workspace(t, need, name):
 
 def checkpoint_save(x, saved, *, stream=None, wait_before=None, done_after=None):
     """zpp_checkpoint_save: x in 8 bits into ``saved`` = (codes, exps)."""
+    where = _where("checkpoint_save", stream, wait_before, done_after)
+    st = _marshal.checkpoint_save(*where, x, saved)
+    if st is not None:
+        return _check(st, "zpp_checkpoint_save")
     rows, cols = _shape(x, "x")
     mx, ms = _matrices(("x", "saved"), x, _PLAIN, rows, cols, saved, _SAVED, rows, cols)
-    st = _lib.zpp_checkpoint_save(mx, ms, rows, cols, stream_handle(stream),
-                                  _event_handle(wait_before), _event_handle(done_after))
+    st = _lib.zpp_checkpoint_save(mx, ms, rows, cols, *where[2:])
     _check(st, "zpp_checkpoint_save")
 
 
 def checkpoint_load(saved, out, *, stream=None, wait_before=None, done_after=None):
     """zpp_checkpoint_load: the values of ``saved`` into out."""
+    where = _where("checkpoint_load", stream, wait_before, done_after)
+    st = _marshal.checkpoint_load(*where, saved, out)
+    if st is not None:
+        return _check(st, "zpp_checkpoint_load")
     rows, cols = _shape(saved, "saved")
     ms, mo = _matrices(("saved", "out"), saved, _SAVED, rows, cols, out, _PLAIN, rows, cols)
-    st = _lib.zpp_checkpoint_load(ms, mo, rows, cols, stream_handle(stream),
-                                  _event_handle(wait_before), _event_handle(done_after))
+    st = _lib.zpp_checkpoint_load(ms, mo, rows, cols, *where[2:])
     _check(st, "zpp_checkpoint_load")
 
 
@@ -719,6 +745,11 @@ def layer_norm_forward(x, gamma, beta, y, mean, rstd, *, eps, residual=None, tot
     """zpp_layer_norm_forward: y of x (of x + ``residual``, stored as
     ``total``); ``saved``: the checkpoint of what is normalised.  ``beta``,
     ``mean`` and ``rstd`` may be None."""
+    where = _where("layer_norm_forward", stream, wait_before, done_after)
+    st = _marshal.layer_norm_forward(*where, x, residual, y, total, saved, gamma, beta,
+                                     mean, rstd, eps)
+    if st is not None:
+        return _check(st, "zpp_layer_norm_forward")
     rows, cols = _shape(x, "x")
     given = _PLAIN | _ABSENT
     mx, mr, my, mt, ms = _matrices(
@@ -728,8 +759,7 @@ def layer_norm_forward(x, gamma, beta, y, mean, rstd, *, eps, residual=None, tot
     pm, pr = _addresses(("mean", "rstd"), "mean and rstd hold one value a row",
                         mean, _F32 | _OPTIONAL, rows, rstd, _F32 | _OPTIONAL, rows)
     st = _lib.zpp_layer_norm_forward(mx, mr, g, b, kind, rows, cols, eps, my, mt, ms, pm, pr,
-                                     stream_handle(stream), _event_handle(wait_before),
-                                     _event_handle(done_after))
+                                     *where[2:])
     _check(st, "zpp_layer_norm_forward")
 
 
@@ -744,6 +774,12 @@ def layer_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace, 
     """zpp_layer_norm_backward; ``x`` is what the forward pass normalised or its
     checkpoint; ``y``: the forward pass's output again (with ``beta``);
     ``dgamma`` and ``dbeta`` may be None."""
+    where = _where("layer_norm_backward", stream, wait_before, done_after)
+    st = _marshal.layer_norm_backward(*where, dy, x, dresidual, dx, y, gamma, beta, mean,
+                                      rstd, dgamma, dbeta, accumulate,
+                                      _FN["layer_norm_backward_workspace"], workspace)
+    if st is not None:
+        return _check(st, "zpp_layer_norm_backward")
     rows, cols = _shape(dy, "dy")
     given = _PLAIN | _ABSENT
     md, mx, mr, mo, my = _matrices(
@@ -758,30 +794,35 @@ def layer_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace, 
     ws, size = _workspace(workspace, _lib.zpp_layer_norm_backward_workspace(rows, cols),
                           "layer_norm_backward")
     st = _lib.zpp_layer_norm_backward(md, mx, g, b, kind, pm, pr, mr, rows, cols, mo, my, pg, pb,
-                                      1 if accumulate else 0, ws, size, stream_handle(stream),
-                                      _event_handle(wait_before), _event_handle(done_after))
+                                      1 if accumulate else 0, ws, size, *where[2:])
     _check(st, "zpp_layer_norm_backward")
 
 
 def gelu_forward(u, a, *, saved=None, stream=None, wait_before=None, done_after=None):
     """zpp_gelu_forward: a of u; ``saved``: the checkpoint of u."""
+    where = _where("gelu_forward", stream, wait_before, done_after)
+    st = _marshal.gelu_forward(*where, u, a, saved)
+    if st is not None:
+        return _check(st, "zpp_gelu_forward")
     rows, cols = _shape(u, "u")
     mu, ma, ms = _matrices(("u", "a", "saved"), u, _PLAIN, rows, cols, a, _PLAIN, rows, cols,
                            saved, _SAVED | _ABSENT, rows, cols)
-    st = _lib.zpp_gelu_forward(mu, rows, cols, ma, ms, stream_handle(stream),
-                               _event_handle(wait_before), _event_handle(done_after))
+    st = _lib.zpp_gelu_forward(mu, rows, cols, ma, ms, *where[2:])
     _check(st, "zpp_gelu_forward")
 
 
 def gelu_backward(da, u, du, *, a=None, stream=None, wait_before=None, done_after=None):
     """zpp_gelu_backward; ``u`` is the forward pass's input or its checkpoint;
     ``a``: the forward pass's output again."""
+    where = _where("gelu_backward", stream, wait_before, done_after)
+    st = _marshal.gelu_backward(*where, da, u, du, a)
+    if st is not None:
+        return _check(st, "zpp_gelu_backward")
     rows, cols = _shape(da, "da")
     md, mu, mo, ma = _matrices(
         ("da", "u", "du", "a"), da, _PLAIN, rows, cols, u, _PLAIN | _SAVED, rows, cols,
         du, _PLAIN, rows, cols, a, _PLAIN | _ABSENT, rows, cols)
-    st = _lib.zpp_gelu_backward(md, mu, rows, cols, mo, ma, stream_handle(stream),
-                                _event_handle(wait_before), _event_handle(done_after))
+    st = _lib.zpp_gelu_backward(md, mu, rows, cols, mo, ma, *where[2:])
     _check(st, "zpp_gelu_backward")
 
 
@@ -795,14 +836,18 @@ def weight_grad(dy, x, dw, workspace, *, accumulate=False, stream=None, wait_bef
     """zpp_weight_grad: dw = dy^T x (added to it where ``accumulate``); ``x`` is
     the layer's input in bf16 or its checkpoint, ``workspace`` may be None where
     `weight_grad_workspace` is 0."""
+    where = _where("weight_grad", stream, wait_before, done_after)
+    st = _marshal.weight_grad(*where, dy, x, dw, accumulate, _FN["weight_grad_workspace"],
+                              workspace)
+    if st is not None:
+        return _check(st, "zpp_weight_grad")
     rows, n = _shape(dy, "dy")
     k = _shape(x, "x")[1]
     md, mx, mw = _matrices(("dy", "x", "dw"), dy, 1, rows, n, x, 1 | _SAVED, rows, k,
                            dw, 2, n, k)
     ws, size = _workspace(workspace, _lib.zpp_weight_grad_workspace(rows, n, k), "weight_grad")
     st = _lib.zpp_weight_grad(md, mx, rows, n, k, mw, 1 if accumulate else 0, ws, size,
-                              stream_handle(stream), _event_handle(wait_before),
-                              _event_handle(done_after))
+                              *where[2:])
     _check(st, "zpp_weight_grad")
 
 
