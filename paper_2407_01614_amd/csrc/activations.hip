@@ -61,11 +61,10 @@ __device__ __forceinline__ Place place_of(const Blocks &b, size_t block0, size_t
 // 1.6e-6 up to u = 5, where exp's argument is rounded.  The density of the
 // backward pass is the same exponential.
 struct Normal {
-    float cdf, density;
+    float tail, density;  // P(-u), p(u)
 };
 __device__ __forceinline__ Normal normal(float u) {
-    const float a = __builtin_fabsf(u);
-    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3f, a, 1.0f));
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3f, u, 1.0f));
     float q = 0.035674769f;
     q = __builtin_fmaf(q, t, -0.15720305f);
     q = __builtin_fmaf(q, t, 0.20635340f);
@@ -74,13 +73,19 @@ __device__ __forceinline__ Normal normal(float u) {
     q = __builtin_fmaf(q, t, 0.099913508f);
     q = __builtin_fmaf(q, t, 0.12075396f);
     q = __builtin_fmaf(q, t, 0.11962930f);
-    const float e = __builtin_amdgcn_exp2f(a * a * -0.72134752f);  // exp(-u^2 / 2)
-    const float tail = q * t * e;
-    return {u < 0.0f ? tail : 1.0f - tail, 0.39894228f * e};
+    const float e = __builtin_amdgcn_exp2f(u * u * -0.72134752f);  // exp(-u^2 / 2)
+    return {q * t * e, 0.39894228f * e};
 }
-// u with -Inf (whose product with P = 0 has no value) brought to where P is 0
-// already, and its square kept finite.
-__device__ __forceinline__ float above_tail(float u) { return u < -16.0f ? -16.0f : u; }
+// |u|, kept to 16 where the tail and the density are 0 already, so that Inf, whose
+// product with them has no value, takes its limit.  NaN stays.
+__device__ __forceinline__ float magnitude(float u) {
+    const float a = __builtin_fabsf(u);
+    return a > 16.0f ? 16.0f : a;
+}
+// u P(u) from both sides: u - u P(-u), or -|u| P(-|u|).
+__device__ __forceinline__ float gelu(float u, float a, float tail) {
+    return __builtin_fmaf(-a, tail, u > 0.0f ? u : 0.0f);
+}
 
 struct SaveArgs {
     Mat in, saved;
@@ -111,7 +116,7 @@ struct SaveOp {
     __device__ void store(const Args &a, const Place &p) {
         float v[8];
         chunk_values(x, v);
-        save_chunk<RAGGED>(a.saved, p.in(a.saved), p.valid, p.block, v);
+        save_chunk<RAGGED>(a.saved, p.in(a.saved), p.valid, p.block, max_bits(x), v);
     }
 };
 
@@ -148,13 +153,13 @@ struct GeluForwardOp {
         chunk_values(x, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float u = above_tail(v[e]);
-            y[e] = u * normal(u).cdf;
+            const float m = magnitude(v[e]);
+            y[e] = gelu(v[e], m, normal(m).tail);
         }
         if (p.valid)
             store_chunk<TYPE, RAGGED>(a.a, p.in(a.a), p.valid, make_chunk<TYPE>(y));
         if (a.saved.data)
-            save_chunk<RAGGED>(a.saved, p.in(a.saved), p.valid, p.block, v);
+            save_chunk<RAGGED>(a.saved, p.in(a.saved), p.valid, p.block, max_bits(x), v);
     }
 };
 
@@ -176,12 +181,12 @@ struct GeluBackwardOp {
         chunk_values(d, g);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float u = above_tail(v[e]);
-            const Normal n = normal(u);
-            // from 16 on the density is 0 in fp32 and u may be Inf
-            const float slope = u > 16.0f ? 1.0f : __builtin_fmaf(u, n.density, n.cdf);
-            g[e] *= slope;
-            y[e] = u * n.cdf;
+            const float m = magnitude(v[e]);
+            const Normal n = normal(m);
+            // P(u) + u p(u): for u < 0, P(-|u|) - |u| p, otherwise 1 less that
+            const float below = __builtin_fmaf(-m, n.density, n.tail);
+            g[e] *= v[e] < 0.0f ? below : 1.0f - below;
+            y[e] = gelu(v[e], m, n.tail);
         }
         if (p.valid) {
             store_chunk<TYPE, RAGGED>(a.du, p.in(a.du), p.valid, make_chunk<TYPE>(g));

@@ -128,11 +128,11 @@ __device__ __forceinline__ void store_row(const Mat &m, size_t row, const RowLan
 }
 
 // Writes the checkpoint of the elements that the 8 lanes of a block hold, all
-// of which take part.  x is 0 in elements that are not the lane's.
+// of which take part, `top` each one's largest.
 template <bool RAGGED>
 __device__ __forceinline__ void save_row(const Mat &m, size_t row, const RowLane &l,
-                                         uint32_t blocks, const float (&x)[8]) {
-    const uint32_t exp = act_exp(max8(max_bits(x, 8)));
+                                         uint32_t blocks, uint32_t top, const float (&x)[8]) {
+    const uint32_t exp = act_exp(max8(top));
     if (!l.in)
         return;
     const u32x2 w = act_codes(x, exp);
@@ -217,13 +217,20 @@ __global__ __launch_bounds__(kMaxThreads) void norm_forward_kernel(NormForwardAr
         params(0);
     for (size_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         float x[V][8], sum[1] = {0.0f};
+        uint32_t top[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
+            if (!RAGGED)
+                top[v] = max_bits(cx[v]);
             norm_input<TYPE>(a, cx[v], cr[v], x[v], [&](const Chunk<TYPE> &t) {
+                if (!RAGGED)
+                    top[v] = max_bits(t);
                 if (l[v].in)
                     store_row<TYPE, RAGGED>(a.total, row, l[v], t);
             });
             clear_others<RAGGED>(x[v], l[v]);
+            if (RAGGED)
+                top[v] = max_bits(x[v]);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 sum[0] += x[v][e];
@@ -262,7 +269,7 @@ __global__ __launch_bounds__(kMaxThreads) void norm_forward_kernel(NormForwardAr
             if (l[v].in)
                 store_row<TYPE, RAGGED>(a.y, row, l[v], make_chunk<TYPE>(y));
             if (a.saved.data)
-                save_row<RAGGED>(a.saved, row, l[v], blocks, x[v]);
+                save_row<RAGGED>(a.saved, row, l[v], blocks, top[v], x[v]);
         }
         if (V > 1 && row + gridDim.x < a.rows)
             fetch(row + gridDim.x);
@@ -319,7 +326,7 @@ __global__ __launch_bounds__(kMaxThreads) void norm_forward_long_kernel(NormForw
                         store_chunk<TYPE>(a.y, row * a.y.stride + col, valid, make_chunk<TYPE>(y));
                     if (a.saved.data)
                         save_chunk(a.saved, row * a.saved.stride + col, valid,
-                                   row * blocks + col / kActBlock, x);
+                                   row * blocks + col / kActBlock, valid ? max_bits(x) : 0u, x);
                 }
             }
             if (pass == 2)

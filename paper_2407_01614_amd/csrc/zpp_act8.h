@@ -222,16 +222,29 @@ __device__ __forceinline__ uint32_t act_exp(uint32_t absbits) {
     return absbits >= 0x7F800000u ? 255u : (uint32_t)(e < 1 ? 1 : e);
 }
 
-// A lane's share of a block's largest magnitude, as fp32 bits (whose order is
-// that of the magnitudes, NaN above Inf above all).
-__device__ __forceinline__ uint32_t max_bits(const float (&x)[8], uint32_t valid) {
+// A lane's share of a block's largest magnitude, as fp32 bits, whose order is
+// that of the magnitudes, Inf and then NaN above all: of a chunk as loaded (what a
+// partial one holds past the row's end is the row's last element again), and of
+// values.
+__device__ __forceinline__ uint32_t max_bits(const Chunk<kBf16> &c) {
+    u16x2 a = absbits2(c.w[0]);
+#pragma unroll
+    for (int e = 1; e < 4; ++e)
+        a = __builtin_elementwise_max(a, absbits2(c.w[e]));
+    return (uint32_t)(a.x > a.y ? a.x : a.y) << 16;
+}
+__device__ __forceinline__ uint32_t max_bits(const float (&x)[8]) {
     uint32_t a = 0;
 #pragma unroll
-    for (uint32_t e = 0; e < 8; ++e) {
+    for (int e = 0; e < 8; ++e) {
         const uint32_t b = __float_as_uint(x[e]) & 0x7FFFFFFFu;
-        a = e < valid && b > a ? b : a;
+        a = b > a ? b : a;
     }
     return a;
+}
+__device__ __forceinline__ uint32_t max_bits(const Chunk<kF32> &c) {
+    const float x[8] = {c.lo.x, c.lo.y, c.lo.z, c.lo.w, c.hi.x, c.hi.y, c.hi.z, c.hi.w};
+    return max_bits(x);
 }
 // Largest of 8 neighbouring lanes' (one block's), in all of them.
 __device__ __forceinline__ uint32_t max8(uint32_t a) {
@@ -244,25 +257,33 @@ __device__ __forceinline__ uint32_t max8(uint32_t a) {
 }
 
 // Codes of eight elements of a block with this exponent byte.  x * 2^-e is
-// exact (its magnitude is at most 127, at e = 122 up to 64 and kept to 63),
-// and the addition of 1.5 * 2^23 rounds it to the integer as rint does.
+// exact, so the fma with 1.5 * 2^23 rounds it to the integer as rint does.  Its
+// magnitude is at most 127, but up to 64 at the largest exponent, where 63 is kept.
 __device__ __forceinline__ u32x2 act_codes(const float (&x)[8], uint32_t exp) {
-    const float inv = __uint_as_float((exp == 255u ? 0u : 254u - exp) << 23);
-    const float most = exp >= 249u ? 63.0f : 127.0f;
+    const float inv = __uint_as_float((254u - exp) << 23);
     uint32_t b[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-        b[e] = code_bits(__builtin_amdgcn_fmed3f(x[e] * inv, -most, most));
-    const u32x2 w = {pack_low_bytes(b[0], b[1], b[2], b[3]), pack_low_bytes(b[4], b[5], b[6], b[7])};
-    return exp == 255u ? u32x2{0, 0} : w;
+        b[e] = __float_as_uint(__builtin_fmaf(x[e], inv, kRoundMagic));
+    if (__builtin_expect(exp >= 249u, 0)) {
+        // with 255, a block of Inf or NaN, the codes are 0
+        const float most = exp == 255u ? 0.0f : 63.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float y = exp == 255u ? 0.0f : x[e] * inv;
+            b[e] = code_bits(__builtin_amdgcn_fmed3f(y, -most, most));
+        }
+    }
+    return u32x2{pack_low_bytes(b[0], b[1], b[2], b[3]), pack_low_bytes(b[4], b[5], b[6], b[7])};
 }
 
-// Writes the checkpoint of the elements that the 8 lanes of a block hold.  All
-// 8 lanes take part, with `valid` 0 where a lane is past the row's end.
+// Writes the checkpoint of the elements that the 8 lanes of a block hold, `top`
+// the lane's largest.  All 8 lanes take part, with `valid` 0 and `top` 0 where a
+// lane is past the row's end.
 template <bool RAGGED = true>
 __device__ __forceinline__ void save_chunk(const Mat &m, size_t off, uint32_t valid, size_t block,
-                                           const float (&x)[8]) {
-    const uint32_t exp = act_exp(max8(max_bits(x, RAGGED ? valid : 8)));
+                                           uint32_t top, const float (&x)[8]) {
+    const uint32_t exp = act_exp(max8(top));
     if (valid) {
         const u32x2 w = act_codes(x, exp);
         uint8_t *p = reinterpret_cast<uint8_t *>(m.data) + off;
