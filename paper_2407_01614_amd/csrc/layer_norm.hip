@@ -638,16 +638,16 @@ __global__ __launch_bounds__(kJoinWaves *kWave) void norm_backward_join(
     const float *p = partials + (size_t)blockIdx.y * width + at;
     float sum = 0.0f;
     if (in) {
-        // eight loads at a time; those past the last are not added
-        for (uint32_t i = wave; i < count; i += 8 * kJoinWaves) {
-            float v[8];
+        // sixteen loads at a time; those past the last are not added
+        for (uint32_t i = wave; i < count; i += 16 * kJoinWaves) {
+            float v[16];
 #pragma unroll
-            for (uint32_t u = 0; u < 8; ++u) {
+            for (uint32_t u = 0; u < 16; ++u) {
                 const uint32_t pair = i + u * kJoinWaves;
                 v[u] = p[(size_t)(pair < count ? pair : count - 1) * 2 * width];
             }
 #pragma unroll
-            for (uint32_t u = 0; u < 8; ++u)
+            for (uint32_t u = 0; u < 16; ++u)
                 sum += i + u * kJoinWaves < count ? v[u] : 0.0f;
         }
     }
