@@ -52,17 +52,17 @@ struct Operand {
     const uint8_t *data;  // of token 0
     const uint8_t *exps;
     size_t pitch;         // bytes between tokens
+    size_t span;          // bytes from the first element to past the last
     uint32_t blocks;      // exponents between tokens
     uint32_t col;         // the lane's bytes into a token
     uint32_t at, exp_at;  // its bytes and exponents past a turn's first token
     uint32_t block;       // its exponent's place in a token
-    uint32_t valid;       // elements of its chunk inside the row
     uint32_t margin;      // tokens before the matrix's end whose chunks may pass it
 };
 
 template <int TYPE>
-__device__ __forceinline__ Operand<TYPE> operand(const Mat &m, uint32_t cols, uint32_t col,
-                                                 uint32_t token) {
+__device__ __forceinline__ Operand<TYPE> operand(const Mat &m, size_t rows, uint32_t cols,
+                                                 uint32_t col, uint32_t token) {
     constexpr uint32_t kSize = TYPE == kBf16 ? 2 : 1;
     Operand<TYPE> o;
     const uint32_t last = (cols - 1) / 8 * 8;
@@ -70,12 +70,12 @@ __device__ __forceinline__ Operand<TYPE> operand(const Mat &m, uint32_t cols, ui
     o.data = reinterpret_cast<const uint8_t *>(m.data);
     o.exps = m.exps;
     o.pitch = m.stride * kSize;
+    o.span = (rows - 1) * o.pitch + cols * kSize;
     o.blocks = (cols + kActBlock - 1) / kActBlock;
     o.col = col * kSize;
     o.block = col / kActBlock;
     o.at = token * (uint32_t)o.pitch + o.col;
     o.exp_at = token * o.blocks + o.block;
-    o.valid = cols - col < 8 ? cols - col : 8;
     // the last chunk ends last + 8 - cols elements past its row
     o.margin = cols % 8 ? (uint32_t)((last + 8 - cols + m.stride - 1) / m.stride) : 0;
     return o;
@@ -107,28 +107,45 @@ __device__ __forceinline__ void fetch(Piece<kI8> &p, const Operand<kI8> &o, size
     }
 }
 
-// A token's chunk by itself: whole, or, where that would pass the matrix's end,
-// its `valid` elements one by one.
-__device__ __forceinline__ void fetch_token(Chunk<kBf16> &c, const Operand<kBf16> &o, size_t token,
-                                            bool all) {
-    const uint16_t *p = reinterpret_cast<const uint16_t *>(o.data + token * o.pitch + o.col);
-    if (all) {
-        c.w = ld_at<u32x4, 2>(p);
-        return;
+// Bytes off .. off + size(V) of an operand, which may pass its end by less than
+// that: the last whole vector before the end is loaded then, and moved down to
+// its place (what fills up reaches only results that are not stored).  An
+// operand smaller than one vector is loaded byte by byte.
+template <class V, int A>
+__device__ __forceinline__ V load_inside(const uint8_t *p, size_t off, size_t span) {
+    constexpr size_t kSize = sizeof(V);
+    V v = {};
+    if (__builtin_expect(span < kSize, 0)) {
+        for (size_t b = off; b < span; ++b)
+            v[(b - off) / 4] |= (uint32_t)p[b] << (8 * ((b - off) % 4));
+        return v;
     }
-    for (uint32_t e = 0; e < o.valid; ++e)
-        c.w[e / 2] |= (uint32_t)p[e] << (16 * (e % 2));
+    const uint32_t over = off + kSize > span ? (uint32_t)(off + kSize - span) : 0;
+    v = ld_at<V, A>(p + (off - over));
+    uint64_t w[kSize / 8 + 1] = {};
+    __builtin_memcpy(w, &v, kSize);
+    const uint32_t shift = 8 * (over % 8);
+#pragma unroll
+    for (uint32_t i = 0; i < kSize / 8; ++i) {
+        if (kSize > 8 && over >= 8)
+            w[i] = w[i + 1];
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kSize / 8; ++i)
+        w[i] = shift ? w[i] >> shift | w[i + 1] << (64 - shift) : w[i];
+    __builtin_memcpy(&v, w, kSize);
+    return v;
+}
+__device__ __forceinline__ void fetch_token(Chunk<kBf16> &c, const Operand<kBf16> &o, size_t token,
+                                            bool inside) {
+    const size_t off = token * o.pitch + o.col;
+    c.w = inside ? ld_at<u32x4, 2>(o.data + off) : load_inside<u32x4, 2>(o.data, off, o.span);
 }
 __device__ __forceinline__ void fetch_token(Chunk<kI8> &c, const Operand<kI8> &o, size_t token,
-                                            bool all) {
-    const uint8_t *p = o.data + token * o.pitch + o.col;
+                                            bool inside) {
+    const size_t off = token * o.pitch + o.col;
+    c.codes = inside ? ld_at<u32x2, 1>(o.data + off) : load_inside<u32x2, 1>(o.data, off, o.span);
     c.exp = o.exps[token * o.blocks + o.block];
-    if (all) {
-        c.codes = ld_at<u32x2, 1>(p);
-        return;
-    }
-    for (uint32_t e = 0; e < o.valid; ++e)
-        c.codes[e / 4] |= (uint32_t)p[e] << (8 * (e % 4));
 }
 
 // A turn at the end: tokens from `end` on are zeros.  `token`: the lane's first.
@@ -139,7 +156,7 @@ __device__ __forceinline__ void fetch_end(Piece<TYPE> &p, const Operand<TYPE> &o
     for (uint32_t i = 0; i < 4; ++i) {
         p.t[i] = Chunk<TYPE>{};
         if (token + i < end)
-            fetch_token(p.t[i], o, token + i, o.valid == 8 || token + i + o.margin < rows);
+            fetch_token(p.t[i], o, token + i, token + i + o.margin < rows);
     }
 }
 
@@ -252,8 +269,8 @@ __global__ __launch_bounds__(WAVES_N *WAVES_K *kWave) void weight_grad_kernel(We
     // the lane's piece: neighbouring lanes take the two halves of a unit
     const uint32_t chunk = chunk_of<TILE>(tid / 2 % kChunks), group = tid % 2 + 2 * (tid / (2 * kChunks));
     const uint32_t wn = wave / WAVES_K * (TILE / WAVES_N), wk = wave % WAVES_K * (TILE / WAVES_K);
-    const Operand<kBf16> od = operand<kBf16>(a.dy, a.n, n0 + chunk * 8, group * 4);
-    const Operand<X> ox = operand<X>(a.x, a.k, k0 + chunk * 8, group * 4);
+    const Operand<kBf16> od = operand<kBf16>(a.dy, a.rows, a.n, n0 + chunk * 8, group * 4);
+    const Operand<X> ox = operand<X>(a.x, a.rows, a.k, k0 + chunk * 8, group * 4);
 
     f32x16 acc[MN][MK];
 #pragma unroll
