@@ -716,8 +716,15 @@ template <int TYPE, int V>
 void start_forward(const NormForwardArgs &a, hipStream_t stream) {
     const size_t lanes = ((size_t)a.cols + 8 * V - 1) / (8 * V);
     const uint32_t threads = (uint32_t)((lanes + kWave - 1) / kWave * kWave);
-    // the lanes that the GPU holds at once: 2048 a CU up to 64 registers
-    const size_t fit = (size_t)kCus * ((V == 1 ? 2048 : 1024) / threads);
+    // The workgroups that the GPU holds at once, by a SIMD's waves: 8 of up to 64
+    // registers (bf16), 6 of up to 80 (fp32), 4 with two chunks a lane.  A workgroup
+    // of more than 4 waves is counted with its fullest SIMD's, so that no part of the
+    // grid waits for a second round: 10 waves, of which a CU's lanes hold three times,
+    // fit twice (4096x5120 bf16 with three counted 22.8 us, 18.0 with two; 2048x4544
+    // fp32 with 8 waves a SIMD 23.4, 18.8 so).
+    constexpr uint32_t kWaves = V == 2 ? 4 : TYPE == kF32 ? 6 : 8;
+    const uint32_t waves = threads / kWave;
+    const size_t fit = (size_t)kCus * (waves > 4 ? kWaves / ((waves + 3) / 4) : kWaves * 4 / waves);
     const dim3 grid((unsigned)(a.rows < fit ? a.rows : fit));
     if (a.cols % 8)
         hipLaunchKernelGGL((norm_forward_kernel<TYPE, V, true>), grid, dim3(threads), 0, stream, a);
