@@ -183,19 +183,22 @@ __device__ __forceinline__ float inverse_root(float v) {
 }
 
 // One row a turn, V chunks a lane, the i-th `threads` lanes after the one
-// before.  With V == 1 the next row is on its way while this one's sums are made
-// and gamma and beta stay in registers; two chunks a lane leave no registers for
-// either.
+// before; the next row is on its way while this one's sums are made.  With V == 1
+// gamma and beta stay in registers; two chunks a lane leave none for them, and
+// they lie in LDS as fp32, [2][V][2 halves][threads][4] (8192x16384 bf16, read in
+// each row instead and the next row fetched after it: 190 us, 92 so).
 template <int TYPE, int V, bool RAGGED>
 __global__ __launch_bounds__(kMaxThreads) void norm_forward_kernel(NormForwardArgs a) {
     __shared__ GroupSum<1> scratch;
+    extern __shared__ float shared[];
     const uint32_t blocks = (a.cols + kActBlock - 1) / kActBlock;
     const uint32_t waves = blockDim.x / kWave;
     const float per = 1.0f / (float)a.cols;
     uint32_t turn = 0;
     RowLane l[V];
     float gamma[8], beta[8];
-    auto params = [&](int v) {
+    f32x4 *const params = reinterpret_cast<f32x4 *>(shared) + threadIdx.x;
+    auto params_of = [&](int v) {
         load_param(a.gamma, a.param_type, l[v].col, l[v].in ? 8 : 0, gamma);
         load_param(a.beta, a.param_type, l[v].col, l[v].in ? 8 : 0, beta);
     };
@@ -213,9 +216,32 @@ __global__ __launch_bounds__(kMaxThreads) void norm_forward_kernel(NormForwardAr
             }
     };
     fetch(blockIdx.x);
-    if constexpr (V == 1)
-        params(0);
+    if constexpr (V == 1) {
+        params_of(0);
+    } else {
+        // a lane reads only what it has written
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            params_of(v);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int e = 4 * half;
+                params[(2 * v + half) * blockDim.x] =
+                    f32x4{gamma[e], gamma[e + 1], gamma[e + 2], gamma[e + 3]};
+                params[(2 * (V + v) + half) * blockDim.x] =
+                    f32x4{beta[e], beta[e + 1], beta[e + 2], beta[e + 3]};
+            }
+        }
+    }
     for (size_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        if constexpr (RAGGED && V > 1) {
+            // the masks that follow from `first` are made again in each row: kept,
+            // they take more scalar registers than there are (4096x8201 bf16 38.8 us,
+            // 34.0 so; with one chunk a lane they fit, and 4096x4550 goes from 17.9 to 19.5)
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                asm volatile("" : "+v"(l[v].first));
+        }
         float x[V][8], sum[1] = {0.0f};
         uint32_t top[V];
 #pragma unroll
@@ -235,7 +261,7 @@ __global__ __launch_bounds__(kMaxThreads) void norm_forward_kernel(NormForwardAr
             for (int e = 0; e < 8; ++e)
                 sum[0] += x[v][e];
         }
-        if (V == 1 && row + gridDim.x < a.rows)
+        if (row + gridDim.x < a.rows)
             fetch(row + gridDim.x);
         group_sum(sum, scratch, turn, 0, waves);
         const float mean = sum[0] * per;
@@ -261,8 +287,18 @@ __global__ __launch_bounds__(kMaxThreads) void norm_forward_kernel(NormForwardAr
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             float y[8];
-            if constexpr (V > 1)
-                params(v);
+            if constexpr (V > 1) {
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const f32x4 w = params[(2 * v + half) * blockDim.x];
+                    const f32x4 b = params[(2 * (V + v) + half) * blockDim.x];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        gamma[4 * half + e] = w[e];
+                        beta[4 * half + e] = b[e];
+                    }
+                }
+            }
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 y[e] = __builtin_fmaf((x[v][e] - mean) * rstd, gamma[e], beta[e]);
@@ -271,8 +307,6 @@ __global__ __launch_bounds__(kMaxThreads) void norm_forward_kernel(NormForwardAr
             if (a.saved.data)
                 save_row<RAGGED>(a.saved, row, l[v], blocks, top[v], x[v]);
         }
-        if (V > 1 && row + gridDim.x < a.rows)
-            fetch(row + gridDim.x);
     }
 }
 
@@ -712,8 +746,24 @@ void start_backward(const NormBackwardArgs &a, const RowShape &s, hipStream_t st
 
 namespace {
 
+template <int TYPE, int V, bool RAGGED>
+hipError_t start_forward(const NormForwardArgs &a, dim3 grid, uint32_t threads,
+                         hipStream_t stream) {
+    const size_t lds = V > 1 ? (size_t)threads * V * 2 * 8 * sizeof(float) : 0;
+    if constexpr (V > 1) {
+        // more than 64 KB of LDS has to be asked for, once
+        static const hipError_t allowed = hipFuncSetAttribute(
+            reinterpret_cast<const void *>(norm_forward_kernel<TYPE, V, RAGGED>),
+            hipFuncAttributeMaxDynamicSharedMemorySize, kMaxThreads * V * 2 * 8 * sizeof(float));
+        if (allowed != hipSuccess)
+            return allowed;
+    }
+    hipLaunchKernelGGL((norm_forward_kernel<TYPE, V, RAGGED>), grid, dim3(threads), lds, stream, a);
+    return hipGetLastError();
+}
+
 template <int TYPE, int V>
-void start_forward(const NormForwardArgs &a, hipStream_t stream) {
+hipError_t start_forward(const NormForwardArgs &a, hipStream_t stream) {
     const size_t lanes = ((size_t)a.cols + 8 * V - 1) / (8 * V);
     const uint32_t threads = (uint32_t)((lanes + kWave - 1) / kWave * kWave);
     // The workgroups that the GPU holds at once, by a SIMD's waves: 8 of up to 64
@@ -726,27 +776,26 @@ void start_forward(const NormForwardArgs &a, hipStream_t stream) {
     const uint32_t waves = threads / kWave;
     const size_t fit = (size_t)kCus * (waves > 4 ? kWaves / ((waves + 3) / 4) : kWaves * 4 / waves);
     const dim3 grid((unsigned)(a.rows < fit ? a.rows : fit));
-    if (a.cols % 8)
-        hipLaunchKernelGGL((norm_forward_kernel<TYPE, V, true>), grid, dim3(threads), 0, stream, a);
-    else
-        hipLaunchKernelGGL((norm_forward_kernel<TYPE, V, false>), grid, dim3(threads), 0, stream,
-                           a);
+    return a.cols % 8 ? start_forward<TYPE, V, true>(a, grid, threads, stream)
+                      : start_forward<TYPE, V, false>(a, grid, threads, stream);
 }
 
 }  // namespace
 
 hipError_t launch_norm_forward(const NormForwardArgs &a, int type, hipStream_t stream) {
-    return with_type(type, [&](auto t) {
+    hipError_t e = hipSuccess;
+    const hipError_t last = with_type(type, [&](auto t) {
         constexpr int T = decltype(t)::value;
         if (a.cols < 8 || a.cols > 2 * kMostRegCols)
             hipLaunchKernelGGL((norm_forward_long_kernel<T>),
                                dim3((unsigned)(a.rows < 2 * kCus ? a.rows : 2 * kCus)),
                                dim3(kMaxThreads), 0, stream, a);
         else if (a.cols <= kMostRegCols)
-            start_forward<T, 1>(a, stream);
+            e = start_forward<T, 1>(a, stream);
         else
-            start_forward<T, 2>(a, stream);
+            e = start_forward<T, 2>(a, stream);
     });
+    return e != hipSuccess ? e : last;
 }
 
 size_t norm_backward_workspace(size_t rows, size_t cols) {

@@ -602,3 +602,25 @@ def test_weight_grad_of_tokens_far_apart(zpp):
     near, x = ref.values(rows, n, 1, BF16), ref.values(rows, k, 2, BF16)
     dy.copy_(near)
     assert same(run_grad(zpp, dy, x, n, k), run_grad(zpp, near, x, n, k))
+
+
+# Two chunks a lane, several rows a workgroup: the next row fetched while one is
+# summed, partial last chunks among them
+@TYPES
+@pytest.mark.parametrize("rows,cols,pad", [(700, 8201, 0), (531, 14847, 3), (513, 12288, 1)])
+def test_norm_forward_of_many_long_rows(zpp, rows, cols, pad, dtype):
+    eps = 1e-5
+    x, r = ref.values(rows, cols, 1, dtype, pad), ref.values(rows, cols, 2, dtype)
+    gamma, beta = norm_params(cols, dtype, 3)
+    y, total = ref.matrix(rows, cols, dtype, pad), ref.matrix(rows, cols, dtype)
+    mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    saved = zpp.empty_checkpoint(rows, cols)
+    zpp.layer_norm_forward(x, gamma, beta, y, mean, rstd, eps=eps, residual=r, total=total,
+                           saved=saved)
+    assert torch.equal(total, (x.float() + r.float()).to(dtype))
+    want, bound = ref.norm_forward(total.double(), gamma.double(), beta.double(), eps, dtype)
+    for got, w, b, what in zip((y, mean, rstd), want, bound, ("y", "mean", "rstd")):
+        ref.check(got, w, b, what)
+    codes, exps = ref.encode(total.float().cpu().numpy())
+    assert np.array_equal(saved[0].cpu().numpy(), codes)
+    assert np.array_equal(saved[1].cpu().numpy(), exps)
