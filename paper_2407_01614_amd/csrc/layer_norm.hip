@@ -3,8 +3,8 @@
 // A row of up to 8192 features lives in the registers of one workgroup, eight
 // consecutive elements a lane, so HBM is read once and the mean is known before
 // the squares are summed.  A row's lanes are as many as it asks for, in whole
-// waves (4544 features: 568 chunks on 576 lanes).  The forward pass takes rows of
-// up to 16384 so, two chunks a lane; longer rows are read again for each sum.
+// waves (4544 features: 568 chunks on 576 lanes).  Rows of up to 16384 are held
+// so with two chunks a lane; longer ones are read again for each sum.
 //
 // RAGGED: rows whose last chunk of 8 is partial.  The lane that has it takes the
 // row's last 8 elements instead and leaves out those that are the lane's before
@@ -69,11 +69,12 @@ __device__ __forceinline__ void load_param(const void *p, int type, uint32_t col
         x[e] = 0.0f;
     if (!p || !valid)
         return;
-    const Mat m = {const_cast<void *>(p), nullptr, 0};
+    uint8_t *at = reinterpret_cast<uint8_t *>(const_cast<void *>(p)) + col * (type == kF32 ? 4 : 2);
+    const Mat m = {at, nullptr, 0};
     if (type == kF32)
-        chunk_values(load_chunk<kF32>(m, col, valid, 0), x);
+        chunk_values(load_chunk<kF32>(m, 0, valid, 0), x);
     else
-        chunk_values(load_chunk<kBf16>(m, col, valid, 0), x);
+        chunk_values(load_chunk<kBf16>(m, 0, valid, 0), x);
 }
 
 __device__ __forceinline__ uint32_t valid_at(uint32_t col, uint32_t cols) {
@@ -102,28 +103,40 @@ __device__ __forceinline__ RowLane row_lane(uint32_t lane, uint32_t cols) {
     return l;
 }
 
+// A lane's elements of a row: the row's address is the same in all lanes and stays
+// in scalar registers, a lane adds 32 bits.
+template <int TYPE>
+__device__ __forceinline__ Mat lane_at(const Mat &m, size_t row, const RowLane &l,
+                                       uint32_t blocks) {
+    constexpr uint32_t kSize = TYPE == kF32 ? 4 : TYPE == kBf16 ? 2 : 1;
+    Mat at = m;
+    at.data = reinterpret_cast<uint8_t *>(m.data) + row * m.stride * kSize + l.col * kSize;
+    if (TYPE == kI8)
+        at.exps = m.exps + row * blocks + l.block;
+    return at;
+}
+
 template <int TYPE>
 __device__ __forceinline__ Chunk<TYPE> load_row(const Mat &m, size_t row, const RowLane &l,
                                                 uint32_t blocks) {
-    return load_chunk<TYPE, false>(m, row * m.stride + l.col, 8, row * blocks + l.block);
+    return load_chunk<TYPE, false>(lane_at<TYPE>(m, row, l, blocks), 0, 8, 0);
 }
 
 template <int TYPE, bool RAGGED>
 __device__ __forceinline__ void store_row(const Mat &m, size_t row, const RowLane &l,
                                           const Chunk<TYPE> &c) {
-    const size_t off = row * m.stride + l.col;
+    const Mat at = lane_at<TYPE>(m, row, l, 0);
     if (!RAGGED || l.first == 0) {
-        store_chunk<TYPE, false>(m, off, 8, c);
+        store_chunk<TYPE, false>(at, 0, 8, c);
         return;
     }
 #pragma unroll
     for (uint32_t e = 1; e < 8; ++e)
         if (e >= l.first) {
             if constexpr (TYPE == kBf16)
-                reinterpret_cast<uint16_t *>(m.data)[off + e] =
-                    (uint16_t)(c.w[e / 2] >> (16 * (e % 2)));
+                reinterpret_cast<uint16_t *>(at.data)[e] = (uint16_t)(c.w[e / 2] >> (16 * (e % 2)));
             else
-                reinterpret_cast<float *>(m.data)[off + e] = e < 4 ? c.lo[e] : c.hi[e - 4];
+                reinterpret_cast<float *>(at.data)[e] = e < 4 ? c.lo[e] : c.hi[e - 4];
         }
 }
 
@@ -136,7 +149,8 @@ __device__ __forceinline__ void save_row(const Mat &m, size_t row, const RowLane
     if (!l.in)
         return;
     const u32x2 w = act_codes(x, exp);
-    uint8_t *p = reinterpret_cast<uint8_t *>(m.data) + row * m.stride + l.col;
+    const Mat at = lane_at<kI8>(m, row, l, blocks);
+    uint8_t *p = reinterpret_cast<uint8_t *>(at.data);
     if (!RAGGED || l.first == 0) {
         st_nt_at<u32x2, 1>(p, w);
     } else {
@@ -146,7 +160,7 @@ __device__ __forceinline__ void save_row(const Mat &m, size_t row, const RowLane
                 p[e] = (uint8_t)(w[e / 4] >> (8 * (e % 4)));
     }
     if ((threadIdx.x & 7) == 0)
-        m.exps[row * blocks + l.block] = (uint8_t)exp;
+        *at.exps = (uint8_t)exp;
 }
 
 // Elements that are not the lane's set to 0.
@@ -389,16 +403,19 @@ __global__ __launch_bounds__(kMaxThreads) void norm_forward_long_kernel(NormForw
 // [2][cols] a workgroup, which a second kernel adds in a fixed order.
 struct RowShape {
     uint32_t threads;  // lanes of a row; 0: the row does not fit registers
+    uint32_t chunks;   // chunks of 8 that they hold, one or two each
     uint32_t teams;    // rows side by side in a workgroup of the backward pass
     uint32_t grid;     // its workgroups, pairs of arrays in the workspace
 };
 
 RowShape row_shape(size_t rows, size_t cols) {
-    RowShape s = {0, 0, 0};
-    if (cols > kMostRegCols || cols < 8)
+    RowShape s = {0, 0, 0, 0};
+    if (cols > 2 * kMostRegCols || cols < 8)
         return s;
-    const size_t chunks = (cols + 7) / 8;
-    s.threads = (uint32_t)((chunks + kWave - 1) / kWave * kWave);
+    const uint32_t each = cols > kMostRegCols ? 2 : 1;
+    const size_t lanes = ((cols + 7) / 8 + each - 1) / each;
+    s.threads = (uint32_t)((lanes + kWave - 1) / kWave * kWave);
+    s.chunks = s.threads * each;
     s.teams = kMaxThreads / s.threads;
     const size_t groups = (rows + s.teams - 1) / s.teams;
     s.grid = (uint32_t)(groups < kCus ? groups : kCus);
@@ -549,6 +566,161 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward_kernel(NormBackward
     }
 }
 
+// Two chunks a lane, in 128 registers: gamma and the rows' sum of dy lie in LDS as
+// fp32, the row itself stays as it was loaded and is unpacked again after its
+// sums, and beta is read where it is used.  From bf16 the next row is fetched
+// ahead; fp32, and bf16 that also writes y, leave no registers for that and fetch
+// a row when its turn comes.  A lane past the row takes the row's last chunk, so
+// that no load is in a branch, and clears it.  8192x12288, dx and the weights'
+// gradients: bf16 109 us, fp32 260; as long rows, read twice, 212 and 440.
+template <int TYPE, int X, bool AGAIN, bool RAGGED>
+__global__ __launch_bounds__(kMaxThreads) void norm_backward_wide_kernel(NormBackwardArgs a) {
+    constexpr bool kAhead = TYPE == kBf16 && !AGAIN;
+    constexpr bool kEarly = TYPE == kBf16;  // dresidual is fetched before the sums
+    __shared__ GroupSum<2> scratch;
+    // gamma, then the sum of dy, [2][2 halves][2 chunks][kMaxThreads][4]
+    extern __shared__ float shared[];
+    const uint32_t blocks = (a.cols + kActBlock - 1) / kActBlock;
+    const uint32_t threads = blockDim.x, waves = threads / kWave;
+    const float per = 1.0f / (float)a.cols;
+    uint32_t turn = 0;
+    RowLane l[2];
+    float dg[2][8];
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+        l[v] = row_lane<RAGGED>(v * threads + threadIdx.x, a.cols);
+        if (!l[v].in) {
+            l[v].col = a.cols - 8;
+            l[v].block = l[v].col / kActBlock;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            dg[v][e] = 0.0f;
+    }
+    // a lane reads only what it has written
+    f32x4 *const params = reinterpret_cast<f32x4 *>(shared) + threadIdx.x;
+    auto param = [&](int v, float (&p)[8]) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const f32x4 q = params[(2 * half + v) * kMaxThreads];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                p[4 * half + e] = q[e];
+        }
+    };
+    Chunk<TYPE> nd[2], cd[2], cr[2];
+    Chunk<X> nx[2], cx[2];
+    float stat[2];
+    auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+    auto fetch = [&](size_t row) {
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+            nd[v] = load_row<TYPE>(a.dy, row, l[v], blocks);
+            nx[v] = load_row<X>(a.x, row, l[v], blocks);
+        }
+        stat[0] = a.mean[row];
+        stat[1] = a.rstd[row];
+    };
+    if (kAhead)
+        fetch(blockIdx.x);
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+        float p[8];
+        load_param(a.gamma, a.param_type, l[v].col, l[v].in ? 8 : 0, p);
+        params[v * kMaxThreads] = f32x4{p[0], p[1], p[2], p[3]};
+        params[(2 + v) * kMaxThreads] = f32x4{p[4], p[5], p[6], p[7]};
+        params[(4 + v) * kMaxThreads] = params[(6 + v) * kMaxThreads] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    for (size_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        // addresses and masks are made again in each row: kept, they take registers
+#pragma unroll
+        for (int v = 0; v < 2; ++v)
+            asm volatile("" : "+v"(l[v].first), "+v"(l[v].col), "+v"(l[v].block));
+        if (!kAhead)
+            fetch(row);
+        const float mean = stat[0], scale = stat[1];
+        float s[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+            float d[8], g[8], h[8];
+            cd[v] = l[v].in ? nd[v] : Chunk<TYPE>{};
+            cx[v] = l[v].in ? nx[v] : Chunk<X>{};
+            fence();
+            chunk_values(cd[v], d);
+            clear_others<RAGGED>(d, l[v]);
+            chunk_values(cx[v], h);
+            params[(4 + v) * kMaxThreads] += f32x4{d[0], d[1], d[2], d[3]};
+            params[(6 + v) * kMaxThreads] += f32x4{d[4], d[5], d[6], d[7]};
+            param(v, g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                h[e] = (h[e] - mean) * scale;
+                dg[v][e] = __builtin_fmaf(d[e], h[e], dg[v][e]);
+                g[e] *= d[e];
+                s[0] += g[e];
+                s[1] = __builtin_fmaf(g[e], h[e], s[1]);
+            }
+        }
+        fence();
+        if (kEarly && a.dresidual.data) {
+#pragma unroll
+            for (int v = 0; v < 2; ++v)
+                cr[v] = load_row<TYPE>(a.dresidual, row, l[v], blocks);
+        }
+        if (kAhead && row + gridDim.x < a.rows)
+            fetch(row + gridDim.x);
+        group_sum(s, scratch, turn, 0, waves);
+        const float c1 = s[0] * per, c2 = s[1] * per;
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+            if (!l[v].in)
+                continue;
+            fence();
+            hold(cd[v]);
+            hold(cx[v]);
+            float d[8], g[8], h[8];
+            chunk_values(cd[v], d);
+            chunk_values(cx[v], h);
+            param(v, g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                h[e] = (h[e] - mean) * scale;
+                d[e] = scale * __builtin_fmaf(-h[e], c2, g[e] * d[e] - c1);
+            }
+            if (a.dresidual.data) {
+                float past[8];
+                if (!kEarly)
+                    cr[v] = load_row<TYPE>(a.dresidual, row, l[v], blocks);
+                chunk_values(cr[v], past);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    d[e] += past[e];
+            }
+            store_row<TYPE, RAGGED>(a.dx, row, l[v], make_chunk<TYPE>(d));
+            if constexpr (AGAIN) {
+                fence();
+                float y[8];
+                load_param(a.beta, a.param_type, l[v].col, 8, y);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    y[e] = __builtin_fmaf(h[e], g[e], y[e]);
+                store_row<TYPE, RAGGED>(a.y, row, l[v], make_chunk<TYPE>(y));
+            }
+        }
+    }
+    if (!a.partials)
+        return;
+    f32x4 *const out =
+        reinterpret_cast<f32x4 *>(a.partials) + (size_t)blockIdx.x * 8 * threads + threadIdx.x;
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+        out[v * threads] = f32x4{dg[v][0], dg[v][1], dg[v][2], dg[v][3]};
+        out[(2 + v) * threads] = f32x4{dg[v][4], dg[v][5], dg[v][6], dg[v][7]};
+        out[(4 + v) * threads] = params[(4 + v) * kMaxThreads];
+        out[(6 + v) * threads] = params[(6 + v) * kMaxThreads];
+    }
+}
+
 // Rows too long for registers: the rows' two sums by one kernel (into the
 // workspace's head), then dx and the weights' gradients column strip by strip.
 template <int TYPE, int X>
@@ -645,10 +817,10 @@ __global__ __launch_bounds__(kStripThreads) void norm_backward_long_kernel(NormB
 
 // The workgroups' pairs of arrays added: 64 columns a workgroup, its 16 waves
 // taking every 16th pair, joined in order.  An array holds `width` columns, in
-// their order (threads == 0) or as the register kernels lay them out.
+// their order (chunks == 0) or as the register kernels lay them out.
 constexpr uint32_t kJoinWaves = 16;
 __global__ __launch_bounds__(kJoinWaves *kWave) void norm_backward_join(
-    const float *partials, uint32_t count, uint32_t width, uint32_t threads, uint32_t cols,
+    const float *partials, uint32_t count, uint32_t width, uint32_t chunks, uint32_t cols,
     float *dgamma, float *dbeta, int accumulate) {
     __shared__ float part[kJoinWaves][kWave];
     const uint32_t wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
@@ -658,8 +830,8 @@ __global__ __launch_bounds__(kJoinWaves *kWave) void norm_backward_join(
     const uint32_t at = blockIdx.x * kWave + lane;
     uint32_t col = at;
     bool in = at < width;
-    if (threads && in) {
-        const uint32_t half = at / (4 * threads), i = at % (4 * threads);
+    if (chunks && in) {
+        const uint32_t half = at / (4 * chunks), i = at % (4 * chunks);
         const uint32_t e = 4 * half + i % 4, start = i / 4 * 8;
         // a last, partial chunk holds the row's last 8 columns
         in = start < cols;
@@ -695,14 +867,11 @@ __global__ __launch_bounds__(kJoinWaves *kWave) void norm_backward_join(
     }
 }
 
-// Calls f(std::integral_constant<int, type>()).
+// f(std::integral_constant<int, type>()).
 template <class F>
 hipError_t with_type(int type, F &&f) {
-    if (type == kBf16)
-        f(std::integral_constant<int, kBf16>());
-    else
-        f(std::integral_constant<int, kF32>());
-    return hipGetLastError();
+    return type == kBf16 ? f(std::integral_constant<int, kBf16>())
+                         : f(std::integral_constant<int, kF32>());
 }
 
 uint32_t long_row_groups(size_t rows, size_t cols) {
@@ -711,27 +880,36 @@ uint32_t long_row_groups(size_t rows, size_t cols) {
     return (uint32_t)(groups < rows ? groups : rows);
 }
 
-template <int TYPE, int X, bool AGAIN>
-void start_backward(const NormBackwardArgs &a, const RowShape &s, hipStream_t stream) {
-    const size_t params = 2 * 2 * sizeof(f32x4), sums = s.teams > 1 ? 2 * sizeof(f32x4) * s.teams : 0;
-    const size_t lds = s.threads * (params > sums ? params : sums);
+template <int TYPE, int X, bool AGAIN, bool RAGGED>
+hipError_t start_backward(const NormBackwardArgs &a, const RowShape &s, hipStream_t stream) {
     const dim3 grid(s.grid), threads(s.threads * s.teams);
-    if (a.cols % 8)
-        hipLaunchKernelGGL((norm_backward_kernel<TYPE, X, AGAIN, true>), grid, threads,
-                           lds, stream, a, s.threads, s.teams);
-    else
-        hipLaunchKernelGGL((norm_backward_kernel<TYPE, X, AGAIN, false>), grid,
-                           threads, lds, stream, a, s.threads, s.teams);
+    if (s.chunks > s.threads) {
+        constexpr size_t kLds = 2 * 2 * 2 * kMaxThreads * sizeof(f32x4);
+        // more than 64 KB of LDS has to be asked for, once
+        static const hipError_t allowed = hipFuncSetAttribute(
+            reinterpret_cast<const void *>(norm_backward_wide_kernel<TYPE, X, AGAIN, RAGGED>),
+            hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
+        if (allowed != hipSuccess)
+            return allowed;
+        hipLaunchKernelGGL((norm_backward_wide_kernel<TYPE, X, AGAIN, RAGGED>), grid, threads, kLds,
+                           stream, a);
+        return hipGetLastError();
+    }
+    const size_t params = (AGAIN ? 2 : 1) * 2 * sizeof(f32x4) * s.threads;
+    const size_t sums = s.teams > 1 ? 2 * sizeof(f32x4) * s.teams * s.threads : 0;
+    hipLaunchKernelGGL((norm_backward_kernel<TYPE, X, AGAIN, RAGGED>), grid, threads,
+                       params > sums ? params : sums, stream, a, s.threads, s.teams);
+    return hipGetLastError();
 }
 
 template <int TYPE, int X>
-void start_backward(const NormBackwardArgs &a, const RowShape &s, hipStream_t stream) {
+hipError_t start_backward(const NormBackwardArgs &a, const RowShape &s, hipStream_t stream) {
     if (s.threads) {
-        if (a.y.data)
-            start_backward<TYPE, X, true>(a, s, stream);
-        else
-            start_backward<TYPE, X, false>(a, s, stream);
-        return;
+        if (a.cols % 8)
+            return a.y.data ? start_backward<TYPE, X, true, true>(a, s, stream)
+                            : start_backward<TYPE, X, false, true>(a, s, stream);
+        return a.y.data ? start_backward<TYPE, X, true, false>(a, s, stream)
+                        : start_backward<TYPE, X, false, false>(a, s, stream);
     }
     const dim3 strips((a.cols + 8 * kStripThreads - 1) / (8 * kStripThreads),
                       long_row_groups(a.rows, a.cols));
@@ -740,6 +918,7 @@ void start_backward(const NormBackwardArgs &a, const RowShape &s, hipStream_t st
                        stream, a);
     hipLaunchKernelGGL((norm_backward_long_kernel<TYPE, X>), strips, dim3(kStripThreads), 0, stream,
                        a);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -783,19 +962,16 @@ hipError_t start_forward(const NormForwardArgs &a, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_norm_forward(const NormForwardArgs &a, int type, hipStream_t stream) {
-    hipError_t e = hipSuccess;
-    const hipError_t last = with_type(type, [&](auto t) {
+    return with_type(type, [&](auto t) {
         constexpr int T = decltype(t)::value;
-        if (a.cols < 8 || a.cols > 2 * kMostRegCols)
-            hipLaunchKernelGGL((norm_forward_long_kernel<T>),
-                               dim3((unsigned)(a.rows < 2 * kCus ? a.rows : 2 * kCus)),
-                               dim3(kMaxThreads), 0, stream, a);
-        else if (a.cols <= kMostRegCols)
-            e = start_forward<T, 1>(a, stream);
-        else
-            e = start_forward<T, 2>(a, stream);
+        if (a.cols >= 8 && a.cols <= 2 * kMostRegCols)
+            return a.cols <= kMostRegCols ? start_forward<T, 1>(a, stream)
+                                          : start_forward<T, 2>(a, stream);
+        hipLaunchKernelGGL((norm_forward_long_kernel<T>),
+                           dim3((unsigned)(a.rows < 2 * kCus ? a.rows : 2 * kCus)),
+                           dim3(kMaxThreads), 0, stream, a);
+        return hipGetLastError();
     });
-    return e != hipSuccess ? e : last;
 }
 
 size_t norm_backward_workspace(size_t rows, size_t cols) {
@@ -803,7 +979,7 @@ size_t norm_backward_workspace(size_t rows, size_t cols) {
         return 0;
     const RowShape s = row_shape(rows, cols);
     if (s.threads)
-        return (size_t)s.grid * 2 * s.threads * 8 * sizeof(float);
+        return (size_t)s.grid * 2 * s.chunks * 8 * sizeof(float);
     return (2 * rows + (size_t)long_row_groups(rows, cols) * 2 * cols) * sizeof(float);
 }
 
@@ -817,10 +993,8 @@ hipError_t launch_norm_backward(const NormBackwardArgs &args, int type, int x_ty
     if (a.rows) {
         const hipError_t e = with_type(type, [&](auto t) {
             constexpr int T = decltype(t)::value;
-            if (x_type == kI8)
-                start_backward<T, kI8>(a, s, stream);
-            else
-                start_backward<T, T>(a, s, stream);
+            return x_type == kI8 ? start_backward<T, kI8>(a, s, stream)
+                                 : start_backward<T, T>(a, s, stream);
         });
         if (e != hipSuccess)
             return e;
@@ -830,9 +1004,9 @@ hipError_t launch_norm_backward(const NormBackwardArgs &args, int type, int x_ty
     const uint32_t pairs =
         !a.rows ? 0 : s.threads ? s.grid : long_row_groups(a.rows, a.cols);
     const float *partials = args.partials + (s.threads ? 0 : 2 * a.rows);
-    const uint32_t width = s.threads ? s.threads * 8 : a.cols;
+    const uint32_t width = s.threads ? s.chunks * 8 : a.cols;
     hipLaunchKernelGGL(norm_backward_join, dim3((width + kWave - 1) / kWave, 2),
-                       dim3(kJoinWaves * kWave), 0, stream, partials, pairs, width, s.threads,
+                       dim3(kJoinWaves * kWave), 0, stream, partials, pairs, width, s.chunks,
                        a.cols, a.dgamma, a.dbeta, a.accumulate);
     return hipGetLastError();
 }

@@ -624,3 +624,65 @@ def test_norm_forward_of_many_long_rows(zpp, rows, cols, pad, dtype):
     codes, exps = ref.encode(total.float().cpu().numpy())
     assert np.array_equal(saved[0].cpu().numpy(), codes)
     assert np.array_equal(saved[1].cpu().numpy(), exps)
+
+
+@pytest.mark.parametrize("again", [False, True], ids=["plain", "again"])
+@pytest.mark.parametrize("from_saved", [False, True], ids=["same", "i8"])
+@TYPES
+@pytest.mark.parametrize("rows,cols,pad", [(1, 8208, 0), (700, 8201, 3), (300, 14847, 0),
+                                           (513, 12288, 1)])
+def test_norm_backward_of_long_rows(zpp, rows, cols, pad, dtype, from_saved, again):
+    """Two chunks a lane, from one row to several a workgroup."""
+    x = ref.values(rows, cols, 7, dtype, pad)
+    dy = ref.values(rows, cols, 8, dtype, pad, std=1e-3)
+    dres = ref.values(rows, cols, 9, dtype, std=1e-3) if again else None
+    gamma, beta = norm_params(cols, F32 if from_saved else dtype, 10)
+    mean = x.float().mean(1)
+    rstd = torch.rsqrt((x.float() - mean[:, None]).square().mean(1) + 1e-5)
+    arg, xs = ref.saved(x) if from_saved else (x, x.double())
+    want, bound = ref.norm_backward(dy.double(), xs, gamma.double(), beta.double(), mean.double(),
+                                    rstd.double(), None if dres is None else dres.double(), dtype)
+    dx = ref.matrix(rows, cols, dtype, pad, fill=5.0)
+    y = ref.matrix(rows, cols, dtype, 3) if again else None
+    dg, db = torch.full((cols,), 7.0, device="cuda"), torch.full((cols,), 7.0, device="cuda")
+    ws = torch.empty(zpp.layer_norm_backward_workspace(rows, cols), dtype=torch.uint8,
+                     device="cuda").fill_(0xFF)
+    zpp.layer_norm_backward(dy, arg, gamma, mean, rstd, dx, dg, db, ws, dresidual=dres,
+                            beta=beta if again else None, y=y)
+    for got, w, b, what in zip((dx, dg, db, y), want, bound, ("dx", "dgamma", "dbeta", "y")):
+        if got is not None:
+            ref.check(got, w, b, what)
+    if pad and rows > 1:
+        gaps = dx.as_strided((rows - 1, pad), (cols + pad, 1), dx.storage_offset() + cols)
+        assert bool((gaps == 5.0).all())
+    ag, ab, once = dg.clone(), db.clone(), dx.clone()
+    zpp.layer_norm_backward(dy, arg, gamma, mean, rstd, dx, ag, ab, ws, dresidual=dres,
+                            beta=beta if again else None, y=y, accumulate=True)
+    assert same(dx, once) and same(ag, dg + dg) and same(ab, db + db)
+
+
+@TYPES
+def test_norm_backward_of_long_rows_keeps_a_rows_infinity_to_itself(zpp, dtype):
+    """A row whose last element has no value: no other row's dx changes, and of the
+    weights' gradients that column alone."""
+    rows, cols = 5, 8201
+    x, dy = ref.values(rows, cols, 7, dtype), ref.values(rows, cols, 8, dtype, std=1e-3)
+    gamma, _ = norm_params(cols, dtype, 10)
+    mean = x.float().mean(1)
+    rstd = torch.rsqrt((x.float() - mean[:, None]).square().mean(1) + 1e-5)
+    ws = torch.empty(zpp.layer_norm_backward_workspace(rows, cols), dtype=torch.uint8,
+                     device="cuda")
+    results = []
+    for value in (0.5, float("inf"), float("nan")):
+        x[2, cols - 1] = value
+        dx, dg, db = ref.matrix(rows, cols, dtype), torch.empty(cols, device="cuda"), \
+            torch.empty(cols, device="cuda")
+        zpp.layer_norm_backward(dy, x, gamma, mean, rstd, dx, dg, db, ws)
+        results.append((dx, dg, db))
+    clean = results[0]
+    others = [0, 1, 3, 4]
+    for dx, dg, db in results[1:]:
+        assert same(dx[others].contiguous(), clean[0][others].contiguous())
+        assert same(dg[:-1], clean[1][:-1]) and same(db, clean[2])
+        assert not bool(torch.isfinite(dg[-1]))
+        assert not bool(torch.isfinite(dx[2]).any())
