@@ -268,7 +268,8 @@ __global__ __launch_bounds__(WAVES_N *WAVES_K *kWave) void weight_grad_kernel(We
 
     // the lane's piece: neighbouring lanes take the two halves of a unit
     const uint32_t chunk = chunk_of<TILE>(tid / 2 % kChunks), group = tid % 2 + 2 * (tid / (2 * kChunks));
-    const uint32_t wn = wave / WAVES_K * (TILE / WAVES_N), wk = wave % WAVES_K * (TILE / WAVES_K);
+    const uint32_t wn = (uint32_t)__builtin_amdgcn_readfirstlane((int)(wave / WAVES_K)) * (TILE / WAVES_N);
+    const uint32_t wk = wave % WAVES_K * (TILE / WAVES_K);
     const Operand<kBf16> od = operand<kBf16>(a.dy, a.rows, a.n, n0 + chunk * 8, group * 4);
     const Operand<X> ox = operand<X>(a.x, a.rows, a.k, k0 + chunk * 8, group * 4);
 
@@ -447,22 +448,59 @@ __global__ __launch_bounds__(WAVES_N *WAVES_K *kWave) void weight_grad_kernel(We
         out = a.parts + ((size_t)split * tail + (tile - a.whole)) * (TILE * TILE);
         stride = TILE;
     }
-    const bool add = direct && a.accumulate;
+    // A lane's rows are apart by multiples of the stride that are the same in all
+    // lanes.  Sixteen of dw's elements are on their way at a time where dw is added
+    // to, and rows are checked in the last row of tiles alone, by groups of eight.
+    auto store = [&](auto add, auto check) {
 #pragma unroll
-    for (int j = 0; j < MK; ++j) {
-        const uint32_t col = wk + j * 32 + lane % 32;
-        if (k0 + col >= a.k)
-            continue;
+        for (int j = 0; j < MK; ++j) {
+            const uint32_t col = wk + j * 32 + lane % 32;
+            if (k0 + col >= a.k)
+                continue;
+            const uint32_t row = wn + 4 * (lane / 32);
+            float *p = out + row * stride + col;
 #pragma unroll
-        for (int i = 0; i < MN; ++i)
+            for (int i = 0; i < MN; ++i) {
+                // f(r, q) for the rows that there are
+                auto rows = [&](auto &&f) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const uint32_t row = wn + i * 32 + 8 * (r / 4) + 4 * (lane / 32) + r % 4;
-                if (n0 + row < a.n) {
-                    float *p = out + row * stride + col;
-                    *p = add ? *p + acc[i][j][r] : acc[i][j][r];
+                    for (int g = 0; g < 4; ++g) {
+                        const uint32_t first = n0 + wn + i * 32 + 8 * g;
+                        float *q = p + (i * 32 + 8 * g) * stride;
+                        if (!decltype(check)::value || first + 8 <= a.n) {
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                f(4 * g + r, q + r * stride);
+                        } else if (first < a.n) {
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                if (first + 4 * (lane / 32) + r < a.n)
+                                    f(4 * g + r, q + r * stride);
+                        }
+                    }
+                };
+                if constexpr (decltype(add)::value) {
+                    float was[16];
+                    rows([&](int r, const float *q) { was[r] = *q; });
+                    rows([&](int r, float *q) { *q = was[r] + acc[i][j][r]; });
+                } else {
+                    rows([&](int r, float *q) { *q = acc[i][j][r]; });
                 }
             }
+        }
+    };
+    constexpr std::true_type yes;
+    constexpr std::false_type no;
+    const bool check = direct && a.n - n0 < TILE;
+    if (direct && a.accumulate) {
+        if (check)
+            store(yes, yes);
+        else
+            store(yes, no);
+    } else if (check) {
+        store(no, yes);
+    } else {
+        store(no, no);
     }
 }
 

@@ -686,3 +686,25 @@ def test_norm_backward_of_long_rows_keeps_a_rows_infinity_to_itself(zpp, dtype):
         assert same(dg[:-1], clean[1][:-1]) and same(db, clean[2])
         assert not bool(torch.isfinite(dg[-1]))
         assert not bool(torch.isfinite(dx[2]).any())
+
+
+# Rows of dw that end inside a tile's group of eight, at its edge, and inside the
+# lower half of a tile; added to what is there, in rows that lie apart
+@pytest.mark.parametrize("rows", [1, 200])
+@pytest.mark.parametrize("n,k", [(3, 5), (12, 130), (136, 8), (205, 33), (1000, 777), (259, 300)])
+def test_weight_grad_adds_at_ragged_ends(zpp, rows, n, k):
+    dy, x = ref.values(rows, n, 1, BF16, std=1e-3), ref.values(rows, k, 2, BF16)
+    want, bound = ref.weight_grad(dy.double(), x.double())
+    dw = ref.matrix(n, k, F32, 3, 1, fill=9.0)
+    ws = torch.empty(zpp.weight_grad_workspace(rows, n, k), dtype=torch.uint8, device="cuda")
+    zpp.weight_grad(dy, x, dw, ws)
+    ref.check(dw, want, bound, "dw")
+    once = dw.clone()
+    before = torch.randn(n, k, device="cuda")
+    dw.copy_(before)
+    zpp.weight_grad(dy, x, dw, ws, accumulate=True)
+    # one rounding of the same sum and what was there
+    assert same(dw, before + once)
+    if n > 1:
+        gaps = dw.as_strided((n - 1, 3), (k + 3, 1), dw.storage_offset() + k)
+        assert bool((gaps == 9.0).all())
