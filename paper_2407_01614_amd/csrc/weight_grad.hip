@@ -450,7 +450,9 @@ __global__ __launch_bounds__(WAVES_N *WAVES_K *kWave) void weight_grad_kernel(We
     }
     // A lane's rows are apart by multiples of the stride that are the same in all
     // lanes.  Sixteen of dw's elements are on their way at a time where dw is added
-    // to, and rows are checked in the last row of tiles alone, by groups of eight.
+    // to, and rows are checked in the last row of tiles alone, by groups of eight
+    // (each element checked and addressed by itself: 1x300x300 7.9 us, 5.2 so;
+    // 128x4544x18176 added to dw 384, 144).
     auto store = [&](auto add, auto check) {
 #pragma unroll
         for (int j = 0; j < MK; ++j) {
@@ -504,9 +506,10 @@ __global__ __launch_bounds__(WAVES_N *WAVES_K *kWave) void weight_grad_kernel(We
     }
 }
 
-// dw (+)= the tail tiles' splits, in order: a workgroup takes 4 rows of a tile,
-// lanes neighbouring columns.
-constexpr uint32_t kJoinRows = 4;
+// dw (+)= the tail tiles' splits, in order: a workgroup takes 2 rows of a tile,
+// lanes neighbouring columns.  Loads wait for each other's splits no more than they
+// have to (one split at a time, 4 rows: 8192x128x128 25.2 us, 11.8 so).
+constexpr uint32_t kJoinRows = 2;
 template <int TILE>
 __global__ __launch_bounds__(TILE) void weight_grad_join(WeightGradArgs a) {
     const uint32_t tail = a.tiles_n * a.tiles_k - a.whole;
@@ -520,11 +523,29 @@ __global__ __launch_bounds__(TILE) void weight_grad_join(WeightGradArgs a) {
     // rows past the last are the last again, and not stored
     const uint32_t rows = a.n - n0 < kJoinRows ? a.n - n0 : kJoinRows;
     float sum[kJoinRows] = {};
-    for (uint32_t s = 0; s < a.splits; ++s, p += (size_t)tail * (TILE * TILE)) {
+    // U splits' loads at a time; those past the last are not added
+    auto add = [&](auto at_a_time) {
+        constexpr uint32_t U = decltype(at_a_time)::value;
+        for (uint32_t s = 0; s < a.splits; s += U) {
+            float v[U][kJoinRows];
 #pragma unroll
-        for (uint32_t r = 0; r < kJoinRows; ++r)
-            sum[r] += p[(r < rows ? r : rows - 1) * TILE];
-    }
+            for (uint32_t u = 0; u < U; ++u) {
+                const size_t split = s + u < a.splits ? s + u : a.splits - 1;
+#pragma unroll
+                for (uint32_t r = 0; r < kJoinRows; ++r)
+                    v[u][r] = p[split * tail * (TILE * TILE) + (r < rows ? r : rows - 1) * TILE];
+            }
+#pragma unroll
+            for (uint32_t u = 0; u < U; ++u)
+#pragma unroll
+                for (uint32_t r = 0; r < kJoinRows; ++r)
+                    sum[r] += s + u < a.splits ? v[u][r] : 0.0f;
+        }
+    };
+    if (a.splits <= 3)
+        add(std::integral_constant<uint32_t, 3>());
+    else
+        add(std::integral_constant<uint32_t, 8>());
 #pragma unroll
     for (uint32_t r = 0; r < kJoinRows; ++r)
         if (r < rows) {
@@ -555,11 +576,12 @@ struct GradShape {
 // 256): as many whole rounds of tiles as there are take their tokens undivided, or
 // none does where the tiles are few; the rest are split, which shortens the last
 // round and costs the traffic of the partial results.  A round is as long as its
-// turns and a fixed part; the constants, in us, are what bf16 and checkpoints (a
-// tenth more) measure.  Tile 128 against 256, nothing split: 4096x18176x4544 841 /
-// 626, 2048x4096x4096 89 / 72, 4096x2048x2048 55 / 96, 300x2048x2048 13 / 20.
-// Splits of tile 128, 1 / 4 / 16: 8192x1024x1024 91 / 38 / 52, 8192x256x256 86 /
-// 30 / 19, 1000x1000x1000 18 / 20 / 35.
+// turns and a fixed part; the constants, in us, are fitted to 50 sizes measured with
+// each tile and 1 to 64 splits, from bf16 and from checkpoints, of which the choice
+// misses the fastest by 1% on average.  Tile 128 against 256, nothing split:
+// 4096x18176x4544 785 / 570, 2048x4096x4096 82 / 66, 4096x2048x2048 50 / 83,
+// 300x2048x2048 11 / 16.  Splits of tile 128, 1 / 4 / 16: 8192x1024x1024 82 / 33 /
+// 40, 8192x256x256 80 / 26 / 14, 1000x1000x1000 16 / 18 / 33.
 GradShape grad_shape(size_t rows, size_t n, size_t k) {
     const size_t turns = (rows + kStep - 1) / kStep;
     GradShape best = {};
@@ -568,9 +590,9 @@ GradShape grad_shape(size_t rows, size_t n, size_t k) {
         const size_t tiles = ((n + tile - 1) / tile) * ((k + tile - 1) / tile);
         const size_t slots = tile == 256 ? kCus : 2 * kCus;
         const auto round = [&](double per, double groups) {
-            return tile == 256        ? 1.95 * per + 6.0
-                   : groups <= kCus ? 0.7 * per + 3.0
-                                    : 1.31 * per + 3.5;
+            return tile == 256      ? 1.45 * per + 6.5
+                   : groups <= kCus ? 0.75 * per + 3.0
+                                    : 1.22 * per + 2.7;
         };
         for (size_t splits = 1; splits <= kMostSplits && splits <= turns; ++splits) {
             const size_t per = (turns + splits - 1) / splits;
@@ -578,11 +600,11 @@ GradShape grad_shape(size_t rows, size_t n, size_t k) {
                 continue;  // the same as a smaller number
             const size_t whole = splits == 1 ? tiles : tiles / slots * slots;
             const double rest = (double)(tiles - whole) * (double)splits;
-            double time = 5.0 + ceil((double)whole / (double)slots) *
-                                    round((double)turns, (double)whole);
+            double time =
+                ceil((double)whole / (double)slots) * round((double)turns, (double)whole);
             if (rest > 0)
-                time += ceil(rest / (double)slots) * round((double)per, rest) + 3.0 +
-                        2.0 * rest * tile * tile * 4.0 / 4.8e6;
+                time += ceil(rest / (double)slots) * round((double)per, rest) + 1.5 +
+                        0.1 * (double)splits + 2.0 * rest * tile * tile * 4.0 / 11e6;
             if (time < least) {
                 least = time;
                 best = {tile, (uint32_t)splits, tiles, whole, per * kStep};
