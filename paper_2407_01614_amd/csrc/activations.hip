@@ -3,7 +3,11 @@
 //
 // All four are one pass over matrices: eight neighbouring lanes take one block
 // of 64 elements of a row, 16 bytes of bf16 a lane, so the block's largest
-// magnitude is three DPP steps over values that are in registers anyway.
+// magnitude is three DPP steps over values that are in registers anyway.  HBM
+// bounds them where matrices are long (a copy here runs at 6.74 TB/s): bf16
+// 8192x8192 saved 32.7 us (6.2 TB/s) and read back 33.2 (6.1); GELU of
+// 2048x32768 with its checkpoint 56.5 (6.0); back from a checkpoint, its output
+// again as well, 4096x18176 80.7 (6.5).  Short ones are bound by their launch.
 #include <initializer_list>
 
 #include "zpp_act8.h"

@@ -4,7 +4,11 @@
 // consecutive elements a lane, so HBM is read once and the mean is known before
 // the squares are summed.  A row's lanes are as many as it asks for, in whole
 // waves (4544 features: 568 chunks on 576 lanes).  Rows of up to 16384 are held
-// so with two chunks a lane; longer ones are read again for each sum.
+// so with two chunks a lane; longer ones are read again for each sum.  HBM bounds
+// long batches (a copy here runs at 6.74 TB/s): 8192x8192 bf16 with residual and
+// checkpoint forward 106 us (5.7 TB/s), backward 84 (5.6) and 5 for the join of
+// the weights' gradients; 4096x4544 backward 32 (5.2) and 5.  Short ones are
+// bound by their launches and first loads.
 //
 // RAGGED: rows whose last chunk of 8 is partial.  The lane that has it takes the
 // row's last 8 elements instead and leaves out those that are the lane's before

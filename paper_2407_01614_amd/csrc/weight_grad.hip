@@ -6,6 +6,11 @@
 // features, turns them in registers (byte permutes pair the tokens; a
 // checkpoint's codes are scaled on the way, exactly) and lays them into LDS
 // feature by feature, from where a lane reads its 16 bytes at once.
+//
+// Long sums are bound by the matrix cores at the clock that power leaves them:
+// 4096x18176x4544 from a checkpoint 601-628 us, 1077-1125 TFLOP/s, from bf16 575, 1176
+// (the library's product of that layout, its result in bf16: 632), short ones by
+// writing dw (one token into 8192x8192: 43 us, 6.3 TB/s).
 #include <math.h>
 
 #include <initializer_list>
