@@ -22,7 +22,7 @@ constexpr uint32_t kGroups = kThreads / 8;  // lane groups, blocks side by side
 // without gaps and rows are whole blocks (FLAT), the place in one long row.
 struct Place {
     size_t row, col, block;
-    uint32_t valid;  // 0 past the row's or the matrix's end
+    uint32_t valid;  // elements to the row's end, kApart + 4 at most; 0 past either end
     __device__ __forceinline__ size_t in(const Mat &m) const { return row * m.stride + col; }
 };
 
@@ -38,22 +38,24 @@ struct Blocks {
     uint64_t magic;
 };
 
-template <bool FLAT>
+template <bool FLAT, uint32_t APART>
 __device__ __forceinline__ Place place_of(const Blocks &b, size_t block0, size_t row0,
                                           uint32_t rem0, uint32_t i) {
+    constexpr uint32_t kFull = APART + 4;
+    const uint32_t lane = (threadIdx.x & 7) * (APART == 4 ? 8 : 4);
     Place p;
     p.block = block0 + i;
     if constexpr (FLAT) {
         p.row = 0;
-        p.col = block0 * kActBlock + (i * kActBlock + (threadIdx.x & 7) * 8);
-        p.valid = i < b.total - block0 ? 8 : 0;
+        p.col = block0 * kActBlock + (i * kActBlock + lane);
+        p.valid = i < b.total - block0 ? kFull : 0;
     } else {
         const uint32_t x = rem0 + i;
         const uint32_t q = (uint32_t)__umul64hi((uint64_t)x << 6, b.magic);
-        const uint32_t col = (x - q * b.per_row) * kActBlock + (threadIdx.x & 7) * 8;
+        const uint32_t col = (x - q * b.per_row) * kActBlock + lane;
         p.row = row0 + q;
         p.col = col;
-        p.valid = i < b.total - block0 && col < b.cols ? (b.cols - col < 8 ? b.cols - col : 8) : 0;
+        p.valid = i < b.total - block0 && col < b.cols ? (b.cols - col < kFull ? b.cols - col : kFull) : 0;
     }
     return p;
 }
@@ -104,52 +106,58 @@ struct GeluBackwardArgs {
     Mat da, u, du, a;
 };
 
+// A lane's eight elements of a block: in a row for bf16, 16 bytes; as fp32 four and
+// four that are 32 apart, so that each access of the block's 8 lanes is whole lines
+// (fp32 8192x8192, GELU forward with its checkpoint 114 us, 94 so, backward 150 and
+// 124).
+constexpr uint32_t apart(int type) { return type == kF32 ? 32 : 4; }
+
 // The operators: what a lane loads, and what it makes of it.  kUnroll: blocks a
 // lane group takes (GELU's backward pass from bf16, 8192x8192, one / two: 70 / 76
 // us; its forward pass 54 / 48).
 template <int TYPE>
 struct SaveOp {
-    static constexpr uint32_t kUnroll = 2;
+    static constexpr uint32_t kUnroll = 2, kApart = apart(TYPE);
     typedef SaveArgs Args;
     Chunk<TYPE> x;
     template <bool RAGGED>
     __device__ void load(const Args &a, const Place &p) {
-        x = load_chunk<TYPE, RAGGED>(a.in, p.in(a.in), p.valid, p.block);
+        x = load_chunk<TYPE, RAGGED, kApart>(a.in, p.in(a.in), p.valid, p.block);
     }
     template <bool RAGGED>
     __device__ void store(const Args &a, const Place &p) {
         float v[8];
         chunk_values(x, v);
-        save_chunk<RAGGED>(a.saved, p.in(a.saved), p.valid, p.block, max_bits(x), v);
+        save_chunk<RAGGED, kApart>(a.saved, p.in(a.saved), p.valid, p.block, max_bits(x), v);
     }
 };
 
 template <int TYPE>
 struct LoadOp {
-    static constexpr uint32_t kUnroll = 2;
+    static constexpr uint32_t kUnroll = 2, kApart = apart(TYPE);
     typedef LoadArgs Args;
     Chunk<kI8> x;
     template <bool RAGGED>
     __device__ void load(const Args &a, const Place &p) {
-        x = load_chunk<kI8, RAGGED>(a.saved, p.in(a.saved), p.valid, p.block);
+        x = load_chunk<kI8, RAGGED, kApart>(a.saved, p.in(a.saved), p.valid, p.block);
     }
     template <bool RAGGED>
     __device__ void store(const Args &a, const Place &p) {
         float v[8];
         chunk_values(x, v);
         if (p.valid)
-            store_chunk<TYPE, RAGGED>(a.out, p.in(a.out), p.valid, make_chunk<TYPE>(v));
+            store_chunk<TYPE, RAGGED, kApart>(a.out, p.in(a.out), p.valid, make_chunk<TYPE>(v));
     }
 };
 
 template <int TYPE>
 struct GeluForwardOp {
-    static constexpr uint32_t kUnroll = 2;
+    static constexpr uint32_t kUnroll = 2, kApart = apart(TYPE);
     typedef GeluForwardArgs Args;
     Chunk<TYPE> x;
     template <bool RAGGED>
     __device__ void load(const Args &a, const Place &p) {
-        x = load_chunk<TYPE, RAGGED>(a.u, p.in(a.u), p.valid, p.block);
+        x = load_chunk<TYPE, RAGGED, kApart>(a.u, p.in(a.u), p.valid, p.block);
     }
     template <bool RAGGED>
     __device__ void store(const Args &a, const Place &p) {
@@ -161,22 +169,22 @@ struct GeluForwardOp {
             y[e] = gelu(v[e], m, normal(m).tail);
         }
         if (p.valid)
-            store_chunk<TYPE, RAGGED>(a.a, p.in(a.a), p.valid, make_chunk<TYPE>(y));
+            store_chunk<TYPE, RAGGED, kApart>(a.a, p.in(a.a), p.valid, make_chunk<TYPE>(y));
         if (a.saved.data)
-            save_chunk<RAGGED>(a.saved, p.in(a.saved), p.valid, p.block, max_bits(x), v);
+            save_chunk<RAGGED, kApart>(a.saved, p.in(a.saved), p.valid, p.block, max_bits(x), v);
     }
 };
 
 template <int TYPE, int SAVED>
 struct GeluBackwardOp {
-    static constexpr uint32_t kUnroll = SAVED == kI8 ? 2 : 1;
+    static constexpr uint32_t kUnroll = SAVED == kI8 ? 2 : 1, kApart = apart(TYPE);
     typedef GeluBackwardArgs Args;
     Chunk<TYPE> d;
     Chunk<SAVED> x;
     template <bool RAGGED>
     __device__ void load(const Args &a, const Place &p) {
-        d = load_chunk<TYPE, RAGGED>(a.da, p.in(a.da), p.valid, p.block);
-        x = load_chunk<SAVED, RAGGED>(a.u, p.in(a.u), p.valid, p.block);
+        d = load_chunk<TYPE, RAGGED, kApart>(a.da, p.in(a.da), p.valid, p.block);
+        x = load_chunk<SAVED, RAGGED, kApart>(a.u, p.in(a.u), p.valid, p.block);
     }
     template <bool RAGGED>
     __device__ void store(const Args &a, const Place &p) {
@@ -193,9 +201,9 @@ struct GeluBackwardOp {
             y[e] = gelu(v[e], m, n.tail);
         }
         if (p.valid) {
-            store_chunk<TYPE, RAGGED>(a.du, p.in(a.du), p.valid, make_chunk<TYPE>(g));
+            store_chunk<TYPE, RAGGED, kApart>(a.du, p.in(a.du), p.valid, make_chunk<TYPE>(g));
             if (a.a.data)
-                store_chunk<TYPE, RAGGED>(a.a, p.in(a.a), p.valid, make_chunk<TYPE>(y));
+                store_chunk<TYPE, RAGGED, kApart>(a.a, p.in(a.a), p.valid, make_chunk<TYPE>(y));
         }
     }
 };
@@ -215,7 +223,7 @@ __global__ __launch_bounds__(kThreads) void blocks_kernel(typename Op::Args args
     Place p[kUnroll];
 #pragma unroll
     for (uint32_t i = 0; i < kUnroll; ++i) {
-        p[i] = place_of<FLAT>(b, block0, row0, rem0, i * kGroups + threadIdx.x / 8);
+        p[i] = place_of<FLAT, Op::kApart>(b, block0, row0, rem0, i * kGroups + threadIdx.x / 8);
         if (p[i].valid)
             op[i].template load<!FLAT>(args, p[i]);
         else

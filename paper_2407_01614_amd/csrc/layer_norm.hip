@@ -22,7 +22,7 @@ namespace zpp {
 namespace {
 
 constexpr uint32_t kMaxThreads = 1024;
-constexpr uint32_t kMostRegCols = kMaxThreads * 8;  // features of a row in registers
+constexpr uint32_t kMostRegCols = kMaxThreads * 8;  // features of a row, a chunk a lane
 
 // Sums of Q values over a row's lanes, the same in every lane.  Two buffers in
 // turn: a wave writes a buffer again only after the barrier of the call between,

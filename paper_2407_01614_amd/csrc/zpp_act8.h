@@ -39,19 +39,29 @@ __device__ __forceinline__ void st_at(void *p, V v) {
     *reinterpret_cast<U *>(p) = v;
 }
 
-// Eight elements at p, `valid` >= 1 of them inside the row (those past them read
-// as the row's last).  A row's last, partial chunk takes single loads at clamped
-// places, which do not wait for each other; RAGGED false: there is none, `valid`
-// is 8.  Codes are read as ordinary, temporal loads: 8 bytes a lane, they left
-// half of each line's fetch behind as streaming ones (8192x8192 read back: 34.8
-// us, 29.4 so).
-template <int TYPE, bool RAGGED = true>
+// A chunk's elements lie at p: eight in a row, or (APART 32) four and another four
+// 32 elements on, so that 8 lanes share a block's fp32 as whole lines.  Its element
+// e is at place_at(e).
+template <uint32_t APART>
+__device__ __forceinline__ constexpr uint32_t place_at(uint32_t e) {
+    return e < 4 ? e : APART + e - 4;
+}
+
+// The eight elements, `valid` >= 1 of the APART + 4 from p inside the row (what is
+// past them reads as the row's last).  A row's last, partial chunk takes single
+// loads at clamped places, which do not wait for each other; RAGGED false: there is
+// none.  Codes are read as ordinary, temporal loads: 8 bytes a lane, they left half
+// of each line's fetch behind as streaming ones (8192x8192 read back: 34.8 us, 29.4
+// so).
+template <int TYPE, bool RAGGED = true, uint32_t APART = 4>
 __device__ __forceinline__ Chunk<TYPE> load_chunk(const Mat &m, size_t off, uint32_t valid,
                                                   size_t block) {
+    static_assert(APART == 4 || TYPE != kBf16);
+    const bool whole = !RAGGED || valid >= APART + 4;
     Chunk<TYPE> c;
     if constexpr (TYPE == kBf16) {
         const uint16_t *p = reinterpret_cast<const uint16_t *>(m.data) + off;
-        if (!RAGGED || valid >= 8) {
+        if (whole) {
             c.w = ld_nt_at<u32x4, 2>(p);
         } else {
 #pragma unroll
@@ -61,25 +71,27 @@ __device__ __forceinline__ Chunk<TYPE> load_chunk(const Mat &m, size_t off, uint
         }
     } else if constexpr (TYPE == kF32) {
         const float *p = reinterpret_cast<const float *>(m.data) + off;
-        if (!RAGGED || valid >= 8) {
+        if (whole) {
             c.lo = ld_nt_at<f32x4, 4>(p);
-            c.hi = ld_nt_at<f32x4, 4>(p + 4);
+            c.hi = ld_nt_at<f32x4, 4>(p + APART);
         } else {
 #pragma unroll
             for (uint32_t e = 0; e < 4; ++e) {
                 c.lo[e] = p[clamped(e, valid)];
-                c.hi[e] = p[clamped(e + 4, valid)];
+                c.hi[e] = p[clamped(APART + e, valid)];
             }
         }
     } else {
         const uint8_t *p = reinterpret_cast<const uint8_t *>(m.data) + off;
-        if (!RAGGED || valid >= 8) {
+        if (whole && APART == 4) {
             c.codes = ld_at<u32x2, 1>(p);
+        } else if (whole) {
+            c.codes = u32x2{ld_at<uint32_t, 1>(p), ld_at<uint32_t, 1>(p + APART)};
         } else {
             c.codes = u32x2{0, 0};
 #pragma unroll
             for (uint32_t e = 0; e < 8; ++e)
-                c.codes[e / 4] |= (uint32_t)p[clamped(e, valid)] << (8 * (e % 4));
+                c.codes[e / 4] |= (uint32_t)p[clamped(place_at<APART>(e), valid)] << (8 * (e % 4));
         }
         c.exp = m.exps[block];
     }
@@ -145,16 +157,18 @@ __device__ __forceinline__ Chunk<TYPE> make_chunk(const float (&x)[8]) {
     return c;
 }
 
-// Stores the first `valid` >= 1 elements of the chunk.  fp32 is stored as
-// ordinary, temporal: a lane's two halves are 16 bytes each, and streaming stores
-// of every other 16 bytes did not meet in the L2 (a checkpoint read back as
-// 8192x8192 fp32: 91 us, 69 so).
-template <int TYPE, bool RAGGED = true>
+// Stores the chunk's elements that are inside the row (`valid` as above).  Eight fp32
+// in a row are stored as ordinary, temporal: streaming stores of every other 16
+// bytes do not meet in the L2 (a checkpoint read back as 8192x8192 fp32: 91 us, 69
+// so, and 48 with the halves apart, whole lines as streaming stores).
+template <int TYPE, bool RAGGED = true, uint32_t APART = 4>
 __device__ __forceinline__ void store_chunk(const Mat &m, size_t off, uint32_t valid,
                                             const Chunk<TYPE> &c) {
+    static_assert(APART == 4 || TYPE != kBf16);
+    const bool whole = !RAGGED || valid >= APART + 4;
     if constexpr (TYPE == kBf16) {
         uint16_t *p = reinterpret_cast<uint16_t *>(m.data) + off;
-        if (!RAGGED || valid >= 8) {
+        if (whole) {
             st_nt_at<u32x4, 2>(p, c.w);
         } else {
 #pragma unroll
@@ -164,14 +178,17 @@ __device__ __forceinline__ void store_chunk(const Mat &m, size_t off, uint32_t v
         }
     } else {
         float *p = reinterpret_cast<float *>(m.data) + off;
-        if (!RAGGED || valid >= 8) {
+        if (whole && APART == 4) {
             st_at<f32x4, 4>(p, c.lo);
             st_at<f32x4, 4>(p + 4, c.hi);
+        } else if (whole) {
+            st_nt_at<f32x4, 4>(p, c.lo);
+            st_nt_at<f32x4, 4>(p + APART, c.hi);
         } else {
 #pragma unroll
             for (uint32_t e = 0; e < 8; ++e)
-                if (e < valid)
-                    p[e] = e < 4 ? c.lo[e] : c.hi[e - 4];
+                if (place_at<APART>(e) < valid)
+                    p[place_at<APART>(e)] = e < 4 ? c.lo[e] : c.hi[e - 4];
         }
     }
 }
@@ -280,20 +297,24 @@ __device__ __forceinline__ u32x2 act_codes(const float (&x)[8], uint32_t exp) {
 // Writes the checkpoint of the elements that the 8 lanes of a block hold, `top`
 // the lane's largest.  All 8 lanes take part, with `valid` 0 and `top` 0 where a
 // lane is past the row's end.
-template <bool RAGGED = true>
+template <bool RAGGED = true, uint32_t APART = 4>
 __device__ __forceinline__ void save_chunk(const Mat &m, size_t off, uint32_t valid, size_t block,
                                            uint32_t top, const float (&x)[8]) {
     const uint32_t exp = act_exp(max8(top));
     if (valid) {
         const u32x2 w = act_codes(x, exp);
         uint8_t *p = reinterpret_cast<uint8_t *>(m.data) + off;
-        if (!RAGGED || valid >= 8) {
+        const bool whole = !RAGGED || valid >= APART + 4;
+        if (whole && APART == 4) {
             st_nt_at<u32x2, 1>(p, w);
+        } else if (whole) {
+            st_at<uint32_t, 1>(p, w.x);
+            st_at<uint32_t, 1>(p + APART, w.y);
         } else {
 #pragma unroll
             for (uint32_t e = 0; e < 8; ++e)
-                if (e < valid)
-                    p[e] = (uint8_t)(w[e / 4] >> (8 * (e % 4)));
+                if (place_at<APART>(e) < valid)
+                    p[place_at<APART>(e)] = (uint8_t)(w[e / 4] >> (8 * (e % 4)));
         }
         if ((threadIdx.x & 7) == 0)
             m.exps[block] = (uint8_t)exp;

@@ -708,3 +708,38 @@ def test_weight_grad_adds_at_ragged_ends(zpp, rows, n, k):
     if n > 1:
         gaps = dw.as_strided((n - 1, 3), (k + 3, 1), dw.storage_offset() + k)
         assert bool((gaps == 9.0).all())
+
+
+@TYPES
+@pytest.mark.parametrize("cols", [1, 3, 4, 5, 7, 8, 9, 28, 31, 32, 33, 35, 36, 37, 60, 63, 65, 92,
+                                  95, 96, 97, 100, 127])
+def test_each_end_of_a_block(zpp, cols, dtype):
+    """Rows that end at every kind of place in a lane's share of a block: results to
+    the last element, and nothing beyond it written."""
+    rows, pad = 7, 5
+    x = hard_values(rows, cols, cols, dtype, pad, 1)
+    codes, exps = ref.encode(x.float().cpu().numpy())
+    saved = (ref.matrix(rows, cols, torch.int8, pad, 3, fill=99),
+             torch.empty(rows, -(-cols // 64), dtype=torch.uint8, device="cuda"))
+    out, again = (ref.matrix(rows, cols, dtype, pad, 1, fill=7.0) for _ in range(2))
+    u = ref.values(rows, cols, 5, dtype, pad)
+    da = ref.values(rows, cols, 6, dtype, std=1e-3)
+    a, du = (ref.matrix(rows, cols, dtype, pad, 2, fill=7.0) for _ in range(2))
+    arg, us = ref.saved(u)
+    zpp.checkpoint_save(x, saved)
+    zpp.checkpoint_load(saved, out)
+    zpp.gelu_forward(u, a)
+    zpp.gelu_backward(da, arg, du, a=again)
+    assert np.array_equal(saved[0].cpu().numpy(), codes)
+    assert np.array_equal(saved[1].cpu().numpy(), exps)
+    want = torch.from_numpy(ref.decode(codes, exps)).cuda().to(dtype)
+    assert torch.equal(out.nan_to_num(), want.nan_to_num())
+    assert torch.equal(torch.isnan(out), torch.isnan(want))
+    (wa, _), (ba, _) = ref.gelu(u.double(), da.double(), dtype)
+    ref.check(a, wa, ba, "a")
+    (wa, wd), (ba, bd) = ref.gelu(us, da.double(), dtype)
+    ref.check(again, wa, ba, "a again")
+    ref.check(du, wd, bd, "du")
+    for m, was in ((saved[0], 99), (out, 7.0), (a, 7.0), (du, 7.0), (again, 7.0)):
+        gaps = m.as_strided((rows - 1, pad), (cols + pad, 1), m.storage_offset() + cols)
+        assert bool((gaps == was).all())
