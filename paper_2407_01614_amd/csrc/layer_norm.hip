@@ -889,12 +889,12 @@ hipError_t start_backward(const NormBackwardArgs &a, const RowShape &s, hipStrea
     const dim3 grid(s.grid), threads(s.threads * s.teams);
     if (s.chunks > s.threads) {
         constexpr size_t kLds = 2 * 2 * 2 * kMaxThreads * sizeof(f32x4);
-        // more than 64 KB of LDS has to be asked for, once
-        static const hipError_t allowed = hipFuncSetAttribute(
-            reinterpret_cast<const void *>(norm_backward_wide_kernel<TYPE, X, AGAIN, RAGGED>),
-            hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
-        if (allowed != hipSuccess)
-            return allowed;
+        static std::atomic<uint64_t> asked{0};
+        const hipError_t e = allow_lds(
+            reinterpret_cast<const void *>(norm_backward_wide_kernel<TYPE, X, AGAIN, RAGGED>), kLds,
+            asked);
+        if (e != hipSuccess)
+            return e;
         hipLaunchKernelGGL((norm_backward_wide_kernel<TYPE, X, AGAIN, RAGGED>), grid, threads, kLds,
                            stream, a);
         return hipGetLastError();
@@ -934,12 +934,12 @@ hipError_t start_forward(const NormForwardArgs &a, dim3 grid, uint32_t threads,
                          hipStream_t stream) {
     const size_t lds = V > 1 ? (size_t)threads * V * 2 * 8 * sizeof(float) : 0;
     if constexpr (V > 1) {
-        // more than 64 KB of LDS has to be asked for, once
-        static const hipError_t allowed = hipFuncSetAttribute(
-            reinterpret_cast<const void *>(norm_forward_kernel<TYPE, V, RAGGED>),
-            hipFuncAttributeMaxDynamicSharedMemorySize, kMaxThreads * V * 2 * 8 * sizeof(float));
-        if (allowed != hipSuccess)
-            return allowed;
+        static std::atomic<uint64_t> asked{0};
+        const hipError_t e =
+            allow_lds(reinterpret_cast<const void *>(norm_forward_kernel<TYPE, V, RAGGED>),
+                      (size_t)kMaxThreads * V * 2 * 8 * sizeof(float), asked);
+        if (e != hipSuccess)
+            return e;
     }
     hipLaunchKernelGGL((norm_forward_kernel<TYPE, V, RAGGED>), grid, dim3(threads), lds, stream, a);
     return hipGetLastError();

@@ -624,11 +624,10 @@ hipError_t start(const WeightGradArgs &a, const GradShape &s, hipStream_t stream
     constexpr size_t kLds = 2 * 2 * TILE * kStep * 2;
     const void *kernel =
         reinterpret_cast<const void *>(weight_grad_kernel<X, TILE, WAVES_N, WAVES_K>);
-    // more than 64 KB of LDS has to be asked for, once
-    static const hipError_t allowed =
-        hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
-    if (allowed != hipSuccess)
-        return allowed;
+    static std::atomic<uint64_t> asked{0};
+    const hipError_t e = allow_lds(kernel, kLds, asked);
+    if (e != hipSuccess)
+        return e;
     const size_t tail = s.tiles - s.whole, groups = s.whole + tail * s.splits;
     hipLaunchKernelGGL((weight_grad_kernel<X, TILE, WAVES_N, WAVES_K>), dim3((unsigned)groups),
                        dim3(WAVES_N * WAVES_K * kWave), kLds, stream, a);

@@ -1,13 +1,31 @@
-// Device-side pieces of the layer operators: eight consecutive elements of a
-// row as a lane's share (bf16, fp32 or a checkpoint's codes), the decisions of
-// the 8-bit checkpoint, and sums over lanes.
+// Pieces of the layer operators' kernels: eight elements of a row as a lane's
+// share (bf16, fp32 or a checkpoint's codes), the decisions of the 8-bit
+// checkpoint, and sums over lanes.
 #pragma once
+
+#include <atomic>
 
 #include "zpp_device.h"
 #include "zpp_layer.h"
 #include "zpp_quant.h"
 
 namespace zpp {
+
+// More than 64 KB of LDS has to be asked for, once on each device; `asked`, a
+// kernel's own, has a bit for each of the first 64 where that is done.
+inline hipError_t allow_lds(const void *kernel, size_t bytes, std::atomic<uint64_t> &asked) {
+    int device = 0;
+    hipError_t e = hipGetDevice(&device);
+    if (e != hipSuccess)
+        return e;
+    const uint64_t bit = (unsigned)device < 64 ? (uint64_t)1 << device : 0;
+    if (asked.load(std::memory_order_relaxed) & bit)
+        return hipSuccess;
+    e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == hipSuccess)
+        asked.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
 
 // Eight elements as they are loaded; turned to fp32 only where they are used,
 // so that loads in flight hold 4 (bf16), 8 (fp32) or 3 (codes) registers.
