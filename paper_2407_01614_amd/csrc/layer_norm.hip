@@ -200,6 +200,25 @@ __device__ __forceinline__ float inverse_root(float v) {
     return __builtin_amdgcn_rsqf(tiny ? v * 0x1p64f : v) * (tiny ? 0x1p32f : 1.0f);
 }
 
+// sum / n, rounded: taken up unrounded in some of the differences from it (as the
+// product of an fma), it would not be what their mean corrects.
+__device__ __forceinline__ float rounded_mean(float sum, float per) {
+#pragma clang fp contract(off)
+    return sum * per;
+}
+
+// A row's mean, made of its sum, may be ulps off by the roundings of the sum and of the
+// quotient.  The mean `off` of the differences from it is what it is off by:
+//     mean = near + mean(d),  variance = mean(d^2) - mean(d)^2
+// Without that a row of 1000 times 700, whose mean then is 700.00006, has y off by
+// 0.02 gamma at an eps of 1e-5.  The product is not rounded before it is taken off
+// (beyond 2^64 it may pass fp32 where the mean of squares, Inf, stands), and what
+// rounding leaves below 0 is 0.
+__device__ __forceinline__ float variance(float off, float square) {
+    const float var = __builtin_fmaf(-off, off, square);
+    return var < 0.0f ? 0.0f : var;
+}
+
 // One row a turn, V chunks a lane, the i-th `threads` lanes after the one
 // before; the next row is on its way while this one's sums are made.  With V == 1
 // gamma and beta stay in registers; two chunks a lane leave none for them, and
@@ -222,7 +241,9 @@ __global__ __launch_bounds__(kMaxThreads) void norm_forward_kernel(NormForwardAr
     };
 #pragma unroll
     for (int v = 0; v < V; ++v)
-        l[v] = row_lane<RAGGED>(v * blockDim.x + threadIdx.x, a.cols);
+        // a row of two chunks a lane has more than kMaxThreads: its last is a second one
+        l[v] = v == V - 1 ? row_lane<RAGGED>(v * blockDim.x + threadIdx.x, a.cols)
+                          : row_lane<false>(v * blockDim.x + threadIdx.x, a.cols);
     Chunk<TYPE> cx[V] = {}, cr[V] = {};
     auto fetch = [&](size_t row) {
 #pragma unroll
@@ -256,9 +277,7 @@ __global__ __launch_bounds__(kMaxThreads) void norm_forward_kernel(NormForwardAr
             // the masks that follow from `first` are made again in each row: kept,
             // they take more scalar registers than there are (4096x8201 bf16 38.8 us,
             // 34.0 so; with one chunk a lane they fit, and 4096x4550 goes from 17.9 to 19.5)
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-                asm volatile("" : "+v"(l[v].first));
+            asm volatile("" : "+v"(l[V - 1].first));
         }
         float x[V][8], sum[1] = {0.0f};
         uint32_t top[V];
@@ -282,20 +301,44 @@ __global__ __launch_bounds__(kMaxThreads) void norm_forward_kernel(NormForwardAr
         if (row + gridDim.x < a.rows)
             fetch(row + gridDim.x);
         group_sum(sum, scratch, turn, 0, waves);
-        const float mean = sum[0] * per;
-        sum[0] = 0.0f;
+        const float near = rounded_mean(sum[0], per);
+        // differences from the mean, and the lane's sum of f of them
+        float mean = near, d[V][8];
+        auto lane_sum = [&](auto &&f) {
+            sum[0] = 0.0f;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            float square = 0.0f;
+            for (int v = 0; v < V; ++v) {
+                float part = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float d = x[v][e] - mean;
-                square += !RAGGED || (uint32_t)e >= l[v].first ? d * d : 0.0f;
+                for (int e = 0; e < 8; ++e)
+                    part += !RAGGED || (uint32_t)e >= l[v].first ? f(d[v][e]) : 0.0f;
+                sum[0] += l[v].in ? part : 0.0f;
             }
-            sum[0] += l[v].in ? square : 0.0f;
-        }
+        };
+        auto center = [&] {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    d[v][e] = x[v][e] - mean;
+        };
+        center();
+        lane_sum([](float q) { return q * q; });
         group_sum(sum, scratch, turn, 0, waves);
-        const float rstd = inverse_root(sum[0] * per + a.eps);
+        float var = sum[0] * per;
+        // What the mean is off by is ulps of the row's magnitude, and no more than
+        // roundings of y where the row varies as much as its mean is; only beyond
+        // that is it summed (16384x4544 bf16 52 us, 61 where it is for every row).  Every
+        // lane of the row has the same sums, to the bit, and takes the same way.
+        if (__builtin_amdgcn_readfirstlane(near * near > var)) {
+            lane_sum([](float q) { return q; });
+            group_sum(sum, scratch, turn, 0, waves);
+            const float off = sum[0] * per;
+            mean = near + off;
+            var = variance(off, var);
+            center();
+        }
+        const float rstd = inverse_root(var + a.eps);
         if (threadIdx.x == 0) {
             if (a.mean)
                 a.mean[row] = mean;
@@ -319,7 +362,7 @@ __global__ __launch_bounds__(kMaxThreads) void norm_forward_kernel(NormForwardAr
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                y[e] = __builtin_fmaf((x[v][e] - mean) * rstd, gamma[e], beta[e]);
+                y[e] = __builtin_fmaf(d[v][e] * rstd, gamma[e], beta[e]);
             if (l[v].in)
                 store_row<TYPE, RAGGED>(a.y, row, l[v], make_chunk<TYPE>(y));
             if (a.saved.data)
@@ -338,15 +381,16 @@ __device__ __forceinline__ Chunk<TYPE> load_part(const Mat &m, size_t row, uint3
 // Rows too long for registers: three passes over each.
 template <int TYPE>
 __global__ __launch_bounds__(kMaxThreads) void norm_forward_long_kernel(NormForwardArgs a) {
-    __shared__ GroupSum<1> scratch;
+    __shared__ GroupSum<2> scratch;
     const uint32_t blocks = (a.cols + kActBlock - 1) / kActBlock;
     const uint32_t waves = blockDim.x / kWave;
     const uint32_t turns = (a.cols + 8 * blockDim.x - 1) / (8 * blockDim.x);
+    const float per = 1.0f / (float)a.cols;
     uint32_t turn = 0;
     for (size_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        float sum[1], mean = 0.0f, rstd = 0.0f;
+        float sum[2], mean = 0.0f, rstd = 0.0f;
         for (int pass = 0; pass < 3; ++pass) {
-            sum[0] = 0.0f;
+            sum[0] = sum[1] = 0.0f;
             for (uint32_t t = 0; t < turns; ++t) {
                 const uint32_t col = (t * blockDim.x + threadIdx.x) * 8;
                 const uint32_t valid = valid_at(col, a.cols);
@@ -364,8 +408,10 @@ __global__ __launch_bounds__(kMaxThreads) void norm_forward_long_kernel(NormForw
                 if (pass < 2) {
 #pragma unroll
                     for (uint32_t e = 0; e < 8; ++e) {
-                        const float d = x[e] - mean;
-                        sum[0] += e < valid ? (pass == 0 ? x[e] : d * d) : 0.0f;
+                        // the mean of the first pass is 0
+                        const float d = e < valid ? x[e] - mean : 0.0f;
+                        sum[0] += d;
+                        sum[1] = __builtin_fmaf(d, d, sum[1]);
                     }
                 } else {
                     float gamma[8], beta[8], y[8];
@@ -384,10 +430,13 @@ __global__ __launch_bounds__(kMaxThreads) void norm_forward_long_kernel(NormForw
             if (pass == 2)
                 break;
             group_sum(sum, scratch, turn, 0, waves);
-            if (pass == 0)
-                mean = sum[0] / (float)a.cols;
-            else
-                rstd = inverse_root(sum[0] / (float)a.cols + a.eps);
+            if (pass == 0) {
+                mean = rounded_mean(sum[0], per);
+            } else {
+                const float off = sum[0] * per;
+                mean += off;
+                rstd = inverse_root(variance(off, sum[1] * per) + a.eps);
+            }
         }
         if (threadIdx.x == 0) {
             if (a.mean)
