@@ -475,6 +475,17 @@ RowShape row_shape(size_t rows, size_t cols) {
     return s;
 }
 
+// (x - mean) rstd of a lane's element e, 0 for a lane past the row (whose rstd is given
+// as 0) and for those that a checkpoint holds as another lane's: such numbers, -mean
+// rstd or a code with another block's scale, may pass fp32, and times a dy of 0 they
+// would be NaN in the row's sums.
+template <int X, bool RAGGED>
+__device__ __forceinline__ float normalised(float x, float mean, float rstd, uint32_t e,
+                                            const RowLane &l) {
+    const float h = (x - mean) * rstd;
+    return RAGGED && X == kI8 && e < l.first ? 0.0f : h;
+}
+
 // One row of each team a turn; the next turn's are on their way while this one's
 // are summed.
 template <int TYPE, int X, bool AGAIN, bool RAGGED>
@@ -545,7 +556,7 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward_kernel(NormBackward
     for (size_t base = (size_t)blockIdx.x * teams; base < a.rows; base += step) {
         const size_t row = base + team;
         const Chunk<TYPE> cr = nr;
-        const float mean = stat[0], scale = stat[1];
+        const float mean = stat[0], scale = l.in ? stat[1] : 0.0f;
         float s[2] = {0.0f, 0.0f}, d[8], g[8], h[8];
         chunk_values(nd, d);
         clear_others<RAGGED>(d, l);
@@ -553,7 +564,7 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward_kernel(NormBackward
         param(0, g);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            h[e] = (h[e] - mean) * scale;
+            h[e] = normalised<X, RAGGED>(h[e], mean, scale, e, l);
             dg[e] = __builtin_fmaf(d[e], h[e], dg[e]);
             db[e] += d[e];
             g[e] *= d[e];
@@ -639,17 +650,19 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward_wide_kernel(NormBac
     uint32_t turn = 0;
     RowLane l[2];
     float dg[2][8];
+    // the row has more chunks than kMaxThreads: every first chunk is whole
+    l[0] = row_lane<false>(threadIdx.x, a.cols);
+    l[0].in = true;
+    l[1] = row_lane<RAGGED>(threads + threadIdx.x, a.cols);
+    if (!l[1].in) {
+        l[1].col = a.cols - 8;
+        l[1].block = l[1].col / kActBlock;
+    }
 #pragma unroll
-    for (int v = 0; v < 2; ++v) {
-        l[v] = row_lane<RAGGED>(v * threads + threadIdx.x, a.cols);
-        if (!l[v].in) {
-            l[v].col = a.cols - 8;
-            l[v].block = l[v].col / kActBlock;
-        }
+    for (int v = 0; v < 2; ++v)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             dg[v][e] = 0.0f;
-    }
     // a lane reads only what it has written
     f32x4 *const params = reinterpret_cast<f32x4 *>(shared) + threadIdx.x;
     auto param = [&](int v, float (&p)[8]) {
@@ -688,7 +701,8 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward_wide_kernel(NormBac
         // addresses and masks are made again in each row: kept, they take registers
 #pragma unroll
         for (int v = 0; v < 2; ++v)
-            asm volatile("" : "+v"(l[v].first), "+v"(l[v].col), "+v"(l[v].block));
+            asm volatile("" : "+v"(l[v].col), "+v"(l[v].block));
+        asm volatile("" : "+v"(l[1].first));
         if (!kAhead)
             fetch(row);
         const float mean = stat[0], scale = stat[1];
@@ -705,9 +719,10 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward_wide_kernel(NormBac
             params[(4 + v) * kMaxThreads] += f32x4{d[0], d[1], d[2], d[3]};
             params[(6 + v) * kMaxThreads] += f32x4{d[4], d[5], d[6], d[7]};
             param(v, g);
+            const float inside = l[v].in ? scale : 0.0f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                h[e] = (h[e] - mean) * scale;
+                h[e] = normalised<X, RAGGED>(h[e], mean, inside, e, l[v]);
                 dg[v][e] = __builtin_fmaf(d[e], h[e], dg[v][e]);
                 g[e] *= d[e];
                 s[0] += g[e];
