@@ -965,6 +965,16 @@ hipError_t start_backward(const NormBackwardArgs &a, const RowShape &s, hipStrea
     }
     const size_t params = (AGAIN ? 2 : 1) * 2 * sizeof(f32x4) * s.threads;
     const size_t sums = s.teams > 1 ? 2 * sizeof(f32x4) * s.teams * s.threads : 0;
+    if constexpr (AGAIN) {
+        // gamma and beta of 1024 lanes are 64 KB, and the rows' sums come on top
+        constexpr size_t kLds = 2 * 2 * sizeof(f32x4) * kMaxThreads;
+        static std::atomic<uint64_t> asked{0};
+        const hipError_t e = allow_lds(
+            reinterpret_cast<const void *>(norm_backward_kernel<TYPE, X, AGAIN, RAGGED>), kLds,
+            asked);
+        if (e != hipSuccess)
+            return e;
+    }
     hipLaunchKernelGGL((norm_backward_kernel<TYPE, X, AGAIN, RAGGED>), grid, threads,
                        params > sums ? params : sums, stream, a, s.threads, s.teams);
     return hipGetLastError();
