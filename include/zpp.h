@@ -412,7 +412,8 @@ typedef enum {
  *       exp = e + 127, code = rint(x * 2^-e) (ties to even), and an element
  *       reads as code * 2^e.  (|code| is kept to 63 where e = 122, the largest
  *       e there is, so that what is read is finite.)
- * An element is off by at most 2^e / 2 <= max |x| / 127 (2^-127 below that).
+ * An element is off by at most 2^e / 2 <= max |x| / 127 (2^-127 below that; at
+ * e = 122, where 63 stands for all above it, by less than 2^e).
  * The scale being a power of two, code * 2^e has 7 significant bits: it is a
  * bf16 number, and no product of the backward pass rounds it again.  1 + 1/64
  * bytes an element. */

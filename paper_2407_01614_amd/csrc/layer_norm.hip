@@ -6,8 +6,8 @@
 // waves (4544 features: 568 chunks on 576 lanes).  Rows of up to 16384 are held
 // so with two chunks a lane; longer ones are read again for each sum.  HBM bounds
 // long batches (a copy here runs at 6.74 TB/s): 8192x8192 bf16 with residual and
-// checkpoint forward 106 us (5.7 TB/s), backward 84 (5.6) and 5 for the join of
-// the weights' gradients; 4096x4544 backward 32 (5.2) and 5.  Short ones are
+// checkpoint forward 107 us (5.7 TB/s), backward 87 (5.4) and 5 for the join of
+// the weights' gradients; 4096x4544 backward 33 (5.1) and 5.  Short ones are
 // bound by their launches and first loads.
 //
 // RAGGED: rows whose last chunk of 8 is partial.  The lane that has it takes the
@@ -633,10 +633,12 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward_kernel(NormBackward
 // Two chunks a lane, in 128 registers: gamma and the rows' sum of dy lie in LDS as
 // fp32, the row itself stays as it was loaded and is unpacked again after its
 // sums, and beta is read where it is used.  From bf16 the next row is fetched
-// ahead; fp32, and bf16 that also writes y, leave no registers for that and fetch
-// a row when its turn comes.  A lane past the row takes the row's last chunk, so
-// that no load is in a branch, and clears it.  8192x12288, dx and the weights'
-// gradients: bf16 109 us, fp32 260; as long rows, read twice, 212 and 440.
+// ahead (127 registers); bf16 that also writes y leaves none for that (118 without
+// it).  fp32 fetches a row when its turn comes: its kernels take 92 to 114, and one
+// with a second row in flight has not been measured.  A lane past the row takes the
+// row's last chunk, so that no load is in a branch, and clears it.  8192x12288, dx
+// and the weights' gradients: bf16 108 us, fp32 247; as long rows, read twice, 212
+// and 440.
 template <int TYPE, int X, bool AGAIN, bool RAGGED>
 __global__ __launch_bounds__(kMaxThreads) void norm_backward_wide_kernel(NormBackwardArgs a) {
     constexpr bool kAhead = TYPE == kBf16 && !AGAIN;
@@ -1028,7 +1030,11 @@ hipError_t start_forward(const NormForwardArgs &a, hipStream_t stream) {
     // of more than 4 waves is counted with its fullest SIMD's, so that no part of the
     // grid waits for a second round: 10 waves, of which a CU's lanes hold three times,
     // fit twice (4096x5120 bf16 with three counted 22.8 us, 18.0 with two; 2048x4544
-    // fp32 with 8 waves a SIMD 23.4, 18.8 so).
+    // fp32 with 8 waves a SIMD 23.4, 18.8 so).  bf16 rows with a partial chunk are
+    // counted as the others, though their kernel's 104 scalar registers leave 7 waves:
+    // rows of 6 to 8 waves then have a second round and would gain by 7 (8192x4001
+    // 35.2 -> 29.6 us), narrower ones would lose (16384x1001 19.1 -> 20.3, 8192x2501
+    // 19.7 -> 21.0).
     constexpr uint32_t kWaves = V == 2 ? 4 : TYPE == kF32 ? 6 : 8;
     const uint32_t waves = threads / kWave;
     const size_t fit = (size_t)kCus * (waves > 4 ? kWaves / ((waves + 3) / 4) : kWaves * 4 / waves);

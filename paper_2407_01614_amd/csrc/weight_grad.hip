@@ -7,10 +7,13 @@
 // checkpoint's codes are scaled on the way, exactly) and lays them into LDS
 // feature by feature, from where a lane reads its 16 bytes at once.
 //
-// Long sums are bound by the matrix cores at the clock that power leaves them:
-// 4096x18176x4544 from a checkpoint 601-628 us, 1077-1125 TFLOP/s, from bf16 575, 1176
-// (the library's product of that layout, its result in bf16: 632), short ones by
-// writing dw (one token into 8192x8192: 43 us, 6.3 TB/s).
+// 4096x18176x4544 from a checkpoint 628-640 us, 1057-1077 TFLOP/s, from bf16 575, 1176
+// (the library's product of that layout, its result in bf16: 632).  Long sums are bound
+// by a turn's steps one after the other more than by any one of them: of a turn's 3230
+// clocks from bf16 (3790 from codes) the matrix cores are busy for 2048 and the LDS for
+// 1280, nearly the whole together, and the conversion of codes comes on top; the clock
+// under that load is 1.5 to 1.8 GHz.  Short sums are bound by writing dw (one token
+// into 8192x8192: 43 us, 6.3 TB/s).
 #include <math.h>
 
 #include <initializer_list>
@@ -583,7 +586,8 @@ struct GradShape {
 // round and costs the traffic of the partial results.  A round is as long as its
 // turns and a fixed part; the constants, in us, are fitted to 50 sizes measured with
 // each tile and 1 to 64 splits, from bf16 and from checkpoints, of which the choice
-// misses the fastest by 1% on average.  Tile 128 against 256, nothing split:
+// misses the fastest by 1% on average; of 32 other sizes by 2%, at worst by 22%
+// (770x320x3648 from bf16: 16.7 us, 13.7 undivided).  Tile 128 against 256, nothing split:
 // 4096x18176x4544 785 / 570, 2048x4096x4096 82 / 66, 4096x2048x2048 50 / 83,
 // 300x2048x2048 11 / 16.  Splits of tile 128, 1 / 4 / 16: 8192x1024x1024 82 / 33 /
 // 40, 8192x256x256 80 / 26 / 14, 1000x1000x1000 16 / 18 / 33.
