@@ -436,11 +436,11 @@ def _own_log_probs(s):
     out = dict(log_probs=s["log_probs"], lse=s["lse"])
     if case["entropy"]:
         out["entropies"] = entropies
+    ws = _workspace(s, zpp.log_probs_workspace(case["rows"], case["vocab"], case["top"]))
     if case["way"] == "train":
-        zpp.log_probs_train(x, targets, s["log_probs"], s["lse"], s["dlog_probs"], s["dx"],
+        zpp.log_probs_train(x, targets, s["log_probs"], s["lse"], s["dlog_probs"], s["dx"], ws,
                             entropies=entropies, dentropies=s.get("dentropies"))
         return dict(out, dx=s["dx"])
-    ws = _workspace(s, zpp.log_probs_workspace(case["rows"], case["vocab"], case["top"]))
     zpp.log_probs_forward(x, targets, s["log_probs"], s["lse"], ws, entropies=entropies,
                           top_ids=s.get("top_ids"), top_log_probs=s.get("top_log_probs"))
     if case["top"]:
