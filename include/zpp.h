@@ -515,6 +515,176 @@ ZPP_API zpp_status zpp_weight_grad(const zpp_matrix *dy, const zpp_matrix *x, si
                                    void *workspace, size_t workspace_bytes, hipStream_t stream,
                                    hipEvent_t wait_before, hipEvent_t done_after);
 
+/* ------------------------------------------------------------------------
+ * Operators of a token model's training step: rotary positions between the
+ * query, key and value product and attention; log probabilities of the next
+ * tokens with their gradient; AdamW over many tensors at once.  The conventions
+ * at the head of this file hold, and those of the layer operators: sums and
+ * statistics in fp32, one rounding of a bf16 result, the same bits each time.
+ * ------------------------------------------------------------------------ */
+
+/* Heads of a batch of tokens: element f of head h of group g of token t lies
+ * t * token_stride + g * group_stride + h * head_stride + f elements from
+ * `data`.  Groups serve layouts that put a key's head behind the query heads
+ * that share it; otherwise there is one. */
+typedef struct {
+    void *data;
+    size_t token_stride, group_stride, head_stride;
+    uint32_t groups, heads;
+} zpp_heads;
+
+/* Rotary positions: pair i of the first `rotated` of every head's `dim`
+ * features, (u, v), turns by the angle a = 2 pi positions[t] turns[i]:
+ *     u' = scale (u cos a - v sin a);  v' = scale (u sin a + v cos a)
+ * and backward by -a, which is the gradient's way:
+ *     du = scale (du' cos a + dv' sin a);  dv = scale (dv' cos a - du' sin a)
+ * The pairs are features (2i, 2i + 1) where `interleaved`, otherwise (i, i +
+ * rotated / 2).  Features from `rotated` on stay as they are (unscaled).
+ * x, out: the same groups and heads; k, k_out: another array that turns with
+ *   it, as the keys, or both NULL.  An output may be its own input (the same
+ *   data and strides), and then features that do not turn are not touched;
+ *   apart from that no output may share an element with another argument.
+ * type: ZPP_BF16 or ZPP_F32.  positions: int64_t[tokens], of any sign.  turns:
+ *   double[rotated / 2], turns a position (theta^(-2i / rotated) / 2 pi, divided by
+ *   what a longer context asks for).  The angle is taken in 64 bits and turned
+ *   into a fraction of a turn before it is rounded.
+ * dim <= 16384; rotated even, <= dim and <= 4096; groups * heads of x and k
+ *   together < 2^16; scale finite. */
+ZPP_API zpp_status zpp_rotary_forward(const zpp_heads *x, const zpp_heads *out, const zpp_heads *k,
+                                      const zpp_heads *k_out, int32_t type, size_t tokens,
+                                      uint32_t dim, uint32_t rotated, const int64_t *positions,
+                                      const double *turns, int32_t interleaved, float scale,
+                                      hipStream_t stream, hipEvent_t wait_before,
+                                      hipEvent_t done_after);
+ZPP_API zpp_status zpp_rotary_backward(const zpp_heads *x, const zpp_heads *out, const zpp_heads *k,
+                                       const zpp_heads *k_out, int32_t type, size_t tokens,
+                                       uint32_t dim, uint32_t rotated, const int64_t *positions,
+                                       const double *turns, int32_t interleaved, float scale,
+                                       hipStream_t stream, hipEvent_t wait_before,
+                                       hipEvent_t done_after);
+
+/* Most alternatives of zpp_log_probs_forward, and the longest row it finds them in. */
+#define ZPP_MAX_TOP 64
+#define ZPP_MAX_TOP_VOCAB 524288
+
+/* Bytes of workspace of zpp_log_probs_forward and, with top = 0, of
+ * zpp_log_probs_train of this size (0: none needed). */
+ZPP_API size_t zpp_log_probs_workspace(size_t rows, size_t vocab, uint32_t top);
+
+/* Log probabilities of given tokens: of every row of logits x, in fp32,
+ *     lse = log sum_j e^(x_j);  log_probs = x_t - lse, t = targets[row]
+ *     entropies = -sum_j p_j log p_j, with p_j = e^(x_j - lse)
+ * x: [rows][vocab], ZPP_BF16 or ZPP_F32; -Inf where a token is masked.
+ * targets: int64_t[rows].  A negative one takes no part: its log probability
+ *   is 0.  One from vocab on is a mistake: its log probability is NaN.
+ * log_probs, lse, entropies: float[rows] out; lse and entropies may be NULL.
+ * top_ids, top_log_probs: int32_t and float [rows][top] out, the most probable
+ *   tokens in falling order, the lower of equals first (both zeros are equal); given
+ *   where top > 0.  top <= vocab, <= ZPP_MAX_TOP, and vocab <= ZPP_MAX_TOP_VOCAB.
+ * A row that is -Inf throughout has no distribution: lse, log_probs and
+ *   top_log_probs are -Inf, its entropy is 0.  A row with a NaN or +Inf: all NaN,
+ *   and top_ids some tokens in range.
+ * workspace: zpp_log_probs_workspace(rows, vocab, top) bytes at 16-byte
+ *   alignment, as for zpp_layer_norm_backward; may be NULL where that is 0.
+ * rows == 0 is a no-op, vocab == 0 is ZPP_EINVAL. */
+ZPP_API zpp_status zpp_log_probs_forward(const zpp_matrix *x, size_t rows, size_t vocab,
+                                         const int64_t *targets, float *log_probs, float *lse,
+                                         float *entropies, uint32_t top, int32_t *top_ids,
+                                         float *top_log_probs, void *workspace,
+                                         size_t workspace_bytes, hipStream_t stream,
+                                         hipEvent_t wait_before, hipEvent_t done_after);
+
+/* The gradient of the logits, g = dlog_probs (0 where the target is negative),
+ * h = dentropies:
+ *     dx_j = g ([j = t] - p_j) - h p_j (log p_j + entropy)
+ * lse, entropies: the forward pass's.  entropies and dentropies: both or neither.
+ * dx: [rows][vocab] of x's type; it may be x itself (the same data and stride).
+ * A row that is -Inf throughout gets zeros; a target from vocab on gives NaN. */
+ZPP_API zpp_status zpp_log_probs_backward(const zpp_matrix *x, size_t rows, size_t vocab,
+                                          const int64_t *targets, const float *lse,
+                                          const float *dlog_probs, const float *entropies,
+                                          const float *dentropies, const zpp_matrix *dx,
+                                          hipStream_t stream, hipEvent_t wait_before,
+                                          hipEvent_t done_after);
+
+/* Both in one call, for a loss whose gradient by the log probabilities (and
+ * entropies) is known before them, as a mean over tokens is: reads x once.
+ * lse is needed here; entropies may be NULL where dentropies is, dentropies: none. */
+ZPP_API zpp_status zpp_log_probs_train(const zpp_matrix *x, size_t rows, size_t vocab,
+                                       const int64_t *targets, float *log_probs, float *lse,
+                                       float *entropies, const float *dlog_probs,
+                                       const float *dentropies, const zpp_matrix *dx,
+                                       void *workspace, size_t workspace_bytes, hipStream_t stream,
+                                       hipEvent_t wait_before, hipEvent_t done_after);
+
+/* One tensor of zpp_adam_tensors_step: n elements of each array, all updated
+ * as zpp_adam_partition_step does.
+ * Moments of ZPP_F32: exp_avg and exp_avg_sq are float[n], the scales unused.
+ * Moments of ZPP_I8: codes, int8_t[n] and uint8_t[n], and scales, float[ceil(n /
+ * ZPP_ADAM_BLOCK)] each, over blocks of consecutive elements (the last may be
+ * shorter):
+ *   first moment: scale = max |m| / 127; code = rint(m * (127 / max |m|)) (ties to
+ *     even), reads as code * scale; all 0 where max |m| < 2^-100;
+ *   second moment, by its root r = sqrt(v): scale = max r / 255^2; code = the
+ *     largest integer c that is 0 or has (c - 1/2)^2 <= r * (255^2 / max r), and at
+ *     least 1 where r > 0 (so that no step divides by a vanished root); reads as
+ *     (c^2 * scale)^2;
+ *   a block with an Inf or NaN: scale NaN, codes 0, every element reads as NaN.
+ * Each operation is rounded to fp32 in the order written.  The step that made the
+ * moments moves the weights by them before they are rounded to codes.
+ * grad: n values of the call's gradient type.  primary_bf16: uint16_t[n] out, or
+ * NULL.  weight_decay: this tensor's, finite. */
+#define ZPP_ADAM_BLOCK 256
+typedef struct {
+    float *master;
+    void *exp_avg, *exp_avg_sq;
+    float *exp_avg_scales, *exp_avg_sq_scales;
+    const void *grad;
+    uint16_t *primary_bf16;
+    size_t n;
+    float weight_decay;
+} zpp_adam_tensor;
+
+/* A list of tensors as the step takes it.  `table`: the device's copy of what
+ * zpp_adam_tensors_table wrote; the other fields are set there. */
+typedef struct {
+    const void *table;
+    uint64_t tiles;
+    uint32_t tensors;
+    int32_t state_type, grad_type;
+} zpp_adam_table;
+
+/* Bytes of the table of so many tensors. */
+ZPP_API size_t zpp_adam_tensors_table_bytes(size_t tensors);
+
+/* Checks a list of tensors and writes its table into `table_host` (host memory of
+ * zpp_adam_tensors_table_bytes(count) bytes), which the caller copies to
+ * device memory at 16-byte alignment and sets as list->table; the list then serves
+ * any number of steps while the arrays stay where they are.
+ * state_type: ZPP_F32 or ZPP_I8; grad_type: ZPP_F32 or ZPP_BF16.  No two of the
+ * tensors' arrays may overlap, gradients among themselves excepted (ZPP_EOVERLAP).
+ * count < 2^20; tensors of 0 elements are left out. */
+ZPP_API zpp_status zpp_adam_tensors_table(const zpp_adam_tensor *tensors, size_t count,
+                                          int32_t state_type, int32_t grad_type, void *table_host,
+                                          size_t table_bytes, zpp_adam_table *list);
+
+/* One step of all of them.  hp as for zpp_adam_partition_step, but for
+ * weight_decay, which is each tensor's own and has to be 0 here.  With moments in
+ * fp32 and gradients in fp32 the results are, bit for bit, those of
+ * zpp_adam_partition_step tensor by tensor. */
+ZPP_API zpp_status zpp_adam_tensors_step(const zpp_adam_table *list, const zpp_adam_hparams *hp,
+                                         hipStream_t stream, hipEvent_t wait_before,
+                                         hipEvent_t done_after);
+
+/* Moments between 8 bits and fp32, as a checkpoint of the optimizer needs them:
+ * moment 1 (codes are int8_t) or 2 (uint8_t) of n elements. */
+ZPP_API zpp_status zpp_adam_state_save(const float *x, size_t n, int32_t moment, void *codes,
+                                       float *scales, hipStream_t stream, hipEvent_t wait_before,
+                                       hipEvent_t done_after);
+ZPP_API zpp_status zpp_adam_state_load(const void *codes, const float *scales, size_t n,
+                                       int32_t moment, float *out, hipStream_t stream,
+                                       hipEvent_t wait_before, hipEvent_t done_after);
+
 /* Static, NUL-terminated description of a status code.  Takes any int, so
  * that a caller may pass whatever status value it holds: a value that is not
  * one of zpp_status gives "unknown status". */

@@ -21,7 +21,7 @@ MARSHAL_SOURCE = "marshal.cpp"
 
 SOURCES = ["zpp_api.hip", "adam.hip", "refresh.hip", "quant.hip", "gather.hip", "fused.hip",
            "qgz.hip", "receive_adam.hip", "layer_api.hip", "activations.hip", "layer_norm.hip",
-           "weight_grad.hip"]
+           "weight_grad.hip", "token_api.hip", "rotary.hip", "log_probs.hip", "adam_tensors.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

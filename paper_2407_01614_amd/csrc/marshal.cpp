@@ -7,7 +7,7 @@
 // subclass, a wrapper without storage), is answered with None: the binding
 // then runs its own checks, which raise the error or accept the tensor.
 //
-// The layer operators, whose smallest calls are a few microseconds on the GPU,
+// The layer and token operators, whose smallest calls are a few microseconds on the GPU,
 // are called from here as well, their arguments read and checked on the way.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -22,7 +22,10 @@ namespace {
 
 // dtypes an argument may have, as bits of a mask (kOptional: None may stand
 // in the tensor's place)
-enum : unsigned { kF32 = 1, kBF16 = 2, kI16 = 4, kU16 = 8, kI8 = 16, kU8 = 32, kOptional = 64 };
+enum : unsigned {
+    kF32 = 1, kBF16 = 2, kI16 = 4, kU16 = 8, kI8 = 16, kU8 = 32, kOptional = 64, kI32 = 128,
+    kI64 = 256, kF64 = 512
+};
 
 unsigned dtype_bit(at::ScalarType t) {
     switch (t) {
@@ -32,6 +35,9 @@ unsigned dtype_bit(at::ScalarType t) {
     case at::kUInt16: return kU16;
     case at::kChar: return kI8;
     case at::kByte: return kU8;
+    case at::kInt: return kI32;
+    case at::kLong: return kI64;
+    case at::kDouble: return kF64;
     default: return 0;
     }
 }
@@ -191,6 +197,51 @@ class Call {
         return m;
     }
 
+    // Heads [tokens, heads, dim] or [tokens, groups, heads, dim] of a plain type, which
+    // is one for all of the call; nullptr where None stands.
+    const zpp_heads *heads(zpp_heads *h, size_t tokens, size_t dim, int *type) {
+        if (!take() || args_[-1] == Py_None)
+            return nullptr;
+        PyObject *o = args_[-1];
+        if (!THPVariable_CheckExact(o))
+            return fail_heads();
+        const at::Tensor &t = THPVariable_Unpack(o);
+        const int kind = matrix_type(t.scalar_type());
+        const int64_t d = t.dim();
+        if (!t.is_cuda() || t.device().index() != device_ || (d != 3 && d != 4) ||
+            (kind != ZPP_BF16 && kind != ZPP_F32) || (*type >= 0 && kind != *type) ||
+            (size_t)t.size(0) != tokens || (size_t)t.size(d - 1) != dim ||
+            (dim > 1 && t.stride(d - 1) != 1) || t.size(d - 2) > UINT32_MAX ||
+            (d == 4 && t.size(1) > UINT32_MAX))
+            return fail_heads();
+        *type = kind;
+        *h = {t.data_ptr(), (size_t)t.stride(0), d == 4 ? (size_t)t.stride(1) : 0,
+              (size_t)t.stride(d - 2), d == 4 ? (uint32_t)t.size(1) : 1u, (uint32_t)t.size(d - 2)};
+        return h;
+    }
+
+    // Tokens and features of the heads that come next.
+    bool batch(size_t *tokens, size_t *dim) const {
+        if (!good || args_ >= end_ || !THPVariable_CheckExact(*args_))
+            return false;
+        const at::Tensor &t = THPVariable_Unpack(*args_);
+        if (t.dim() != 3 && t.dim() != 4)
+            return false;
+        *tokens = (size_t)t.size(0);
+        *dim = (size_t)t.size(t.dim() - 1);
+        return *dim <= UINT32_MAX;
+    }
+
+    // The length of the one-dimensional tensor that comes next.
+    size_t length() {
+        if (!good || args_ >= end_ || !THPVariable_CheckExact(*args_) ||
+            THPVariable_Unpack(*args_).dim() != 1) {
+            good = false;
+            return 0;
+        }
+        return (size_t)THPVariable_Unpack(*args_).numel();
+    }
+
     // `count` contiguous values with one of the dtypes of the mask.
     template <class T = void>
     T *vector(unsigned mask, bool needed, size_t count) {
@@ -225,6 +276,7 @@ class Call {
 
     // An address as an integer.
     void *handle() { return pointer(); }
+    long long integer() { return take() ? PyLong_AsLongLong(args_[-1]) : 0; }
     double number() { return take() ? PyFloat_AsDouble(args_[-1]) : 0.0; }
     bool truth() { return take() && PyObject_IsTrue(args_[-1]) == 1; }
 
@@ -248,6 +300,10 @@ class Call {
         return PyLong_AsVoidPtr(args_[-1]);
     }
     const zpp_matrix *fail() {
+        good = false;
+        return nullptr;
+    }
+    const zpp_heads *fail_heads() {
         good = false;
         return nullptr;
     }
@@ -401,6 +457,125 @@ PyObject *weight_grad(PyObject *, PyObject *const *args, Py_ssize_t n) {
     });
 }
 
+// rotary(fn, device, stream, wait, done, x, out, k, k_out, positions, turns, interleaved,
+//        scale)
+PyObject *rotary(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    return run_call(args, n, [](Call &c) {
+        zpp_heads m[4];
+        size_t tokens = 0, dim = 0;
+        int type = -1;
+        c.good = c.batch(&tokens, &dim);
+        const zpp_heads *x = c.heads(&m[0], tokens, dim, &type);
+        const zpp_heads *out = c.heads(&m[1], tokens, dim, &type);
+        const zpp_heads *k = c.heads(&m[2], tokens, dim, &type);
+        const zpp_heads *k_out = c.heads(&m[3], tokens, dim, &type);
+        const int64_t *positions = c.vector<int64_t>(kI64, true, tokens);
+        const size_t pairs = c.length();
+        const double *turns = c.vector<double>(kF64, true, pairs);
+        const bool interleaved = c.truth();
+        const float scale = (float)c.number();
+        if (!c.good || PyErr_Occurred() || !x || !out || !k != !k_out || pairs > UINT32_MAX / 2) {
+            c.good = false;
+            return 0;
+        }
+        return (int)reinterpret_cast<decltype(&zpp_rotary_forward)>(c.fn)(
+            x, out, k, k_out, type, tokens, (uint32_t)dim, (uint32_t)(2 * pairs), positions, turns,
+            interleaved, scale, c.stream, c.wait, c.done);
+    });
+}
+
+// log_probs_forward(fn, device, stream, wait, done, x, targets, log_probs, lse, entropies,
+//                   top, top_ids, top_log_probs, sizes, workspace)
+// sizes: the address of zpp_log_probs_workspace
+PyObject *log_probs_forward(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    return run_call(args, n, [](Call &c) {
+        zpp_matrix m;
+        size_t rows = 0, vocab = 0, size = 0;
+        c.good = c.shape(&rows, &vocab);
+        const zpp_matrix *x = c.matrix(&m, kPlain, true, rows, vocab);
+        const int64_t *targets = c.vector<int64_t>(kI64, true, rows);
+        float *log_probs = c.vector<float>(kF32, true, rows);
+        float *lse = c.vector<float>(kF32, false, rows);
+        float *entropies = c.vector<float>(kF32, false, rows);
+        const long long top = c.integer();
+        c.good = c.good && top >= 0 && top <= ZPP_MAX_TOP;
+        int32_t *ids = c.vector<int32_t>(kI32, top > 0, rows * (size_t)top);
+        float *top_log_probs = c.vector<float>(kF32, top > 0, rows * (size_t)top);
+        const auto sizes = reinterpret_cast<decltype(&zpp_log_probs_workspace)>(c.handle());
+        void *ws = c.good ? c.workspace(sizes(rows, vocab, (uint32_t)top), &size) : nullptr;
+        if (!c.good || PyErr_Occurred())
+            return 0;
+        return (int)reinterpret_cast<decltype(&zpp_log_probs_forward)>(c.fn)(
+            x, rows, vocab, targets, log_probs, lse, entropies, (uint32_t)top, ids, top_log_probs,
+            ws, size, c.stream, c.wait, c.done);
+    });
+}
+
+// log_probs_backward(fn, device, stream, wait, done, x, targets, lse, dlog_probs, entropies,
+//                    dentropies, dx)
+PyObject *log_probs_backward(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    return run_call(args, n, [](Call &c) {
+        zpp_matrix m[2];
+        size_t rows = 0, vocab = 0;
+        c.good = c.shape(&rows, &vocab);
+        const zpp_matrix *x = c.matrix(&m[0], kPlain, true, rows, vocab);
+        const int64_t *targets = c.vector<int64_t>(kI64, true, rows);
+        const float *lse = c.vector<float>(kF32, true, rows);
+        const float *dlog_probs = c.vector<float>(kF32, true, rows);
+        const float *entropies = c.vector<float>(kF32, false, rows);
+        const float *dentropies = c.vector<float>(kF32, false, rows);
+        const zpp_matrix *dx = c.matrix(&m[1], kPlain, true, rows, vocab);
+        return c.good ? (int)reinterpret_cast<decltype(&zpp_log_probs_backward)>(c.fn)(
+                            x, rows, vocab, targets, lse, dlog_probs, entropies, dentropies, dx,
+                            c.stream, c.wait, c.done)
+                      : 0;
+    });
+}
+
+// log_probs_train(fn, device, stream, wait, done, x, targets, log_probs, lse, entropies,
+//                 dlog_probs, dentropies, dx, sizes, workspace)
+PyObject *log_probs_train(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    return run_call(args, n, [](Call &c) {
+        zpp_matrix m[2];
+        size_t rows = 0, vocab = 0, size = 0;
+        c.good = c.shape(&rows, &vocab);
+        const zpp_matrix *x = c.matrix(&m[0], kPlain, true, rows, vocab);
+        const int64_t *targets = c.vector<int64_t>(kI64, true, rows);
+        float *log_probs = c.vector<float>(kF32, true, rows);
+        float *lse = c.vector<float>(kF32, true, rows);
+        float *entropies = c.vector<float>(kF32, false, rows);
+        const float *dlog_probs = c.vector<float>(kF32, true, rows);
+        const float *dentropies = c.vector<float>(kF32, false, rows);
+        const zpp_matrix *dx = c.matrix(&m[1], kPlain, true, rows, vocab);
+        const auto sizes = reinterpret_cast<decltype(&zpp_log_probs_workspace)>(c.handle());
+        void *ws = c.good ? c.workspace(sizes(rows, vocab, 0), &size) : nullptr;
+        if (!c.good || PyErr_Occurred())
+            return 0;
+        return (int)reinterpret_cast<decltype(&zpp_log_probs_train)>(c.fn)(
+            x, rows, vocab, targets, log_probs, lse, entropies, dlog_probs, dentropies, dx, ws,
+            size, c.stream, c.wait, c.done);
+    });
+}
+
+// adam_tensors_step(fn, device, stream, wait, done, list, lr, beta1, beta2, eps, step, adamw)
+// list: the address of a zpp_adam_table
+PyObject *adam_tensors_step(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    return run_call(args, n, [](Call &c) {
+        const zpp_adam_table *list = reinterpret_cast<const zpp_adam_table *>(c.handle());
+        zpp_adam_hparams hp{};
+        hp.lr = (float)c.number();
+        hp.beta1 = (float)c.number();
+        hp.beta2 = (float)c.number();
+        hp.eps = (float)c.number();
+        hp.step = c.integer();
+        hp.adamw = c.truth();
+        if (!c.good || PyErr_Occurred())
+            return 0;
+        return (int)reinterpret_cast<decltype(&zpp_adam_tensors_step)>(c.fn)(list, &hp, c.stream,
+                                                                             c.wait, c.done);
+    });
+}
+
 PyMethodDef methods[] = {
 #define ZPP_CALL(name)                                              \
     {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL,       \
@@ -412,6 +587,11 @@ PyMethodDef methods[] = {
     ZPP_CALL(gelu_forward),
     ZPP_CALL(gelu_backward),
     ZPP_CALL(weight_grad),
+    ZPP_CALL(rotary),
+    ZPP_CALL(log_probs_forward),
+    ZPP_CALL(log_probs_backward),
+    ZPP_CALL(log_probs_train),
+    ZPP_CALL(adam_tensors_step),
     {"addresses", (PyCFunction)(void (*)(void))addresses, METH_FASTCALL,
      "addresses(device, tensor, mask, need, ...) -> tuple or None"},
     {"address_array", (PyCFunction)(void (*)(void))address_array, METH_FASTCALL,
@@ -428,6 +608,8 @@ PyMODINIT_FUNC PyInit__marshal() {
     if (m && (PyModule_AddIntConstant(m, "F32", kF32) || PyModule_AddIntConstant(m, "BF16", kBF16) ||
               PyModule_AddIntConstant(m, "I16", kI16) || PyModule_AddIntConstant(m, "U16", kU16) ||
               PyModule_AddIntConstant(m, "I8", kI8) || PyModule_AddIntConstant(m, "U8", kU8) ||
+              PyModule_AddIntConstant(m, "I32", kI32) || PyModule_AddIntConstant(m, "I64", kI64) ||
+              PyModule_AddIntConstant(m, "F64", kF64) ||
               PyModule_AddIntConstant(m, "OPTIONAL", kOptional))) {
         Py_DECREF(m);
         return nullptr;

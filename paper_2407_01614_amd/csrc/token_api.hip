@@ -1,0 +1,548 @@
+// C ABI of the token operators (declared in include/zpp.h): argument checks,
+// stream ordering with events, and dispatch to the kernels.
+#include <math.h>
+#include <stdint.h>
+#include <string.h>
+
+#include <algorithm>
+#include <new>
+#include <vector>
+
+#include "zpp.h"
+#include "zpp_adam_host.h"
+#include "zpp_arguments.h"
+#include "zpp_token.h"
+
+namespace {
+
+using zpp::aligned;
+using zpp::Arguments;
+using zpp::Heads;
+using zpp::kBf;
+using zpp::kFl;
+using zpp::kMostElems;
+using zpp::Mat;
+using zpp::plain_type;
+using zpp::Range;
+using zpp::run;
+using zpp::type_size;
+
+// --------------------------------------------------------------------------
+// Rotary positions
+// --------------------------------------------------------------------------
+
+// The memory of a batch's heads: dimensions of (count, stride) around pieces of
+// `piece` elements, those that follow each other without a gap made one.
+struct Spread {
+    uintptr_t p;
+    size_t count[3], stride[3], piece, size;
+    int dims;
+    size_t extent() const {  // elements from the first to the last, and one
+        size_t e = piece;
+        for (int d = 0; d < dims; ++d)
+            e += (count[d] - 1) * stride[d];
+        return e;
+    }
+};
+
+Spread spread_of(const Heads &h, size_t tokens, size_t dim, size_t size) {
+    Spread s{(uintptr_t)h.data, {}, {}, dim, size, 0};
+    const size_t count[3] = {h.heads, h.groups, tokens}, stride[3] = {h.head, h.group, h.token};
+    for (int d = 0; d < 3; ++d) {  // from the innermost on
+        if (count[d] == 1)
+            continue;
+        if (s.dims == 0 && stride[d] == s.piece) {
+            s.piece *= count[d];
+        } else if (s.dims && stride[d] == s.count[s.dims - 1] * s.stride[s.dims - 1]) {
+            s.count[s.dims - 1] *= count[d];
+        } else {
+            s.count[s.dims] = count[d];
+            s.stride[s.dims++] = stride[d];
+        }
+    }
+    return s;
+}
+
+// Does every element have a place of its own?  Yes where the dimensions, sorted by
+// stride, each step past all of the ones before (all layouts of a tensor and its
+// slices do).
+bool distinct(Spread s) {
+    for (int a = 0; a < s.dims; ++a)
+        for (int b = a + 1; b < s.dims; ++b)
+            if (s.stride[b] < s.stride[a]) {
+                std::swap(s.stride[a], s.stride[b]);
+                std::swap(s.count[a], s.count[b]);
+            }
+    size_t reach = s.piece;
+    for (int d = 0; d < s.dims; ++d) {
+        if (s.stride[d] < reach)
+            return false;
+        reach += (s.count[d] - 1) * s.stride[d];
+    }
+    return true;
+}
+
+// Do the two share a byte?  Exact for pieces at one distance (columns of a fused
+// product) and for heads of tokens at one distance; where neither holds, arrays
+// within each other's extent count as sharing.
+bool share_heads(const Spread &a, const Spread &b) {
+    const uintptr_t a1 = a.p + a.extent() * a.size, b1 = b.p + b.extent() * b.size;
+    if (a.p >= b1 || b.p >= a1)
+        return false;
+    if (a.dims <= 1 && b.dims <= 1) {
+        const auto range = [](const Spread &s) {
+            return Range{(const void *)s.p, s.dims ? s.count[0] : 1, s.piece * s.size,
+                         s.dims ? s.stride[0] * s.size : 0};
+        };
+        Range x = range(a), y = range(b);
+        if (x.rows == 1)
+            x.stride = y.stride;
+        if (y.rows == 1)
+            y.stride = x.stride;
+        return zpp::share(x, y);
+    }
+    // the outermost dimension at one distance, each piece's place within it
+    const int da = a.dims - 1, db = b.dims - 1;
+    if (da < 0 || db < 0)
+        return true;
+    const size_t period = a.stride[da] * a.size;
+    size_t inner_a = 1, inner_b = 1;
+    for (int d = 0; d < da; ++d)
+        inner_a *= a.count[d];
+    for (int d = 0; d < db; ++d)
+        inner_b *= b.count[d];
+    if (period == 0 || period != b.stride[db] * b.size || inner_a > 65536 / inner_b)
+        return true;
+    const auto place = [](const Spread &s, size_t i) {
+        size_t off = 0;
+        for (int d = 0; d < s.dims - 1; ++d) {
+            off += i % s.count[d] * s.stride[d];
+            i /= s.count[d];
+        }
+        return off * s.size;
+    };
+    for (size_t i = 0; i < inner_a; ++i)
+        for (size_t j = 0; j < inner_b; ++j) {
+            const Range x{(const void *)(a.p + place(a, i)), a.count[da], a.piece * a.size, period};
+            const Range y{(const void *)(b.p + place(b, j)), b.count[db], b.piece * b.size, period};
+            if (zpp::share(x, y))
+                return true;
+        }
+    return false;
+}
+
+// One array of heads as it was given: its place, or the reason it is refused.
+zpp_status heads_of(const zpp_heads *h, size_t tokens, size_t dim, size_t size, Heads *out) {
+    if (!h->data)
+        return ZPP_EINVAL;
+    *out = {h->data, h->token_stride, h->group_stride, h->head_stride, h->groups, h->heads};
+    const size_t count[3] = {tokens, h->groups, h->heads};
+    const size_t stride[3] = {h->token_stride, h->group_stride, h->head_stride};
+    size_t extent = dim;
+    for (int d = 0; d < 3; ++d) {
+        if (count[d] == 1)
+            continue;
+        if (stride[d] > kMostElems / count[d])
+            return ZPP_EINVAL;
+        extent += (count[d] - 1) * stride[d];
+        if (extent > kMostElems)
+            return ZPP_EINVAL;
+    }
+    return aligned(h->data, size) ? ZPP_OK : ZPP_EALIGN;
+}
+
+bool in_place(const Heads &x, const Heads &out, size_t tokens) {
+    return x.data == out.data && (tokens == 1 || x.token == out.token) &&
+           (x.groups == 1 || x.group == out.group) && (x.heads == 1 || x.head == out.head);
+}
+
+constexpr uint32_t kMostDim = 16384, kMostRotated = 4096, kMostHeads = 1u << 16;
+
+zpp_status rotary(const zpp_heads *x, const zpp_heads *out, const zpp_heads *k,
+                  const zpp_heads *k_out, int32_t type, size_t tokens, uint32_t dim,
+                  uint32_t rotated, const int64_t *positions, const double *turns,
+                  int32_t interleaved, float scale, bool backward, hipStream_t stream,
+                  hipEvent_t wait_before, hipEvent_t done_after) {
+    if (!x || !out || !k != !k_out || (type != ZPP_BF16 && type != ZPP_F32) || dim > kMostDim ||
+        rotated > dim || rotated > kMostRotated || rotated % 2 || !isfinite(scale) ||
+        x->groups != out->groups || x->heads != out->heads ||
+        (k && (k->groups != k_out->groups || k->heads != k_out->heads)))
+        return ZPP_EINVAL;
+    const size_t heads_x = (size_t)x->groups * x->heads;
+    const size_t heads_k = k ? (size_t)k->groups * k->heads : 0;
+    if (heads_x >= kMostHeads || heads_k >= kMostHeads || heads_x + heads_k >= kMostHeads)
+        return ZPP_EINVAL;
+    zpp::RotaryArgs a{};
+    const bool work = tokens && dim && heads_x + heads_k;
+    if (work) {
+        const size_t size = type_size(type);
+        if (rotated && (!positions || !turns))
+            return ZPP_EINVAL;
+        if (tokens > kMostElems)
+            return ZPP_EINVAL;
+        const zpp_heads *given[4] = {x, out, k, k_out};
+        Heads *to[4] = {&a.x, &a.out, &a.k, &a.k_out};
+        zpp_status worst = ZPP_OK;
+        for (int i = 0; i < 4; ++i) {
+            if (!given[i] || !given[i]->groups || !given[i]->heads)
+                continue;
+            const zpp_status st = heads_of(given[i], tokens, dim, size, to[i]);
+            if (st != ZPP_OK && (worst == ZPP_OK || st < worst))
+                worst = st;
+        }
+        if (worst == ZPP_EINVAL)
+            return worst;
+        if (worst != ZPP_OK || (rotated && (!aligned(positions, 8) || !aligned(turns, 8))))
+            return ZPP_EALIGN;
+        a.copy_x = a.x.heads && !in_place(a.x, a.out, tokens);
+        a.copy_k = a.k.heads && !in_place(a.k, a.k_out, tokens);
+        Spread s[4];
+        bool there[4];
+        for (int i = 0; i < 4; ++i) {
+            there[i] = to[i]->groups && to[i]->heads;
+            if (there[i])
+                s[i] = spread_of(*to[i], tokens, dim, size);
+        }
+        for (int o = 1; o < 4; o += 2) {
+            if (!there[o])
+                continue;
+            if (!distinct(s[o]))
+                return ZPP_EINVAL;
+            for (int i = 0; i < 4; ++i) {
+                if (i == o || !there[i] || (i == o - 1 && !(o == 1 ? a.copy_x : a.copy_k)))
+                    continue;
+                if (share_heads(s[o], s[i]))
+                    return ZPP_EOVERLAP;
+            }
+            const Range whole{(const void *)s[o].p, 1, s[o].extent() * size, 0};
+            if (rotated && (zpp::share(whole, {positions, 1, tokens * 8, 0}) ||
+                            zpp::share(whole, {turns, 1, (size_t)rotated / 2 * 8, 0})))
+                return ZPP_EOVERLAP;
+        }
+        a.positions = positions;
+        a.turns = turns;
+        a.tokens = tokens;
+        a.dim = dim;
+        a.rotated = rotated;
+        a.scale = scale;
+        a.interleaved = interleaved != 0;
+        a.backward = backward;
+    }
+    return run(stream, wait_before, done_after, work,
+               [&] { return zpp::launch_rotary(a, type, stream); });
+}
+
+// --------------------------------------------------------------------------
+// Log probabilities
+// --------------------------------------------------------------------------
+constexpr size_t kMostVocab = (size_t)1 << 31;  // exclusive
+
+// Checks that the calls share, and the arguments that they have in common.
+zpp::LogProbsArgs log_probs_args(Arguments &args, const zpp_matrix *x, size_t rows, size_t vocab,
+                                 const int64_t *targets) {
+    zpp::LogProbsArgs a{};
+    if (rows && !vocab)
+        args.fail(ZPP_EINVAL);
+    a.x = args.matrix(x, plain_type(x), true, false);
+    args.vector(targets, rows, 8, true, false);
+    a.targets = targets;
+    a.rows = rows;
+    a.vocab = (uint32_t)vocab;
+    return a;
+}
+
+// dx, which may be x itself.
+Mat gradient(Arguments &args, const zpp_matrix *x, const zpp_matrix *dx, size_t rows) {
+    const bool itself = x && dx && x->data && x->data == dx->data && x->type == dx->type &&
+                        (rows <= 1 || x->stride == dx->stride);
+    // an input here, where it is held against the other outputs as x was
+    return args.matrix(dx, plain_type(x), true, !itself);
+}
+
+// --------------------------------------------------------------------------
+// AdamW over many tensors
+// --------------------------------------------------------------------------
+constexpr size_t kMostTensors = (size_t)1 << 20;  // exclusive
+
+struct Piece {
+    uintptr_t from, to;
+    bool output;
+};
+
+bool valid_list(const zpp_adam_table *l) {
+    return l && (l->state_type == ZPP_F32 || l->state_type == ZPP_I8) &&
+           (l->grad_type == ZPP_F32 || l->grad_type == ZPP_BF16) && l->tensors < kMostTensors &&
+           l->tiles < UINT32_MAX && !l->tensors == !l->tiles && (!l->tensors || l->table);
+}
+
+zpp_status state_args(const void *codes, const float *scales, const float *x, size_t n,
+                      int32_t moment, bool save) {
+    if ((moment != 1 && moment != 2) || n > kMostElems)
+        return ZPP_EINVAL;
+    Arguments args(1, 1);
+    args.vector(x, n, 4, true, !save);
+    args.vector(codes, n, 1, true, save);
+    args.vector(scales, (n + ZPP_ADAM_BLOCK - 1) / ZPP_ADAM_BLOCK, 4, true, save);
+    return args.check();
+}
+
+}  // namespace
+
+extern "C" {
+
+ZPP_API zpp_status zpp_rotary_forward(const zpp_heads *x, const zpp_heads *out, const zpp_heads *k,
+                                      const zpp_heads *k_out, int32_t type, size_t tokens,
+                                      uint32_t dim, uint32_t rotated, const int64_t *positions,
+                                      const double *turns, int32_t interleaved, float scale,
+                                      hipStream_t stream, hipEvent_t wait_before,
+                                      hipEvent_t done_after) {
+    return rotary(x, out, k, k_out, type, tokens, dim, rotated, positions, turns, interleaved,
+                  scale, false, stream, wait_before, done_after);
+}
+
+ZPP_API zpp_status zpp_rotary_backward(const zpp_heads *x, const zpp_heads *out, const zpp_heads *k,
+                                       const zpp_heads *k_out, int32_t type, size_t tokens,
+                                       uint32_t dim, uint32_t rotated, const int64_t *positions,
+                                       const double *turns, int32_t interleaved, float scale,
+                                       hipStream_t stream, hipEvent_t wait_before,
+                                       hipEvent_t done_after) {
+    return rotary(x, out, k, k_out, type, tokens, dim, rotated, positions, turns, interleaved,
+                  scale, true, stream, wait_before, done_after);
+}
+
+ZPP_API size_t zpp_log_probs_workspace(size_t rows, size_t vocab, uint32_t top) {
+    if (vocab >= kMostVocab || (vocab && rows > kMostElems / vocab) ||
+        (top && (top > ZPP_MAX_TOP || top > vocab || vocab > ZPP_MAX_TOP_VOCAB)))
+        return 0;
+    return zpp::log_probs_workspace(rows, vocab, top);
+}
+
+ZPP_API zpp_status zpp_log_probs_forward(const zpp_matrix *x, size_t rows, size_t vocab,
+                                         const int64_t *targets, float *log_probs, float *lse,
+                                         float *entropies, uint32_t top, int32_t *top_ids,
+                                         float *top_log_probs, void *workspace,
+                                         size_t workspace_bytes, hipStream_t stream,
+                                         hipEvent_t wait_before, hipEvent_t done_after) {
+    Arguments args(rows, vocab);
+    if (top && (top > ZPP_MAX_TOP || top > vocab || vocab > ZPP_MAX_TOP_VOCAB))
+        args.fail(ZPP_EINVAL);
+    zpp::LogProbsArgs a = log_probs_args(args, x, rows, vocab, targets);
+    args.vector(log_probs, rows, 4, true, true);
+    args.vector(lse, rows, 4, false, true);
+    args.vector(entropies, rows, 4, false, true);
+    if (top && rows <= kMostElems / ZPP_MAX_TOP) {
+        args.vector(top_ids, rows * top, 4, true, true);
+        args.vector(top_log_probs, rows * top, 4, true, true);
+    }
+    args.workspace(workspace, workspace_bytes, zpp_log_probs_workspace(rows, vocab, top));
+    const zpp_status st = args.check();
+    if (st != ZPP_OK)
+        return st;
+    a.log_probs = log_probs;
+    a.lse = lse;
+    a.entropies = entropies;
+    a.top = top;
+    a.top_ids = top_ids;
+    a.top_log_probs = top_log_probs;
+    a.workspace = workspace;
+    return run(stream, wait_before, done_after, rows != 0,
+               [&] { return zpp::launch_log_probs_forward(a, x->type, stream); });
+}
+
+ZPP_API zpp_status zpp_log_probs_backward(const zpp_matrix *x, size_t rows, size_t vocab,
+                                          const int64_t *targets, const float *lse,
+                                          const float *dlog_probs, const float *entropies,
+                                          const float *dentropies, const zpp_matrix *dx,
+                                          hipStream_t stream, hipEvent_t wait_before,
+                                          hipEvent_t done_after) {
+    Arguments args(rows, vocab);
+    zpp::LogProbsArgs a = log_probs_args(args, x, rows, vocab, targets);
+    if (rows && !entropies != !dentropies)
+        args.fail(ZPP_EINVAL);
+    args.vector(lse, rows, 4, true, false);
+    args.vector(dlog_probs, rows, 4, true, false);
+    args.vector(entropies, rows, 4, false, false);
+    args.vector(dentropies, rows, 4, false, false);
+    a.dx = gradient(args, x, dx, rows);
+    const zpp_status st = args.check();
+    if (st != ZPP_OK)
+        return st;
+    a.lse = const_cast<float *>(lse);
+    a.entropies = const_cast<float *>(entropies);
+    a.dlog_probs = dlog_probs;
+    a.dentropies = dentropies;
+    return run(stream, wait_before, done_after, rows != 0,
+               [&] { return zpp::launch_log_probs_backward(a, x->type, stream); });
+}
+
+ZPP_API zpp_status zpp_log_probs_train(const zpp_matrix *x, size_t rows, size_t vocab,
+                                       const int64_t *targets, float *log_probs, float *lse,
+                                       float *entropies, const float *dlog_probs,
+                                       const float *dentropies, const zpp_matrix *dx,
+                                       void *workspace, size_t workspace_bytes, hipStream_t stream,
+                                       hipEvent_t wait_before, hipEvent_t done_after) {
+    Arguments args(rows, vocab);
+    zpp::LogProbsArgs a = log_probs_args(args, x, rows, vocab, targets);
+    if (rows && dentropies && !entropies)
+        args.fail(ZPP_EINVAL);
+    args.vector(log_probs, rows, 4, true, true);
+    args.vector(lse, rows, 4, true, true);
+    args.vector(entropies, rows, 4, false, true);
+    args.vector(dlog_probs, rows, 4, true, false);
+    args.vector(dentropies, rows, 4, false, false);
+    a.dx = gradient(args, x, dx, rows);
+    args.workspace(workspace, workspace_bytes, zpp_log_probs_workspace(rows, vocab, 0));
+    const zpp_status st = args.check();
+    if (st != ZPP_OK)
+        return st;
+    a.log_probs = log_probs;
+    a.lse = lse;
+    a.entropies = entropies;
+    a.dlog_probs = dlog_probs;
+    a.dentropies = dentropies;
+    a.workspace = workspace;
+    return run(stream, wait_before, done_after, rows != 0,
+               [&] { return zpp::launch_log_probs_train(a, x->type, stream); });
+}
+
+ZPP_API size_t zpp_adam_tensors_table_bytes(size_t tensors) {
+    return tensors && tensors < kMostTensors ? zpp::adam_table_bytes(tensors) : 0;
+}
+
+ZPP_API zpp_status zpp_adam_tensors_table(const zpp_adam_tensor *tensors, size_t count,
+                                          int32_t state_type, int32_t grad_type, void *table_host,
+                                          size_t table_bytes, zpp_adam_table *list) {
+    if (!list || count >= kMostTensors || (count && !tensors) ||
+        (state_type != ZPP_F32 && state_type != ZPP_I8) ||
+        (grad_type != ZPP_F32 && grad_type != ZPP_BF16) ||
+        (count && (!table_host || table_bytes < zpp::adam_table_bytes(count))))
+        return ZPP_EINVAL;
+    if (count && !aligned(table_host, 8))
+        return ZPP_EALIGN;
+    const size_t state = type_size(state_type), grad = type_size(grad_type);
+    const bool codes = state_type == ZPP_I8;
+    bool misaligned = false;
+    uint64_t tiles = 0;
+    for (size_t i = 0; i < count; ++i) {
+        const zpp_adam_tensor &t = tensors[i];
+        if (!isfinite(t.weight_decay))
+            return ZPP_EINVAL;
+        if (!t.n)
+            continue;
+        if (t.n > kMostElems || !t.master || !t.exp_avg || !t.exp_avg_sq || !t.grad ||
+            (codes && (!t.exp_avg_scales || !t.exp_avg_sq_scales)))
+            return ZPP_EINVAL;
+        tiles += (t.n + zpp::kAdamTile - 1) / zpp::kAdamTile;
+        if (tiles >= UINT32_MAX)
+            return ZPP_EINVAL;
+        misaligned |= !aligned(t.master, 4) || !aligned(t.exp_avg, state) ||
+                      !aligned(t.exp_avg_sq, state) || !aligned(t.grad, grad) ||
+                      !aligned(t.primary_bf16, 2) ||
+                      (codes && (!aligned(t.exp_avg_scales, 4) || !aligned(t.exp_avg_sq_scales, 4)));
+    }
+    if (misaligned)
+        return ZPP_EALIGN;
+    try {
+        std::vector<Piece> pieces;
+        pieces.reserve(7 * count);
+        const auto add = [&](const void *p, size_t bytes, bool output) {
+            if (p && bytes)
+                pieces.push_back({(uintptr_t)p, (uintptr_t)p + bytes, output});
+        };
+        std::vector<zpp::AdamEntry> entries;
+        entries.reserve(count);
+        uint64_t first = 0;
+        for (size_t i = 0; i < count; ++i) {
+            const zpp_adam_tensor &t = tensors[i];
+            if (!t.n)
+                continue;
+            const size_t blocks = (t.n + zpp::kAdamTile - 1) / zpp::kAdamTile;
+            add(t.master, 4 * t.n, true);
+            add(t.exp_avg, state * t.n, true);
+            add(t.exp_avg_sq, state * t.n, true);
+            add(codes ? t.exp_avg_scales : nullptr, 4 * blocks, true);
+            add(codes ? t.exp_avg_sq_scales : nullptr, 4 * blocks, true);
+            add(t.grad, grad * t.n, false);
+            add(t.primary_bf16, 2 * t.n, true);
+            entries.push_back({t.master, t.exp_avg, t.exp_avg_sq, t.exp_avg_scales,
+                               t.exp_avg_sq_scales, t.grad, t.primary_bf16, t.n, t.weight_decay,
+                               (uint32_t)first});
+            first += blocks;
+        }
+        // by address: what starts before the furthest end so far overlaps it, and
+        // only gradients may
+        std::sort(pieces.begin(), pieces.end(),
+                  [](const Piece &a, const Piece &b) { return a.from < b.from; });
+        uintptr_t end = 0, end_output = 0;
+        for (const Piece &p : pieces) {
+            if (p.from < (p.output ? end : end_output))
+                return ZPP_EOVERLAP;
+            end = std::max(end, p.to);
+            if (p.output)
+                end_output = std::max(end_output, p.to);
+        }
+        char *out = reinterpret_cast<char *>(table_host);
+        if (!entries.empty())
+            memcpy(out, entries.data(), entries.size() * sizeof(zpp::AdamEntry));
+        std::vector<uint32_t> level(entries.size());
+        for (size_t i = 0; i < entries.size(); ++i)
+            level[i] = entries[i].first;
+        out += entries.size() * sizeof(zpp::AdamEntry);
+        while (!level.empty()) {
+            const size_t n = level.size();
+            level.resize(zpp::padded_level(n), UINT32_MAX);
+            memcpy(out, level.data(), level.size() * sizeof(uint32_t));
+            out += level.size() * sizeof(uint32_t);
+            if (n <= zpp::kSearch)
+                break;
+            std::vector<uint32_t> next;
+            for (size_t i = 0; i < n; i += zpp::kSearch)
+                next.push_back(level[i]);
+            level.swap(next);
+        }
+        *list = {nullptr, tiles, (uint32_t)entries.size(), state_type, grad_type};
+    } catch (const std::bad_alloc &) {
+        return zpp::hip_fail(hipErrorOutOfMemory);
+    }
+    return ZPP_OK;
+}
+
+ZPP_API zpp_status zpp_adam_tensors_step(const zpp_adam_table *list, const zpp_adam_hparams *hp,
+                                         hipStream_t stream, hipEvent_t wait_before,
+                                         hipEvent_t done_after) {
+    const zpp_status st = zpp::check_hparams(hp);
+    if (st != ZPP_OK)
+        return st;
+    if (hp->weight_decay != 0.0f || !valid_list(list))
+        return ZPP_EINVAL;
+    if (!aligned(list->table, 16))
+        return ZPP_EALIGN;
+    zpp::AdamConsts c = zpp::adam_consts(*hp);
+    c.lr_wd = hp->lr;  // times each tensor's decay on the device
+    return run(stream, wait_before, done_after, list->tensors != 0, [&] {
+        return zpp::launch_adam_tensors(list->table, list->tensors, list->tiles, list->state_type,
+                                        list->grad_type, c, stream);
+    });
+}
+
+ZPP_API zpp_status zpp_adam_state_save(const float *x, size_t n, int32_t moment, void *codes,
+                                       float *scales, hipStream_t stream, hipEvent_t wait_before,
+                                       hipEvent_t done_after) {
+    const zpp_status st = state_args(codes, scales, x, n, moment, true);
+    if (st != ZPP_OK)
+        return st;
+    return run(stream, wait_before, done_after, n != 0,
+               [&] { return zpp::launch_adam_state_save(x, n, moment, codes, scales, stream); });
+}
+
+ZPP_API zpp_status zpp_adam_state_load(const void *codes, const float *scales, size_t n,
+                                       int32_t moment, float *out, hipStream_t stream,
+                                       hipEvent_t wait_before, hipEvent_t done_after) {
+    const zpp_status st = state_args(codes, scales, out, n, moment, false);
+    if (st != ZPP_OK)
+        return st;
+    return run(stream, wait_before, done_after, n != 0,
+               [&] { return zpp::launch_adam_state_load(codes, scales, n, moment, out, stream); });
+}
+
+}  // extern "C"

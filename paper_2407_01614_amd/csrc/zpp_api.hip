@@ -7,11 +7,14 @@
 
 #include "zpp.h"
 #include "zpp_abi.h"
+#include "zpp_adam_host.h"
 #include "zpp_launch.h"
 
 namespace {
 
+using zpp::adam_consts;
 using zpp::aligned;
+using zpp::check_hparams;
 using zpp::hip_fail;
 using zpp::record;
 using zpp::wait_on;
@@ -69,36 +72,6 @@ bool any_overlap(const void *const *ptrs, const size_t *bytes, int k) {
     return false;
 }
 
-zpp_status check_hparams(const zpp_adam_hparams *hp) {
-    if (!hp)
-        return ZPP_EINVAL;
-    if (!isfinite(hp->lr) || !isfinite(hp->beta1) || !isfinite(hp->beta2) ||
-        !isfinite(hp->eps) || !isfinite(hp->weight_decay))
-        return ZPP_EINVAL;
-    if (hp->beta1 < 0.0f || hp->beta1 >= 1.0f || hp->beta2 < 0.0f || hp->beta2 >= 1.0f ||
-        hp->eps < 0.0f || hp->step < 1)
-        return ZPP_EINVAL;
-    return ZPP_OK;
-}
-
-// Step-dependent constants, folded on the host in double and rounded once.
-zpp::AdamConsts adam_consts(const zpp_adam_hparams &hp) {
-    zpp::AdamConsts c;
-    const double b1 = hp.beta1, b2 = hp.beta2, lr = hp.lr, wd = hp.weight_decay;
-    const double bc1 = 1.0 - pow(b1, (double)hp.step);
-    const double bc2 = 1.0 - pow(b2, (double)hp.step);
-    c.lr_wd = (float)(lr * wd);
-    c.wd = hp.weight_decay;
-    c.beta1 = hp.beta1;
-    c.one_minus_beta1 = (float)(1.0 - b1);
-    c.beta2 = hp.beta2;
-    c.one_minus_beta2 = (float)(1.0 - b2);
-    c.step_size = (float)(lr / bc1);
-    c.inv_bc2 = (float)(1.0 / bc2);
-    c.eps = hp.eps;
-    c.adamw = hp.adamw ? 1 : 0;
-    return c;
-}
 
 // Bytes of codes and count of scales of an interleaved receive buffer of
 // num_src int4 copies of n elements in blocks of `block`.

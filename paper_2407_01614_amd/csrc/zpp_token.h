@@ -1,0 +1,87 @@
+// Internal launchers of the token operators (rotary positions, log
+// probabilities, AdamW over many tensors).  Arguments are already validated; each
+// launcher only enqueues its kernels on `stream` and returns the launch error.
+#pragma once
+
+#include <hip/hip_runtime_api.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "zpp_launch.h"
+#include "zpp_layer.h"
+
+namespace zpp {
+
+// Heads of a batch of tokens (zpp_heads).
+struct Heads {
+    void *data;
+    size_t token, group, head;  // strides
+    uint32_t groups, heads;
+};
+
+struct RotaryArgs {
+    Heads x, out, k, k_out;  // k without heads: not given
+    const int64_t *positions;
+    const double *turns;
+    size_t tokens;
+    uint32_t dim, rotated;
+    float scale;
+    bool interleaved, backward;
+    bool copy_x, copy_k;  // not in place: features that do not turn are copied
+};
+hipError_t launch_rotary(const RotaryArgs &a, int type, hipStream_t stream);
+
+struct LogProbsArgs {
+    Mat x, dx;
+    const int64_t *targets;
+    float *log_probs, *lse, *entropies;
+    const float *dlog_probs, *dentropies;
+    int32_t *top_ids;
+    float *top_log_probs;
+    void *workspace;
+    size_t rows;
+    uint32_t vocab, top;
+};
+size_t log_probs_workspace(size_t rows, size_t vocab, uint32_t top);
+hipError_t launch_log_probs_forward(const LogProbsArgs &a, int type, hipStream_t stream);
+hipError_t launch_log_probs_backward(const LogProbsArgs &a, int type, hipStream_t stream);
+hipError_t launch_log_probs_train(const LogProbsArgs &a, int type, hipStream_t stream);
+
+// Elements of a tile of the many-tensor step, and of a block of its 8-bit moments.
+constexpr uint32_t kAdamTile = 256;
+
+// A tensor in the table on the device.
+struct AdamEntry {
+    float *p;
+    void *m, *v;
+    float *m_scales, *v_scales;
+    const void *g;
+    uint16_t *primary;
+    uint64_t n;
+    float decay;
+    uint32_t first;  // its first tile, counted over all tensors
+};
+
+// The table: the entries, then levels of first tiles for the search of a tile's
+// tensor.  Level 0 holds every entry's, padded with UINT32_MAX to a multiple of
+// 64; each further level the first of every 64 of the one before, up to a level of
+// 64 values.
+constexpr uint32_t kSearch = 64;
+inline size_t padded_level(size_t n) { return (n + kSearch - 1) / kSearch * kSearch; }
+inline size_t adam_table_bytes(size_t tensors) {
+    size_t words = 0, n = tensors;
+    do {
+        words += padded_level(n);
+        n = (n + kSearch - 1) / kSearch;
+    } while (n > 1);
+    return tensors * sizeof(AdamEntry) + words * sizeof(uint32_t);
+}
+
+hipError_t launch_adam_tensors(const void *table, uint32_t tensors, uint64_t tiles, int state_type,
+                               int grad_type, const AdamConsts &c, hipStream_t stream);
+hipError_t launch_adam_state_save(const float *x, size_t n, int moment, void *codes, float *scales,
+                                  hipStream_t stream);
+hipError_t launch_adam_state_load(const void *codes, const float *scales, size_t n, int moment,
+                                  float *out, hipStream_t stream);
+
+}  // namespace zpp

@@ -9,6 +9,7 @@ Both must have been built (``paper_2407_01614_amd.build``); importing
 this module fails loudly otherwise.  There is no fallback of any kind.
 """
 import ctypes
+import math
 import os
 
 import torch
@@ -102,6 +103,31 @@ _lib.zpp_weight_grad_workspace.restype = _sz
 _lib.zpp_weight_grad_workspace.argtypes = [_sz, _sz, _sz]
 _lib.zpp_weight_grad.restype = ctypes.c_int
 _lib.zpp_weight_grad.argtypes = [_mat, _mat, _sz, _sz, _sz, _mat, _i32, _P, _sz, _P, _P, _P]
+_heads_arg = _P  # a zpp_heads, as the bytes that _heads makes of a tensor
+for _name in ("zpp_rotary_forward", "zpp_rotary_backward"):
+    getattr(_lib, _name).restype = ctypes.c_int
+    getattr(_lib, _name).argtypes = [_heads_arg, _heads_arg, _heads_arg, _heads_arg, _i32, _sz,
+                                     _u32, _u32, _P, _P, _i32, ctypes.c_float, _P, _P, _P]
+_lib.zpp_log_probs_workspace.restype = _sz
+_lib.zpp_log_probs_workspace.argtypes = [_sz, _sz, _u32]
+_lib.zpp_log_probs_forward.restype = ctypes.c_int
+_lib.zpp_log_probs_forward.argtypes = [_mat, _sz, _sz, _P, _P, _P, _P, _u32, _P, _P, _P, _sz, _P,
+                                       _P, _P]
+_lib.zpp_log_probs_backward.restype = ctypes.c_int
+_lib.zpp_log_probs_backward.argtypes = [_mat, _sz, _sz, _P, _P, _P, _P, _P, _mat, _P, _P, _P]
+_lib.zpp_log_probs_train.restype = ctypes.c_int
+_lib.zpp_log_probs_train.argtypes = [_mat, _sz, _sz, _P, _P, _P, _P, _P, _P, _mat, _P, _sz, _P,
+                                     _P, _P]
+_lib.zpp_adam_tensors_table_bytes.restype = _sz
+_lib.zpp_adam_tensors_table_bytes.argtypes = [_sz]
+_lib.zpp_adam_tensors_table.restype = ctypes.c_int
+_lib.zpp_adam_tensors_table.argtypes = [_P, _sz, _i32, _i32, _P, _sz, _P]
+_lib.zpp_adam_tensors_step.restype = ctypes.c_int
+_lib.zpp_adam_tensors_step.argtypes = [_P, ctypes.POINTER(AdamHParams), _P, _P, _P]
+_lib.zpp_adam_state_save.restype = ctypes.c_int
+_lib.zpp_adam_state_save.argtypes = [_P, _sz, _i32, _P, _P, _P, _P, _P]
+_lib.zpp_adam_state_load.restype = ctypes.c_int
+_lib.zpp_adam_state_load.argtypes = [_P, _P, _sz, _i32, _P, _P, _P, _P]
 _lib.zpp_status_string.restype = ctypes.c_char_p
 _lib.zpp_status_string.argtypes = [ctypes.c_int]
 _lib.zpp_last_hip_error.restype = ctypes.c_int
@@ -116,8 +142,11 @@ EXPORTS = ("zpp_adam_partition_step", "zpp_adam_step_refresh_quantize", "zpp_ref
            "zpp_qgz_receive_step_refresh_quantize_interleaved", "zpp_checkpoint_save",
            "zpp_checkpoint_load", "zpp_layer_norm_forward", "zpp_layer_norm_backward_workspace",
            "zpp_layer_norm_backward", "zpp_gelu_forward", "zpp_gelu_backward",
-           "zpp_weight_grad_workspace", "zpp_weight_grad", "zpp_status_string",
-           "zpp_last_hip_error")
+           "zpp_weight_grad_workspace", "zpp_weight_grad", "zpp_rotary_forward",
+           "zpp_rotary_backward", "zpp_log_probs_workspace", "zpp_log_probs_forward",
+           "zpp_log_probs_backward", "zpp_log_probs_train", "zpp_adam_tensors_table_bytes",
+           "zpp_adam_tensors_table", "zpp_adam_tensors_step", "zpp_adam_state_save",
+           "zpp_adam_state_load", "zpp_status_string", "zpp_last_hip_error")
 
 
 class ZppError(RuntimeError):
@@ -691,7 +720,8 @@ def _fn(name):
 _FN = {name: _fn("zpp_" + name) for name in (
     "checkpoint_save", "checkpoint_load", "layer_norm_forward", "layer_norm_backward",
     "layer_norm_backward_workspace", "gelu_forward", "gelu_backward", "weight_grad",
-    "weight_grad_workspace")}
+    "weight_grad_workspace", "rotary_forward", "rotary_backward", "log_probs_workspace",
+    "log_probs_forward", "log_probs_backward", "log_probs_train", "adam_tensors_step")}
 
 
 def _where(name, stream, wait_before, done_after):
@@ -849,6 +879,330 @@ def weight_grad(dy, x, dw, workspace, *, accumulate=False, stream=None, wait_bef
     st = _lib.zpp_weight_grad(md, mx, rows, n, k, mw, 1 if accumulate else 0, ws, size,
                               *where[2:])
     _check(st, "zpp_weight_grad")
+
+
+# --------------------------------------------------------------------------
+# Token operators: rotary positions, log probabilities, AdamW over many tensors.
+# --------------------------------------------------------------------------
+MAX_TOP = 64        # most alternatives of `log_probs_forward`
+ADAM_BLOCK = 256    # values of a block of moments in 8 bits
+
+_I32 = _marshal.I32
+_I64 = _marshal.I64
+_F64 = _marshal.F64
+_DTYPES[_I32] = (torch.int32,)
+_DTYPES[_I64] = (torch.int64,)
+_DTYPES[_F64] = (torch.float64,)
+
+
+class Heads(ctypes.Structure):
+    """Mirror of ``zpp_heads``."""
+    _fields_ = [("data", _P), ("token_stride", _sz), ("group_stride", _sz), ("head_stride", _sz),
+                ("groups", _u32), ("heads", _u32)]
+
+
+def _heads(t, tokens, dim, kind, name):
+    """One array's checks in Python: its zpp_heads, or the error."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if _MATRIX_TYPES.get(t.dtype, 2) == 2:
+        raise TypeError("%s must be bf16 or fp32" % name)
+    if kind is not None and _MATRIX_TYPES[t.dtype] != kind:
+        raise TypeError("%s must have the type of x" % name)
+    if t.dim() not in (3, 4):
+        raise ValueError("%s must be [tokens, heads, features] or [tokens, groups, heads, "
+                         "features]" % name)
+    if not t.is_cuda:
+        raise ValueError("%s must be on the GPU" % name)
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError("%s is on %s, not on the current device cuda:%d"
+                         % (name, t.device, torch.cuda.current_device()))
+    if t.shape[0] != tokens or t.shape[-1] != dim:
+        raise ValueError("%s must have %d tokens and %d features a head, not %s"
+                         % (name, tokens, dim, list(t.shape)))
+    if dim > 1 and t.stride(-1) != 1:
+        raise ValueError("%s: the features of a head must be consecutive" % name)
+    if max(t.shape) >= 1 << 32:
+        raise ValueError("%s is too large" % name)
+    four = t.dim() == 4
+    return bytes(Heads(t.data_ptr(), t.stride(0), t.stride(1) if four else 0, t.stride(-2),
+                       t.shape[1] if four else 1, t.shape[-2]))
+
+
+def _rotary(name, x, positions, turns, out, k, k_out, interleaved, scale, stream, wait_before,
+            done_after):
+    where = _where(name, stream, wait_before, done_after)
+    st = _marshal.rotary(*where, x, out, k, k_out, positions, turns, interleaved, scale)
+    if st is not None:
+        return _check(st, "zpp_" + name)
+    if not isinstance(x, torch.Tensor):
+        raise TypeError("x must be a torch.Tensor")
+    if (k is None) != (k_out is None):
+        raise ValueError("k and k_out go together")
+    if x.dim() not in (3, 4):
+        raise ValueError("x must be [tokens, heads, features] or [tokens, groups, heads, features]")
+    tokens, dim = x.shape[0], x.shape[-1]
+    mx = _heads(x, tokens, dim, None, "x")
+    kind = _MATRIX_TYPES[x.dtype]
+    others = [_heads(t, tokens, dim, kind, n) for t, n in ((out, "out"), (k, "k"),
+                                                           (k_out, "k_out"))]
+    if out is None:
+        raise TypeError("out must be a torch.Tensor")
+    if not isinstance(turns, torch.Tensor) or turns.dim() != 1:
+        raise TypeError("turns must be a one-dimensional torch.Tensor")
+    pos, trn = _addresses(("positions", "turns"), "positions hold one value a token",
+                          positions, _I64, tokens, turns, _F64, turns.numel())
+    st = getattr(_lib, "zpp_" + name)(mx, *others, kind, tokens, dim, 2 * turns.numel(), pos, trn,
+                                      1 if interleaved else 0, scale, *where[2:])
+    _check(st, "zpp_" + name)
+
+
+def rotary_forward(x, positions, turns, out, *, k=None, k_out=None, interleaved=False, scale=1.0,
+                   stream=None, wait_before=None, done_after=None):
+    """zpp_rotary_forward: the heads of ``x`` [tokens, heads, features] or [tokens,
+    groups, heads, features], and of ``k``, turned by their positions (int64) into
+    ``out`` and ``k_out``, which may be ``x`` and ``k``.  ``turns`` (float64) holds
+    the turns a position of each pair: the first 2 * len(turns) features turn."""
+    _rotary("rotary_forward", x, positions, turns, out, k, k_out, interleaved, scale, stream,
+            wait_before, done_after)
+
+
+def rotary_backward(x, positions, turns, out, *, k=None, k_out=None, interleaved=False, scale=1.0,
+                    stream=None, wait_before=None, done_after=None):
+    """zpp_rotary_backward: gradients of `rotary_forward`'s outputs, ``x`` and ``k``,
+    turned back into those of its inputs."""
+    _rotary("rotary_backward", x, positions, turns, out, k, k_out, interleaved, scale, stream,
+            wait_before, done_after)
+
+
+def rotary_turns(rotated, base=10000.0, linear=1.0, device="cuda"):
+    """The turns a position of each pair of ``rotated`` features, float64: base^(-2i /
+    rotated) / (2 pi linear), with positions divided by ``linear``."""
+    at = torch.arange(rotated // 2, dtype=torch.float64)
+    return (float(base) ** (-2 * at / rotated) / (2 * math.pi * linear)).to(device)
+
+
+def log_probs_workspace(rows, vocab, top=0):
+    """Bytes of workspace of `log_probs_forward` and `log_probs_train` (top = 0)."""
+    return _lib.zpp_log_probs_workspace(rows, vocab, top)
+
+
+def _top(top_ids, top_log_probs, rows):
+    """How many alternatives the arrays [rows, top] ask for."""
+    if top_ids is None and top_log_probs is None:
+        return 0
+    for t, name in ((top_ids, "top_ids"), (top_log_probs, "top_log_probs")):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError("top_ids and top_log_probs go together: %s must be a torch.Tensor"
+                            % name)
+        if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != top_ids.shape[1]:
+            raise ValueError("top_ids and top_log_probs must be [rows, top]")
+    return top_ids.shape[1]
+
+
+def log_probs_forward(x, targets, log_probs, lse, workspace, *, entropies=None, top_ids=None,
+                      top_log_probs=None, stream=None, wait_before=None, done_after=None):
+    """zpp_log_probs_forward: of the logits x [rows, vocab] the log probabilities of
+    ``targets`` (int64, negative: none), ``lse`` (may be None), ``entropies``, and the
+    most probable tokens into ``top_ids`` (int32) and ``top_log_probs`` [rows, top].
+    ``workspace`` may be None where `log_probs_workspace` is 0."""
+    where = _where("log_probs_forward", stream, wait_before, done_after)
+    rows, vocab = _shape(x, "x")
+    top = _top(top_ids, top_log_probs, rows)
+    st = _marshal.log_probs_forward(*where, x, targets, log_probs, lse, entropies, top, top_ids,
+                                    top_log_probs, _FN["log_probs_workspace"], workspace)
+    if st is not None:
+        return _check(st, "zpp_log_probs_forward")
+    mx, = _matrices(("x",), x, _PLAIN, rows, vocab)
+    found = _addresses(
+        ("targets", "log_probs", "lse", "entropies", "top_ids", "top_log_probs"),
+        "targets, log_probs, lse and entropies hold one value a row",
+        targets, _I64, rows, log_probs, _F32, rows, lse, _F32 | _OPTIONAL, rows,
+        entropies, _F32 | _OPTIONAL, rows, top_ids, _I32 | _OPTIONAL, rows * top,
+        top_log_probs, _F32 | _OPTIONAL, rows * top)
+    ws, size = _workspace(workspace, _lib.zpp_log_probs_workspace(rows, vocab, top),
+                          "log_probs_forward")
+    st = _lib.zpp_log_probs_forward(mx, rows, vocab, *found[:4], top, *found[4:], ws, size,
+                                    *where[2:])
+    _check(st, "zpp_log_probs_forward")
+
+
+def log_probs_backward(x, targets, lse, dlog_probs, dx, *, entropies=None, dentropies=None,
+                       stream=None, wait_before=None, done_after=None):
+    """zpp_log_probs_backward: the gradient of the logits into ``dx``, which may be
+    ``x``, from the forward pass's ``lse`` (and ``entropies``) and the gradients of its
+    log probabilities (and ``dentropies``)."""
+    where = _where("log_probs_backward", stream, wait_before, done_after)
+    st = _marshal.log_probs_backward(*where, x, targets, lse, dlog_probs, entropies, dentropies,
+                                     dx)
+    if st is not None:
+        return _check(st, "zpp_log_probs_backward")
+    rows, vocab = _shape(x, "x")
+    mx, mo = _matrices(("x", "dx"), x, _PLAIN, rows, vocab, dx, _PLAIN, rows, vocab)
+    found = _addresses(("targets", "lse", "dlog_probs", "entropies", "dentropies"),
+                       "each holds one value a row", targets, _I64, rows, lse, _F32, rows,
+                       dlog_probs, _F32, rows, entropies, _F32 | _OPTIONAL, rows,
+                       dentropies, _F32 | _OPTIONAL, rows)
+    st = _lib.zpp_log_probs_backward(mx, rows, vocab, *found, mo, *where[2:])
+    _check(st, "zpp_log_probs_backward")
+
+
+def log_probs_train(x, targets, log_probs, lse, dlog_probs, dx, workspace, *, entropies=None,
+                    dentropies=None, stream=None, wait_before=None, done_after=None):
+    """zpp_log_probs_train: `log_probs_forward` and `log_probs_backward` in one call,
+    reading x once; ``dx`` may be ``x``."""
+    where = _where("log_probs_train", stream, wait_before, done_after)
+    st = _marshal.log_probs_train(*where, x, targets, log_probs, lse, entropies, dlog_probs,
+                                  dentropies, dx, _FN["log_probs_workspace"], workspace)
+    if st is not None:
+        return _check(st, "zpp_log_probs_train")
+    rows, vocab = _shape(x, "x")
+    mx, mo = _matrices(("x", "dx"), x, _PLAIN, rows, vocab, dx, _PLAIN, rows, vocab)
+    found = _addresses(
+        ("targets", "log_probs", "lse", "entropies", "dlog_probs", "dentropies"),
+        "each holds one value a row", targets, _I64, rows, log_probs, _F32, rows, lse, _F32, rows,
+        entropies, _F32 | _OPTIONAL, rows, dlog_probs, _F32, rows,
+        dentropies, _F32 | _OPTIONAL, rows)
+    ws, size = _workspace(workspace, _lib.zpp_log_probs_workspace(rows, vocab, 0),
+                          "log_probs_train")
+    st = _lib.zpp_log_probs_train(mx, rows, vocab, *found, mo, ws, size, *where[2:])
+    _check(st, "zpp_log_probs_train")
+
+
+class AdamTensor(ctypes.Structure):
+    """Mirror of ``zpp_adam_tensor``."""
+    _fields_ = [("master", _P), ("exp_avg", _P), ("exp_avg_sq", _P), ("exp_avg_scales", _P),
+                ("exp_avg_sq_scales", _P), ("grad", _P), ("primary_bf16", _P), ("n", _sz),
+                ("weight_decay", ctypes.c_float)]
+
+
+class AdamTable(ctypes.Structure):
+    """Mirror of ``zpp_adam_table``."""
+    _fields_ = [("table", _P), ("tiles", ctypes.c_uint64), ("tensors", _u32),
+                ("state_type", _i32), ("grad_type", _i32)]
+
+
+def empty_adam_state(n, moment, device="cuda"):
+    """A first (1) or second (2) moment of n zeros in 8 bits: (codes, scales)."""
+    return (torch.zeros(n, dtype={1: torch.int8, 2: torch.uint8}[moment], device=device),
+            torch.zeros(num_blocks(n, ADAM_BLOCK), device=device))
+
+
+def _state8(state, dtype, name):
+    if not (isinstance(state, tuple) and len(state) == 2):
+        raise TypeError("%s: moments in 8 bits are a tuple (codes, scales)" % name)
+    codes, scales = _dev(state[0], (dtype,), name + "[0]"), _dev(state[1], _DTYPES[_F32],
+                                                                 name + "[1]")
+    if scales.numel() < num_blocks(codes.numel(), ADAM_BLOCK):
+        raise ValueError("%s: too few scales" % name)
+    return codes, scales
+
+
+class AdamTensors:
+    """A list of tensors that `adam_tensors_step` updates: the table of
+    zpp_adam_tensors_table on the device and references to its tensors, whose
+    memory has to stay where it is.
+
+    ``master``: fp32 tensors; ``exp_avg`` and ``exp_avg_sq``: fp32, or all of them in 8
+    bits as (codes, scales) like `empty_adam_state` makes; ``grad``: all fp32 or all
+    bf16; ``primary_bf16``: the bf16 copies, None in the place of one (or of the list) that is not
+    kept; ``weight_decay``: a number, or one for each tensor."""
+
+    def __init__(self, master, exp_avg, exp_avg_sq, grad, primary_bf16=None, *, weight_decay=0.0):
+        master = list(master)
+        count = len(master)
+        lists = [list(x) for x in (exp_avg, exp_avg_sq, grad)]
+        primary = [None] * count if primary_bf16 is None else list(primary_bf16)
+        decay = ([weight_decay] * count if isinstance(weight_decay, (int, float))
+                 else list(weight_decay))
+        if any(len(x) != count for x in (*lists, primary, decay)):
+            raise ValueError("one moment, gradient, copy and decay for each of the %d tensors"
+                             % count)
+        small = count > 0 and isinstance(lists[0][0], tuple)
+        grads = _BF16 if count and isinstance(lists[2][0], torch.Tensor) and \
+            _MATRIX_TYPES.get(lists[2][0].dtype) == 0 else _F32
+        rows = (AdamTensor * count)()
+        self._kept = []
+        for i, (p, m, v, g, out, wd) in enumerate(zip(master, *lists, primary, decay)):
+            n = _dev(p, _DTYPES[_F32], "master[%d]" % i).numel()
+            scales = [None, None]
+            if small:
+                m, scales[0] = _state8(m, torch.int8, "exp_avg[%d]" % i)
+                v, scales[1] = _state8(v, torch.uint8, "exp_avg_sq[%d]" % i)
+            else:
+                _dev(m, _DTYPES[_F32], "exp_avg[%d]" % i)
+                _dev(v, _DTYPES[_F32], "exp_avg_sq[%d]" % i)
+            _dev(g, _DTYPES[grads], "grad[%d]" % i)
+            if out is not None:
+                _dev(out, _DTYPES[_BF16], "primary_bf16[%d]" % i)
+            held = (p, m, v, *scales, g, out)
+            if any(t is not None and t.numel() != n for t in (m, v, g, out)):
+                raise ValueError("tensor %d: master has %d elements, another of its arrays has not"
+                                 % (i, n))
+            rows[i] = AdamTensor(*[None if t is None else t.data_ptr() for t in held], n, wd)
+            self._kept.append(held)
+        size = _lib.zpp_adam_tensors_table_bytes(count)
+        host = torch.zeros(size, dtype=torch.uint8)
+        self._list = AdamTable()
+        _check(_lib.zpp_adam_tensors_table(
+            rows, count, 2 if small else 1, 0 if grads == _BF16 else 1, host.data_ptr(), size,
+            ctypes.byref(self._list)), "zpp_adam_tensors_table")
+        self.device = _device()
+        self._table = host.cuda() if count else None
+        if count:
+            # the copy has to be there for steps on any stream
+            torch.cuda.current_stream().synchronize()
+            self._list.table = self._table.data_ptr()
+        self.address = ctypes.addressof(self._list)
+
+
+def adam_tensors_step(tensors, *, lr, beta1, beta2, eps, step, adamw=True, stream=None,
+                      wait_before=None, done_after=None):
+    """zpp_adam_tensors_step: one step of the tensors of an `AdamTensors`, each with
+    its own weight decay."""
+    if not isinstance(tensors, AdamTensors):
+        raise TypeError("tensors must be AdamTensors")
+    where = _where("adam_tensors_step", stream, wait_before, done_after)
+    if tensors.device != where[1]:
+        raise ValueError("tensors are on cuda:%d, not on the current device cuda:%d"
+                         % (tensors.device, where[1]))
+    st = _marshal.adam_tensors_step(*where, tensors.address, lr, beta1, beta2, eps, step, adamw)
+    if st is None:
+        hp = AdamHParams(lr, beta1, beta2, eps, 0.0, 1 if adamw else 0, int(step))
+        st = _lib.zpp_adam_tensors_step(tensors.address, ctypes.byref(hp), *where[2:])
+    _check(st, "zpp_adam_tensors_step")
+
+
+def _moment(state, name):
+    """Which moment a state in 8 bits is, by its codes' type, and its parts."""
+    codes = state[0] if isinstance(state, tuple) and len(state) == 2 else None
+    first = isinstance(codes, torch.Tensor) and codes.dtype == torch.int8
+    return (1 if first else 2, *_state8(state, torch.int8 if first else torch.uint8, name))
+
+
+def adam_state_save(x, state, *, stream=None, wait_before=None, done_after=None):
+    """zpp_adam_state_save: fp32 moments x into ``state`` = (codes, scales), whose codes
+    are int8 for the first moment and uint8 for the second."""
+    moment, codes, scales = _moment(state, "state")
+    n = codes.numel()
+    p, = _addresses(("x",), "x holds fewer elements than the state", x, _F32, n)
+    st = _lib.zpp_adam_state_save(p, n, moment, codes.data_ptr(), scales.data_ptr(),
+                                  stream_handle(stream), _event_handle(wait_before),
+                                  _event_handle(done_after))
+    _check(st, "zpp_adam_state_save")
+
+
+def adam_state_load(state, out, *, stream=None, wait_before=None, done_after=None):
+    """zpp_adam_state_load: the moments that ``state`` = (codes, scales) holds, in fp32."""
+    moment, codes, scales = _moment(state, "state")
+    n = codes.numel()
+    p, = _addresses(("out",), "out holds fewer elements than the state", out, _F32, n)
+    st = _lib.zpp_adam_state_load(codes.data_ptr(), scales.data_ptr(), n, moment, p,
+                                  stream_handle(stream), _event_handle(wait_before),
+                                  _event_handle(done_after))
+    _check(st, "zpp_adam_state_load")
 
 
 # --------------------------------------------------------------------------
