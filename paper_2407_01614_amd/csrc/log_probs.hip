@@ -8,6 +8,16 @@
 //     lse = r + ln s;  entropy = ln s - w / s
 // r starts at the lowest finite number, so that masked elements add e^-Inf = 0; a
 // row of nothing else ends with s = 0.  Inf or NaN make s NaN.
+//
+// The exponential of the hardware is 2^t and a quarter as fast as an fma, so that a
+// row costs about as long as its way from HBM.  The lanes therefore work in powers
+// of two: with c = log2 e in fp32 and a reference k = r c, rounded, 2^(x c - k) is
+// one fma, which rounds once, and the exponential; k itself is what the sums are
+// relative to, so its rounding loses nothing.  Numbers whose products with c leave
+// the range end in a sum that is 0, Inf or NaN, and then, as for a row that is masked
+// throughout, the row is summed again from the differences x - r.
+#include <type_traits>
+
 #include "zpp_act8.h"
 #include "zpp_token.h"
 
@@ -29,22 +39,28 @@ struct Sums {
 };
 __device__ __forceinline__ Sums no_sums() { return {kLowest, 0.0f, 0.0f}; }
 
-// Both as one.
+// Relative to another reference; BINARY: references and w in powers of two.
+template <bool BINARY>
 __device__ __forceinline__ Sums joined(const Sums &a, float r) {
-    const float d = __builtin_fmaxf(a.r - r, kFar), f = exp_of(d);
+    const float d = __builtin_fmaxf(a.r - r, kFar);
+    const float f = BINARY ? __builtin_amdgcn_exp2f(d) : exp_of(d);
     return {r, a.s * f, __builtin_fmaf(d, a.s, a.w) * f};
 }
+template <bool BINARY>
 __device__ __forceinline__ Sums join2(const Sums &a, const Sums &b) {
     const float r = __builtin_fmaxf(a.r, b.r);
-    const Sums x = joined(a, r), y = joined(b, r);
+    const Sums x = joined<BINARY>(a, r), y = joined<BINARY>(b, r);
     return {r, x.s + y.s, x.w + y.w};
 }
 
-__device__ __forceinline__ float max_wave(float x) {
+__device__ __forceinline__ float max16(float x) {
     x = __builtin_fmaxf(x, dpp<kSwap1>(x));
     x = __builtin_fmaxf(x, dpp<kSwap2>(x));
     x = __builtin_fmaxf(x, dpp<kMirror8>(x));
-    x = __builtin_fmaxf(x, dpp<kMirror16>(x));
+    return __builtin_fmaxf(x, dpp<kMirror16>(x));
+}
+__device__ __forceinline__ float max_wave(float x) {
+    x = max16(x);
     return __builtin_fmaxf(__builtin_fmaxf(lane_value(x, 0), lane_value(x, 16)),
                            __builtin_fmaxf(lane_value(x, 32), lane_value(x, 48)));
 }
@@ -52,84 +68,167 @@ __device__ __forceinline__ float sum_wave(float x) {
     x = sum16(x);
     return (lane_value(x, 0) + lane_value(x, 16)) + (lane_value(x, 32) + lane_value(x, 48));
 }
+template <bool BINARY>
 __device__ __forceinline__ Sums join_wave(const Sums &a) {
-    const Sums x = joined(a, max_wave(a.r));
+    const Sums x = joined<BINARY>(a, max_wave(a.r));
     return {x.r, sum_wave(x.s), sum_wave(x.w)};
 }
 
-// The workgroup's, in all lanes; `shared` holds one for each wave.
-template <uint32_t THREADS>
-__device__ __forceinline__ Sums join_workgroup(Sums a, Sums *shared) {
-    a = join_wave(a);
+// Those of the THREADS lanes that share a row: 16 of a wave, a wave, or a workgroup, for
+// which `shared` holds one for each wave.
+template <uint32_t THREADS, bool BINARY>
+__device__ __forceinline__ Sums join_lanes(Sums a, Sums *shared) {
+    if constexpr (THREADS == 16) {
+        a = joined<BINARY>(a, max16(a.r));
+        return {a.r, sum16(a.s), sum16(a.w)};
+    }
+    a = join_wave<BINARY>(a);
     if constexpr (THREADS > 64) {
+        constexpr uint32_t kWaves = THREADS / 64;
+        static_assert(kWaves == 4 || kWaves == 8 || kWaves == 16);
         if ((threadIdx.x & 63) == 0)
             shared[threadIdx.x / 64] = a;
         __syncthreads();
-        a = shared[0];
-#pragma unroll
-        for (uint32_t w = 1; w < THREADS / 64; ++w)
-            a = join2(a, shared[w]);
+        // a wave's lanes hold all waves' sums and join them as a wave does its own
+        a = shared[threadIdx.x % kWaves];
+        float r = __builtin_fmaxf(a.r, dpp<kSwap1>(a.r));
+        r = __builtin_fmaxf(r, dpp<kSwap2>(r));
+        if constexpr (kWaves > 4)
+            r = __builtin_fmaxf(r, dpp<kMirror8>(r));
+        if constexpr (kWaves > 8)
+            r = __builtin_fmaxf(r, dpp<kMirror16>(r));
+        a = joined<BINARY>(a, lane_value(r, 0));
+        a.s += dpp<kSwap1>(a.s);
+        a.w += dpp<kSwap1>(a.w);
+        a.s += dpp<kSwap2>(a.s);
+        a.w += dpp<kSwap2>(a.w);
+        if constexpr (kWaves > 4) {
+            a.s += dpp<kMirror8>(a.s);
+            a.w += dpp<kMirror8>(a.w);
+        }
+        if constexpr (kWaves > 8) {
+            a.s += dpp<kMirror16>(a.s);
+            a.w += dpp<kMirror16>(a.w);
+        }
+        a = {a.r, lane_value(a.s, 0), lane_value(a.w, 0)};
     }
     return a;
 }
 
-// A row's elements as chunks of eight: chunk i of a row begins at column
-// column(i), its second half follows at once (bf16) or 32 columns on (fp32, where
-// eight lanes take whole lines so).
-template <int TYPE>
-constexpr uint32_t kApart = TYPE == kBf16 ? 4 : 32;
-template <int TYPE>
-__device__ __forceinline__ uint32_t column(uint32_t i) {
-    return TYPE == kBf16 ? i * 8 : (i / 8) * 64 + (i % 8) * 4;
-}
-// Elements from a chunk's column to the row's end, as load_chunk takes them.
-template <int TYPE>
-__device__ __forceinline__ uint32_t valid_of(uint32_t col, uint32_t end) {
-    const uint32_t n = col < end ? end - col : 0;
-    return n < kApart<TYPE> + 4 ? n : kApart<TYPE> + 4;
+// Did the sums in powers of two hold?
+__device__ __forceinline__ bool held(const Sums &a) { return a.s > 0.0f && a.s < infinity(); }
+
+// Sums in powers of two as natural ones: r the fp32 nearest to k / c, and what that
+// is off by taken into s and w.
+__device__ __forceinline__ Sums natural(const Sums &a) {
+    const double r = (double)a.r * (1.0 / (double)kLog2e);
+    const float near = (float)r, d = (float)(r - (double)near), f = 1.0f + d;
+    return {near, a.s * f, __builtin_fmaf(a.w, 1.0f / kLog2e, d * a.s) * f};
 }
 
-// The chunk as loaded, -Inf past the row's end.
+// A row is read in pieces of 16 bytes, eight bf16 or four fp32, neighbouring lanes
+// neighbouring pieces; a lane's pieces are as far apart as the lanes that share the row
+// reach.  `row` is a base that they share, beside which a column takes 32 bits.
 template <int TYPE>
-__device__ __forceinline__ Chunk<TYPE> load_valid(const Mat &m, size_t off, uint32_t valid) {
-    constexpr uint32_t kWhole = kApart<TYPE> + 4;
-    Chunk<TYPE> c;
-    if constexpr (TYPE == kBf16)
-        c.w = u32x4{0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u};
-    else
-        c.lo = c.hi = f32x4{-infinity(), -infinity(), -infinity(), -infinity()};
-    if (valid >= kWhole) {
-        c = load_chunk<TYPE, false, kApart<TYPE>>(m, off, valid, 0);
-    } else if (valid) {
-        const Chunk<TYPE> some = load_chunk<TYPE, true, kApart<TYPE>>(m, off, valid, 0);
+constexpr uint32_t kPer = TYPE == kBf16 ? 8 : 4;
+template <int TYPE>
+constexpr uint32_t kSize = TYPE == kBf16 ? 2 : 4;
+
+template <int TYPE>
+__device__ __forceinline__ char *row_of(const Mat &m, size_t row) {
+    return reinterpret_cast<char *>(m.data) + row * m.stride * kSize<TYPE>;
+}
+
+template <int TYPE>
+__device__ __forceinline__ void values_of(const u32x4 &w, float (&x)[kPer<TYPE>]) {
 #pragma unroll
-        for (uint32_t e = 0; e < 8; ++e)
-            if (place_at<kApart<TYPE>>(e) < valid) {
-                if constexpr (TYPE == kBf16) {
-                    const uint32_t half = 0xFFFFu << (16 * (e % 2));
-                    c.w[e / 2] = (c.w[e / 2] & ~half) | (some.w[e / 2] & half);
-                } else if (e < 4) {
-                    c.lo[e] = some.lo[e];
-                } else {
-                    c.hi[e - 4] = some.hi[e - 4];
-                }
-            }
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (TYPE == kBf16) {
+            x[2 * i] = bf16_lo(w[i]);
+            x[2 * i + 1] = bf16_hi(w[i]);
+        } else {
+            x[i] = __uint_as_float(w[i]);
+        }
     }
-    return c;
+}
+template <int TYPE>
+__device__ __forceinline__ u32x4 piece_of(const float (&x)[kPer<TYPE>]) {
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (TYPE == kBf16)
+            w[i] = bf16_pair(x[2 * i], x[2 * i + 1]);
+        else
+            w[i] = __float_as_uint(x[i]);
+    }
+    return w;
 }
 
-__device__ __forceinline__ float max_of(const float (&x)[8]) {
-    return __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(x[0], x[1]), __builtin_fmaxf(x[2], x[3])),
-                           __builtin_fmaxf(__builtin_fmaxf(x[4], x[5]), __builtin_fmaxf(x[6], x[7])));
+// The first `skip` elements as -Inf.
+template <int TYPE>
+__device__ __forceinline__ void mask(u32x4 &w, uint32_t skip) {
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) {
+        if constexpr (TYPE == kBf16) {
+            if (2 * i < skip)
+                w[i] = (w[i] & 0xFFFF0000u) | 0xFF80u;
+            if (2 * i + 1 < skip)
+                w[i] = (w[i] & 0xFFFFu) | 0xFF800000u;
+        } else if (i < skip) {
+            w[i] = 0xFF800000u;
+        }
+    }
 }
 
-// Eight elements added to the sums, none above a.r.
-template <bool ENTROPY>
-__device__ __forceinline__ void add(Sums &a, const float (&x)[8]) {
+// Where the piece of column `col` lies: the row's last piece is its last 16 bytes,
+// whatever its column, and all loads are whole.  (Rows of less have their own kernel.)
+template <int TYPE>
+__device__ __forceinline__ uint32_t place_of(uint32_t col, uint32_t vocab) {
+    return col < vocab - kPer<TYPE> ? col : vocab - kPer<TYPE>;
+}
+
+// The piece of column `col` of a row or, to `end`, a slice of it: -Inf in the place of
+// what is another piece's or past the end.
+template <int TYPE>
+__device__ __forceinline__ u32x4 load_piece(const char *row, uint32_t col, uint32_t vocab) {
+    return ld_nt_at<u32x4, kSize<TYPE>>(row + place_of<TYPE>(col, vocab) * (size_t)kSize<TYPE>);
+}
+template <int TYPE>
+__device__ __forceinline__ void mask_end(u32x4 &w, uint32_t col, uint32_t end, uint32_t vocab) {
+    if (col + kPer<TYPE> > end)
+        mask<TYPE>(w, col < end ? col - place_of<TYPE>(col, vocab) : kPer<TYPE>);
+}
+
+// Keeps what is made of a piece behind this point: values made once for all passes over
+// the pieces would take twice their registers.
+__device__ __forceinline__ void hold(u32x4 &w) {
+    asm volatile("" : "+v"(w.x), "+v"(w.y), "+v"(w.z), "+v"(w.w));
+}
+__device__ __forceinline__ void hold(uint32_t &x) { asm volatile("" : "+v"(x)); }
+
+template <int N>
+__device__ __forceinline__ float max_of(const float (&x)[N]) {
+    float m = __builtin_fmaxf(__builtin_fmaxf(x[0], x[1]), __builtin_fmaxf(x[2], x[3]));
+    if constexpr (N == 8)
+        m = __builtin_fmaxf(m, __builtin_fmaxf(__builtin_fmaxf(x[4], x[5]),
+                                               __builtin_fmaxf(x[6], x[7])));
+    return m;
+}
+
+// The reference of elements up to r.
+template <bool BINARY>
+__device__ __forceinline__ float reference(float r) {
+    return BINARY ? __builtin_fmaxf(r * kLog2e, kLowest) : r;
+}
+
+// A piece's elements added to the sums, none above their reference.
+template <bool ENTROPY, bool BINARY, int N>
+__device__ __forceinline__ void add(Sums &a, const float (&x)[N]) {
     float s = 0.0f, w = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float d = x[e] - a.r, p = exp_of(d);
+    for (int e = 0; e < N; ++e) {
+        const float d = BINARY ? __builtin_fmaf(x[e], kLog2e, -a.r) : x[e] - a.r;
+        const float p = BINARY ? __builtin_amdgcn_exp2f(d) : exp_of(d);
         s += p;
         if (ENTROPY)
             w = __builtin_fmaf(p, __builtin_fmaxf(d, kFar), w);
@@ -147,16 +246,10 @@ struct RowArgs {
     uint32_t splits, slice;  // slices of a row, and their columns
     Sums *partials;          // [row][split]
     unsigned long long *keys;  // [row][split][top]
-    uint32_t top;
+    uint32_t top, group;  // group: lanes of a group of the selection
     int32_t *top_ids;
     float *top_log_probs;
 };
-
-template <int TYPE>
-__device__ __forceinline__ float element(const Mat &m, size_t off) {
-    return TYPE == kBf16 ? bf16_lo(reinterpret_cast<const uint16_t *>(m.data)[off])
-                         : reinterpret_cast<const float *>(m.data)[off];
-}
 
 // x - lse with lse = r + ln s, in 64 bits: where the token is nearly certain, the
 // difference is far smaller than its terms.
@@ -173,57 +266,105 @@ __device__ __forceinline__ void store_sums(const RowArgs &a, size_t row, const S
     if (a.entropies)
         a.entropies[row] = t.s == 0.0f ? 0.0f : ln - t.w / t.s;
 }
+// A row's target and its logit, read by one lane before the row is.
+struct Target {
+    int64_t at;
+    float x;
+};
 template <int TYPE>
-__device__ __forceinline__ void finish(const RowArgs &a, size_t row, const Sums &t, float ln) {
-    const int64_t target = a.targets[row];
+__device__ __forceinline__ Target target_of(const RowArgs &a, size_t row) {
+    Target t{a.targets[row], 0.0f};
+    if (t.at >= 0 && t.at < (int64_t)a.vocab) {
+        const char *p = row_of<TYPE>(a.x, row) + (size_t)t.at * kSize<TYPE>;
+        t.x = TYPE == kBf16 ? bf16_lo(*reinterpret_cast<const uint16_t *>(p))
+                            : *reinterpret_cast<const float *>(p);
+    }
+    return t;
+}
+__device__ __forceinline__ void finish(const RowArgs &a, size_t row, const Target &target,
+                                       const Sums &t, float ln) {
     float lp = 0.0f;
-    if (target >= (int64_t)a.vocab)
+    if (target.at >= (int64_t)a.vocab)
         lp = not_a_number();
-    else if (target >= 0)
-        lp = log_prob(element<TYPE>(a.x, row * a.x.stride + (size_t)target), t, ln);
+    else if (target.at >= 0)
+        lp = log_prob(target.x, t, ln);
     a.log_probs[row] = lp;
     store_sums(a, row, t, ln);
 }
 
-// THREADS lanes a row or slice: a wave, four rows to a workgroup, or the workgroup.
-constexpr uint32_t kBatch = 4;  // chunks of a lane in flight
-template <int TYPE, uint32_t THREADS, bool ENTROPY>
-__global__ __launch_bounds__(kThreads) void forward_kernel(RowArgs a) {
-    __shared__ Sums shared[kThreads / 64];
+// A lane's sums of columns begin .. end, one of THREADS that share them; BATCH elements in
+// flight.
+constexpr uint32_t kBatch = 32;
+template <int TYPE, uint32_t THREADS, uint32_t BATCH, bool ENTROPY, bool BINARY>
+__device__ __forceinline__ Sums sums_of(const char *row, uint32_t begin, uint32_t end,
+                                        uint32_t vocab, uint32_t lane) {
+    constexpr uint32_t kPieces = BATCH / kPer<TYPE>;
+    Sums t = no_sums();
+    float top = kLowest;
+    for (uint32_t i = begin; i < end; i += BATCH * THREADS) {
+        u32x4 c[kPieces];
+#pragma unroll
+        for (uint32_t b = 0; b < kPieces; ++b)
+            c[b] = load_piece<TYPE>(row, i + (b * THREADS + lane) * kPer<TYPE>, vocab);
+        float x[kPieces][kPer<TYPE>];
+#pragma unroll
+        for (uint32_t b = 0; b < kPieces; ++b) {
+            mask_end<TYPE>(c[b], i + (b * THREADS + lane) * kPer<TYPE>, end, vocab);
+            values_of<TYPE>(c[b], x[b]);
+            top = __builtin_fmaxf(top, max_of(x[b]));
+        }
+        t = joined<BINARY>(t, reference<BINARY>(top));
+#pragma unroll
+        for (uint32_t b = 0; b < kPieces; ++b)
+            add<ENTROPY, BINARY>(t, x[b]);
+    }
+    return t;
+}
+
+// Threads of a workgroup whose rows are shared by so many each, and which of a workgroup's
+// rows a lane is on (the same for a wave, which the compiler cannot know).
+constexpr uint32_t group_of(uint32_t threads) { return threads < kThreads ? kThreads : threads; }
+template <uint32_t THREADS>
+__device__ __forceinline__ uint32_t row_in_group() {
+    if constexpr (THREADS >= kThreads)
+        return 0;
+    const uint32_t r = threadIdx.x / THREADS;
+    return THREADS < 64 ? r : __builtin_amdgcn_readfirstlane(r);
+}
+
+// THREADS lanes a row or slice: 16 or 64 of a workgroup of 256, or the workgroup.
+template <int TYPE, uint32_t THREADS, uint32_t BATCH, bool ENTROPY>
+__global__ __launch_bounds__(group_of(THREADS)) void forward_kernel(RowArgs a) {
+    __shared__ Sums shared[2][group_of(THREADS) / 64];
     const uint32_t lane = threadIdx.x % THREADS;
-    const size_t task = (size_t)blockIdx.x * (kThreads / THREADS) + threadIdx.x / THREADS;
-    const size_t row = a.base + task / a.splits;
-    const uint32_t split = (uint32_t)(task % a.splits);
-    if (THREADS == 64 && row >= a.rows)
-        return;
+    size_t row;
+    uint32_t split = 0;
+    if constexpr (THREADS < kThreads) {
+        row = a.base + (size_t)blockIdx.x * (kThreads / THREADS) + row_in_group<THREADS>();
+        if (row >= a.rows)
+            return;
+    } else {
+        row = a.base + blockIdx.x / a.splits;
+        split = blockIdx.x % a.splits;
+    }
     const uint32_t begin = split * a.slice;
     const uint32_t end = a.vocab - begin < a.slice ? a.vocab : begin + a.slice;
-    const size_t off = row * a.x.stride;
-    Sums t = no_sums();
-    for (uint32_t i = lane; begin + column<TYPE>(i - lane) < end; i += kBatch * THREADS) {
-        Chunk<TYPE> c[kBatch];
-#pragma unroll
-        for (uint32_t b = 0; b < kBatch; ++b) {
-            const uint32_t col = begin + column<TYPE>(i + b * THREADS);
-            c[b] = load_valid<TYPE>(a.x, off + col, valid_of<TYPE>(col, end));
-        }
-        float x[kBatch][8], r = t.r;
-#pragma unroll
-        for (uint32_t b = 0; b < kBatch; ++b) {
-            chunk_values(c[b], x[b]);
-            r = __builtin_fmaxf(r, max_of(x[b]));
-        }
-        t = joined(t, r);
-#pragma unroll
-        for (uint32_t b = 0; b < kBatch; ++b)
-            add<ENTROPY>(t, x[b]);
-    }
-    t = join_workgroup<THREADS>(t, shared);
+    const char *x = row_of<TYPE>(a.x, row);
+    Target target{};
+    if (lane == 0 && a.splits == 1)
+        target = target_of<TYPE>(a, row);
+    Sums t = join_lanes<THREADS, true>(
+        sums_of<TYPE, THREADS, BATCH, ENTROPY, true>(x, begin, end, a.vocab, lane), shared[0]);
+    if (held(t))
+        t = natural(t);
+    else
+        t = join_lanes<THREADS, false>(
+            sums_of<TYPE, THREADS, BATCH, ENTROPY, false>(x, begin, end, a.vocab, lane), shared[1]);
     if (lane == 0) {
         if (a.splits > 1)
             a.partials[row * a.splits + split] = t;
         else
-            finish<TYPE>(a, row, t, logf(t.s));
+            finish(a, row, target, t, logf(t.s));
     }
 }
 
@@ -231,28 +372,31 @@ __global__ __launch_bounds__(kThreads) void forward_kernel(RowArgs a) {
 __device__ __forceinline__ Sums join_slices(const RowArgs &a, size_t row) {
     Sums t = no_sums();
     for (uint32_t i = threadIdx.x & 63; i < a.splits; i += 64)
-        t = join2(t, a.partials[row * a.splits + i]);
-    return join_wave(t);
+        t = join2<false>(t, a.partials[row * a.splits + i]);
+    return join_wave<false>(t);
 }
 
 template <int TYPE>
 __global__ __launch_bounds__(64) void join_kernel(RowArgs a) {
     const size_t row = a.base + blockIdx.x;
+    Target target{};
+    if (threadIdx.x == 0)
+        target = target_of<TYPE>(a, row);
     const Sums t = join_slices(a, row);
     if (threadIdx.x == 0)
-        finish<TYPE>(a, row, t, logf(t.s));
+        finish(a, row, target, t, logf(t.s));
 }
 
 // --------------------------------------------------------------------------
 // The most probable tokens.  An element is one 64-bit key: its value as an integer
 // of the same order, and below it its column, inverted, so that of equals the lower
-// comes first and no two keys are alike.  Every lane finds its largest key; 128
-// groups of two lanes put theirs into LDS, and the k-th largest of these is a
-// threshold that at least k elements reach, few more among them: all are in the k
-// groups whose largest key reaches it.  They are listed, and each one's rank counted.
+// comes first and no two keys are alike.  Every lane finds its largest key; groups of
+// 1 to 8 lanes put theirs into LDS, and the k-th largest of these is a threshold that
+// at least k elements reach, and few more: they all are in the k groups whose largest
+// key reaches it.  They are listed, and each one's rank is counted.
 // --------------------------------------------------------------------------
 typedef unsigned long long Key;
-constexpr uint32_t kGroupsOfTop = kThreads / 2;
+typedef Key KeyPair __attribute__((ext_vector_type(2)));
 constexpr uint32_t kTopPerLane = 32;  // keys of a lane at most
 
 __device__ __forceinline__ Key key_of(float x, uint32_t col) {
@@ -266,33 +410,69 @@ __device__ __forceinline__ float value_of(Key k) {
 }
 __device__ __forceinline__ uint32_t column_of(Key k) { return 0xFFFFFFFFu - (uint32_t)k; }
 
-// The workgroup's `top` largest keys.  each(f) calls f with every key of the lane,
-// at most kTopPerLane; write(rank, key) stores one.  Returns how many there were, if
-// fewer than `top`.  list: 2 kTopPerLane top keys of LDS.
+template <int CTRL>
+__device__ __forceinline__ Key max_beside(Key k) {
+    const Key other = (Key)dpp<CTRL>((uint32_t)(k >> 32)) << 32 | dpp<CTRL>((uint32_t)k);
+    return k > other ? k : other;
+}
+
+// Lanes of a group: the most that leave two groups with keys for each one asked for, of
+// `lanes` that have any.
+inline uint32_t group_lanes(uint32_t lanes, uint32_t top) {
+    uint32_t n = 8;
+    while (n > 1 && lanes / n < 2 * top)
+        n /= 2;
+    return n;
+}
+// The list's length: all keys of `top` groups, and to a multiple of the ranks' loop.
+constexpr uint32_t kRankStep = 8;
+inline uint32_t list_keys(uint32_t per_lane, uint32_t group, uint32_t top) {
+    return (per_lane * group * top + kRankStep - 1) / kRankStep * kRankStep + kRankStep;
+}
+
+// The workgroup's `top` largest keys.  each(f) calls f with every key of the lane;
+// write(rank, key) stores one.  Returns how many were listed, which is less than `top`
+// only where there are no more.  `group` as from group_lanes.
 template <class Each, class Write>
-__device__ __forceinline__ uint32_t select_top(uint32_t top, Key *list, Each &&each,
-                                               Write &&write) {
-    __shared__ Key groups[kGroupsOfTop];
+__device__ __forceinline__ uint32_t select_top(uint32_t top, uint32_t group, Key *list,
+                                               Each &&each, Write &&write) {
+    __shared__ __attribute__((aligned(16))) Key groups[kThreads];
     __shared__ Key threshold;
     __shared__ uint32_t listed;
     Key best = 0;  // below every key
     each([&](Key k) { best = k > best ? k : best; });
-    const Key beside = (Key)dpp<kSwap1>((uint32_t)(best >> 32)) << 32 | dpp<kSwap1>((uint32_t)best);
-    const Key group = best > beside ? best : beside;
-    if (threadIdx.x % 2 == 0)
-        groups[threadIdx.x / 2] = group;
+    Key most = best;
+    if (group > 1)
+        most = max_beside<kSwap1>(most);
+    if (group > 2)
+        most = max_beside<kSwap2>(most);
+    if (group > 4)
+        most = max_beside<kMirror8>(most);
+    const uint32_t part = threadIdx.x % group;
+    if (part == 0)
+        groups[threadIdx.x / group] = most;
     if (threadIdx.x == 0) {
         threshold = 1;  // fewer than `top` groups with a key: all their keys
         listed = 0;
     }
     __syncthreads();
+    // each lane of a group compares with its share of all groups
     uint32_t above = 0;
-#pragma unroll 8
-    for (uint32_t j = 0; j < kGroupsOfTop / 2; ++j)
-        above += groups[(threadIdx.x % 2) * (kGroupsOfTop / 2) + j] > group;
-    above += dpp<kSwap1>(above);
-    if (threadIdx.x % 2 == 0 && group && above == top - 1)
-        threshold = group;
+    const uint32_t share = kThreads / (group * group);
+    const KeyPair *beside = reinterpret_cast<const KeyPair *>(groups + part * share);
+#pragma unroll 4
+    for (uint32_t j = 0; j < share / 2; ++j) {
+        const KeyPair k = beside[j];
+        above += (k.x > most) + (k.y > most);
+    }
+    if (group > 1)
+        above += dpp<kSwap1>(above);
+    if (group > 2)
+        above += dpp<kSwap2>(above);
+    if (group > 4)
+        above += dpp<kMirror8>(above);
+    if (part == 0 && most && above == top - 1)
+        threshold = most;
     __syncthreads();
     const Key least = threshold;
     if (best >= least)
@@ -302,76 +482,105 @@ __device__ __forceinline__ uint32_t select_top(uint32_t top, Key *list, Each &&e
         });
     __syncthreads();
     const uint32_t n = listed;
+    if (threadIdx.x < kRankStep)
+        list[n + threadIdx.x] = 0;
+    __syncthreads();
     for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
         const Key k = list[i];
         uint32_t rank = 0;
-        for (uint32_t j = 0; j < n; ++j)
-            rank += list[j] > k;
+        for (uint32_t j = 0; j < n; j += kRankStep) {
+#pragma unroll
+            for (uint32_t e = 0; e < kRankStep; e += 2) {
+                const KeyPair other = *reinterpret_cast<const KeyPair *>(list + j + e);
+                rank += (other.x > k) + (other.y > k);
+            }
+        }
         if (rank < top)
             write(rank, k);
     }
     return n;
 }
 
-// A slice of a row, C chunks a lane: sums and its most probable tokens.
-template <int TYPE, uint32_t C>
+// A slice of a row, E elements a lane: sums and its most probable tokens; the row's
+// results where it is the only one.
+template <int TYPE, uint32_t E>
 __global__ __launch_bounds__(kThreads) void top_kernel(RowArgs a) {
-    extern __shared__ Key list[];
+    extern __shared__ __attribute__((aligned(16))) Key list[];
     __shared__ Sums shared[kThreads / 64];
+    constexpr uint32_t kPieces = E / kPer<TYPE>;
     const size_t row = a.base + blockIdx.x / a.splits;
     const uint32_t split = blockIdx.x % a.splits, begin = split * a.slice;
     const uint32_t end = a.vocab - begin < a.slice ? a.vocab : begin + a.slice;
-    const size_t off = row * a.x.stride;
-    Chunk<TYPE> c[C];
-    uint32_t valid[C];
+    const char *p = row_of<TYPE>(a.x, row);
+    Target target{};
+    if (threadIdx.x == 0 && a.splits == 1)
+        target = target_of<TYPE>(a, row);
+    u32x4 c[kPieces];
 #pragma unroll
-    for (uint32_t b = 0; b < C; ++b) {
-        const uint32_t col = begin + column<TYPE>(threadIdx.x + b * kThreads);
-        valid[b] = valid_of<TYPE>(col, end);
-        c[b] = load_valid<TYPE>(a.x, off + col, valid[b]);
-    }
-    float x[C][8];
+    for (uint32_t b = 0; b < kPieces; ++b)
+        c[b] = load_piece<TYPE>(p, begin + (b * kThreads + threadIdx.x) * kPer<TYPE>, a.vocab);
+    float x[kPieces][kPer<TYPE>];
     Sums t = no_sums();
 #pragma unroll
-    for (uint32_t b = 0; b < C; ++b) {
-        chunk_values(c[b], x[b]);
+    for (uint32_t b = 0; b < kPieces; ++b) {
+        mask_end<TYPE>(c[b], begin + (b * kThreads + threadIdx.x) * kPer<TYPE>, end, a.vocab);
+        values_of<TYPE>(c[b], x[b]);
         t.r = __builtin_fmaxf(t.r, max_of(x[b]));
     }
 #pragma unroll
-    for (uint32_t b = 0; b < C; ++b)
-        add<true>(t, x[b]);
-    t = join_workgroup<kThreads>(t, shared);
-    if (threadIdx.x == 0)
-        a.partials[row * a.splits + split] = t;
-    Key *out = a.keys + (row * a.splits + split) * a.top;
+    for (uint32_t b = 0; b < kPieces; ++b)
+        add<true, false>(t, x[b]);
+    t = join_lanes<kThreads, false>(t, shared);
+    float ln = 0.0f;
+    if (a.splits == 1)
+        ln = logf(t.s);
+    if (threadIdx.x == 0) {
+        if (a.splits == 1)
+            finish(a, row, target, t, ln);
+        else
+            a.partials[row * a.splits + split] = t;
+    }
     const auto each = [&](auto &&f) {
 #pragma unroll
-        for (uint32_t b = 0; b < C; ++b)
+        for (uint32_t b = 0; b < kPieces; ++b) {
+            const uint32_t col = begin + (b * kThreads + threadIdx.x) * kPer<TYPE>;
+            const uint32_t at = place_of<TYPE>(col, a.vocab);
 #pragma unroll
-            for (uint32_t e = 0; e < 8; ++e)
-                if (place_at<kApart<TYPE>>(e) < valid[b])
-                    f(key_of(x[b][e], begin + column<TYPE>(threadIdx.x + b * kThreads) +
-                                          place_at<kApart<TYPE>>(e)));
+            for (uint32_t e = 0; e < kPer<TYPE>; ++e)
+                if (col < end && at + e >= col)
+                    f(key_of(x[b][e], at + e));
+        }
     };
-    const uint32_t n =
-        select_top(a.top, list, each, [&](uint32_t rank, Key k) { out[rank] = k; });
-    for (uint32_t i = n + threadIdx.x; i < a.top; i += kThreads)
-        out[i] = 0;
+    Key *out = a.keys + (row * a.splits + split) * a.top;
+    const uint32_t n = select_top(a.top, a.group, list, each, [&](uint32_t rank, Key k) {
+        if (a.splits == 1) {
+            a.top_ids[row * a.top + rank] = (int32_t)column_of(k);
+            a.top_log_probs[row * a.top + rank] = log_prob(value_of(k), t, ln);
+        } else {
+            out[rank] = k;
+        }
+    });
+    if (a.splits > 1)
+        for (uint32_t i = n + threadIdx.x; i < a.top; i += kThreads)
+            out[i] = 0;
 }
 
 // The slices joined: sums, and the most probable of the slices' most probable.
 template <int TYPE>
 __global__ __launch_bounds__(kThreads) void top_join_kernel(RowArgs a) {
-    extern __shared__ Key list[];
+    extern __shared__ __attribute__((aligned(16))) Key list[];
     const size_t row = a.base + blockIdx.x;
+    Target target{};
+    if (threadIdx.x == 0)
+        target = target_of<TYPE>(a, row);
     const Sums t = join_slices(a, row);
     const float ln = logf(t.s);
     if (threadIdx.x == 0)
-        finish<TYPE>(a, row, t, ln);
+        finish(a, row, target, t, ln);
     const Key *keys = a.keys + row * a.splits * a.top;
     const uint32_t n = a.splits * a.top;
     select_top(
-        a.top, list,
+        a.top, a.group, list,
         [&](auto &&f) {
             for (uint32_t i = threadIdx.x; i < n; i += kThreads)
                 f(keys[i]);
@@ -393,11 +602,14 @@ struct GradArgs {
     uint32_t vocab, per_row;  // waves of a row
 };
 
-// What a row's elements share: p = e^(x - r - ln), dx = p (c - h max(x - r, kFar)) with
-// c = h (ln - entropy) - g; g once more at the target's column.
+// What a row's elements share.  With p = e^(x - r) / s and d = x - r,
+//     dx = p (f - h max(d, kFar)),  f = h (ln s - entropy) - g
+// and g once more at the target's column.  In powers of two (binary): d = x c - k, f and
+// h divided by s, h by c as well.
 struct RowGrad {
-    float r, ln, c, h, g;
+    float r, ln, f, h, g;
     uint32_t target;
+    bool binary;
 };
 // No column, and not one past a row's end either.
 constexpr uint32_t kNoTarget = UINT32_MAX;
@@ -408,70 +620,140 @@ __device__ __forceinline__ RowGrad row_grad(float r, float ln, bool empty, float
     q.target = target >= 0 && target < (int64_t)vocab ? (uint32_t)target : kNoTarget;
     q.g = target < 0 ? 0.0f : target < (int64_t)vocab ? dlog_prob : not_a_number();
     q.r = r, q.ln = ln, q.h = h;
+    q.binary = false;
     if (empty) {
         // e^-Inf = 0: no element has a share, and none gets a gradient
         q.r = kLowest, q.ln = 0.0f, q.target = kNoTarget;
         q.h = 0.0f;
         q.g = q.g == q.g ? 0.0f : q.g;
     }
-    q.c = __builtin_fmaf(q.h, q.ln - (empty ? 0.0f : entropy), -q.g);
+    q.f = __builtin_fmaf(q.h, q.ln - (empty ? 0.0f : entropy), -q.g);
     return q;
 }
+// The same in powers of two, relative to k, `inv` the inverse of s there; d = (x c - k) / c
+// is `off` more than x - r.
+__device__ __forceinline__ void make_binary(RowGrad &q, float k, float inv, float off) {
+    q.f = __builtin_fmaf(q.h, off, q.f) * inv;
+    q.h *= inv * (1.0f / kLog2e);
+    q.r = k;
+    q.binary = true;
+}
 
-// Eight elements' gradients; found(x): with the target's logit, by the lane that has it.
-template <int TYPE, bool ENTROPY, class F>
-__device__ __forceinline__ Chunk<TYPE> grad_chunk(const RowGrad &q, const Chunk<TYPE> &chunk,
-                                                  uint32_t col, F &&found) {
-    float x[8];
-    chunk_values(chunk, x);
-    const bool near = q.target - col < kApart<TYPE> + 4;
-    if (near) {
+// A piece's gradients; `target`: its element that is the target's, or none (kNoTarget);
+// found(x): with that one's logit.
+template <int TYPE, bool ENTROPY, bool BINARY, class F>
+__device__ __forceinline__ u32x4 grad_piece(const RowGrad &q, const u32x4 &piece, uint32_t target,
+                                            F &&found) {
+    float x[kPer<TYPE>];
+    values_of<TYPE>(piece, x);
+    if (target < kPer<TYPE>) {
 #pragma unroll
-        for (uint32_t e = 0; e < 8; ++e)
-            if (q.target == col + place_at<kApart<TYPE>>(e))
+        for (uint32_t e = 0; e < kPer<TYPE>; ++e)
+            if (target == e)
                 found(x[e]);
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float d = x[e] - q.r, p = exp_of(d - q.ln);
-        float c = q.c;
+    for (uint32_t e = 0; e < kPer<TYPE>; ++e) {
+        const float d = BINARY ? __builtin_fmaf(x[e], kLog2e, -q.r) : x[e] - q.r;
+        const float p = BINARY ? __builtin_amdgcn_exp2f(d) : exp_of(d - q.ln);
+        float f = q.f;
         if (ENTROPY)
-            c = __builtin_fmaf(-q.h, __builtin_fmaxf(d, kFar), c);
-        x[e] = p * c;
+            f = __builtin_fmaf(-q.h, __builtin_fmaxf(d, kFar), f);
+        x[e] = p * f;
     }
-    if (near) {
+    if (target < kPer<TYPE>) {
 #pragma unroll
-        for (uint32_t e = 0; e < 8; ++e)
-            x[e] += q.target == col + place_at<kApart<TYPE>>(e) ? q.g : 0.0f;
+        for (uint32_t e = 0; e < kPer<TYPE>; ++e)
+            x[e] += target == e ? q.g : 0.0f;
     }
-    return make_chunk<TYPE>(x);
+    return piece_of<TYPE>(x);
 }
 
-// A wave takes kBatch chunks a lane of one row.
-template <int TYPE, bool ENTROPY>
+// Elements `from` .. `to` of a piece, whose first would lie at p.
+template <int TYPE>
+__device__ __forceinline__ void store_some(char *p, const u32x4 &w, uint32_t from, uint32_t to) {
+#pragma unroll
+    for (uint32_t e = 0; e < kPer<TYPE>; ++e)
+        if (e >= from && e < to) {
+            if constexpr (TYPE == kBf16)
+                reinterpret_cast<uint16_t *>(p)[e] = (uint16_t)(w[e / 2] >> (16 * (e % 2)));
+            else
+                reinterpret_cast<uint32_t *>(p)[e] = w[e];
+        }
+}
+
+// Sums of logits whose product with c rounds by less than a tenth: others take differences.
+constexpr float kOrdinary = 1e6f;
+
+// LANES of a wave, all or 16, take BATCH elements each of one row.
+template <int TYPE, uint32_t LANES, uint32_t BATCH, bool ENTROPY>
 __global__ __launch_bounds__(kThreads) void backward_kernel(GradArgs a) {
-    const size_t wave = (size_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
-    const size_t row = a.base + wave / a.per_row;
+    constexpr uint32_t kPieces = BATCH / kPer<TYPE>;
+    const size_t part = (size_t)blockIdx.x * (kThreads / LANES) + row_in_group<LANES>();
+    const size_t row = a.base + part / a.per_row;
     if (row >= a.rows)
         return;
-    const uint32_t first = (uint32_t)(wave % a.per_row) * 64 * kBatch + threadIdx.x % 64;
-    Chunk<TYPE> c[kBatch];
+    const uint32_t start = (uint32_t)(part % a.per_row) * LANES * BATCH;
+    const uint32_t first = start + threadIdx.x % LANES * kPer<TYPE>;
+    const char *x = row_of<TYPE>(a.x, row);
+    char *dx = row_of<TYPE>(a.dx, row);
+    const auto pass = [&](auto is_whole) {
+        // the same for a wave: its part has all its columns
+        constexpr bool kWhole = decltype(is_whole)::value;
+        u32x4 c[kPieces];
 #pragma unroll
-    for (uint32_t b = 0; b < kBatch; ++b) {
-        const uint32_t col = column<TYPE>(first + b * 64);
-        c[b] = load_valid<TYPE>(a.x, row * a.x.stride + col, valid_of<TYPE>(col, a.vocab));
-    }
-    const float lse = a.lse[row];
-    const RowGrad q =
-        row_grad(lse, 0.0f, lse == -infinity(), ENTROPY ? a.entropies[row] : 0.0f,
-                 a.dlog_probs[row], ENTROPY ? a.dentropies[row] : 0.0f, a.targets[row], a.vocab);
+        for (uint32_t b = 0; b < kPieces; ++b) {
+            const uint32_t col = first + b * LANES * kPer<TYPE>;
+            const char *p = x + col * (size_t)kSize<TYPE>;
+            if (kWhole || col + kPer<TYPE> <= a.vocab) {
+                c[b] = ld_nt_at<u32x4, kSize<TYPE>>(p);
+            } else if (col < a.vocab) {
+                // the elements before are another wave's, and may be gradients already
+                c[b] = u32x4{0, 0, 0, 0};
 #pragma unroll
-    for (uint32_t b = 0; b < kBatch; ++b) {
-        const uint32_t col = column<TYPE>(first + b * 64), valid = valid_of<TYPE>(col, a.vocab);
-        if (valid)
-            store_chunk<TYPE, true, kApart<TYPE>>(a.dx, row * a.dx.stride + col, valid,
-                                                  grad_chunk<TYPE, ENTROPY>(q, c[b], col, [](float) {}));
-    }
+                for (uint32_t e = 0; e < kPer<TYPE>; ++e) {
+                    const uint32_t at = clamped(e, a.vocab - col);
+                    if constexpr (TYPE == kBf16)
+                        c[b][e / 2] |= (uint32_t)reinterpret_cast<const uint16_t *>(p)[at]
+                                       << (16 * (e % 2));
+                    else
+                        c[b][e] = reinterpret_cast<const uint32_t *>(p)[at];
+                }
+            }
+        }
+        const float lse = a.lse[row];
+        RowGrad q = row_grad(lse, 0.0f, lse == -infinity(), ENTROPY ? a.entropies[row] : 0.0f,
+                             a.dlog_probs[row], ENTROPY ? a.dentropies[row] : 0.0f, a.targets[row],
+                             a.vocab);
+        if (__builtin_fabsf(lse) < kOrdinary) {
+            // e^(x - lse) = 2^(x c - k) 2^-lo, with lse c = k + lo exactly
+            const float k = lse * kLog2e, lo = __builtin_fmaf(lse, kLog2e, -k);
+            make_binary(q, k, __builtin_amdgcn_exp2f(-lo), lo * (1.0f / kLog2e));
+        }
+        const auto each = [&](auto binary) {
+#pragma unroll
+            for (uint32_t b = 0; b < kPieces; ++b) {
+                const uint32_t col = first + b * LANES * kPer<TYPE>;
+                if (!kWhole && col >= a.vocab)
+                    continue;
+                const u32x4 w = grad_piece<TYPE, ENTROPY, decltype(binary)::value>(
+                    q, c[b], q.target - col, [](float) {});
+                char *p = dx + col * (size_t)kSize<TYPE>;
+                if (kWhole || col + kPer<TYPE> <= a.vocab)
+                    st_nt_at<u32x4, kSize<TYPE>>(p, w);
+                else
+                    store_some<TYPE>(p, w, 0, a.vocab - col);
+            }
+        };
+        if (q.binary)
+            each(std::true_type{});
+        else
+            each(std::false_type{});
+    };
+    if (LANES == 64 && start + LANES * BATCH <= a.vocab)
+        pass(std::true_type{});
+    else
+        pass(std::false_type{});
 }
 
 struct TrainArgs {
@@ -480,62 +762,161 @@ struct TrainArgs {
     const float *dlog_probs, *dentropies;
 };
 
-// A row held in registers, C chunks a lane: read once, its sums, then its gradient.
+// Waves of a SIMD to leave registers for: two workgroups a CU where 128 (of 1024 lanes, 64)
+// hold a row's share, so that one's loads and stores run beside the other's arithmetic.
+constexpr uint32_t train_waves(uint32_t threads) { return threads > kThreads ? 4 : 1; }
+
+// A row held in registers, C pieces a lane: read once, its sums, then its gradient.
 template <int TYPE, uint32_t THREADS, uint32_t C, bool ENTROPY>
-__global__ __launch_bounds__(THREADS < kThreads ? kThreads : THREADS) void train_kernel(
+__global__ __launch_bounds__(group_of(THREADS), train_waves(THREADS)) void train_kernel(
     TrainArgs a) {
-    constexpr uint32_t kGroup = THREADS < kThreads ? kThreads : THREADS;
-    __shared__ Sums shared[kGroup / 64];
-    const uint32_t lane = threadIdx.x % THREADS;
-    const size_t row = a.f.base + (size_t)blockIdx.x * (kGroup / THREADS) + threadIdx.x / THREADS;
-    if (THREADS == 64 && row >= a.f.rows)
+    constexpr uint32_t kGroup = group_of(THREADS);
+    __shared__ Sums shared[2][kGroup / 64];
+    const uint32_t vocab = a.f.vocab;
+    uint32_t lane = threadIdx.x % THREADS;
+    const size_t row =
+        a.f.base + (size_t)blockIdx.x * (kGroup / THREADS) + row_in_group<THREADS>();
+    if (THREADS < kThreads && row >= a.f.rows)
         return;
-    const size_t off = row * a.f.x.stride;
-    Chunk<TYPE> c[C];
+    const char *x = row_of<TYPE>(a.f.x, row);
+    char *dx = row_of<TYPE>(a.dx, row);
+    u32x4 c[C];
 #pragma unroll
-    for (uint32_t b = 0; b < C; ++b) {
-        const uint32_t col = column<TYPE>(lane + b * THREADS);
-        c[b] = load_valid<TYPE>(a.f.x, off + col, valid_of<TYPE>(col, a.f.vocab));
-    }
+    for (uint32_t b = 0; b < C; ++b)
+        c[b] = load_piece<TYPE>(x, (lane + b * THREADS) * kPer<TYPE>, vocab);
     const int64_t target = a.f.targets[row];
     const float g = a.dlog_probs[row], h = ENTROPY && a.dentropies ? a.dentropies[row] : 0.0f;
-    Sums t = no_sums();
+    // (and the places of the pieces are not kept either)
+    hold(lane);
+    float top = kLowest;
 #pragma unroll
     for (uint32_t b = 0; b < C; ++b) {
-        float x[8];
-        chunk_values(c[b], x);
-        t.r = __builtin_fmaxf(t.r, max_of(x));
+        mask_end<TYPE>(c[b], (lane + b * THREADS) * kPer<TYPE>, vocab, vocab);
+        float v[kPer<TYPE>];
+        values_of<TYPE>(c[b], v);
+        top = __builtin_fmaxf(top, max_of(v));
     }
+    const auto sums = [&](auto binary) {
+        constexpr bool kBinary = decltype(binary)::value;
+        Sums t{reference<kBinary>(top), 0.0f, 0.0f};
 #pragma unroll
-    for (uint32_t b = 0; b < C; ++b) {
-        float x[8];
-        hold(c[b]);
-        chunk_values(c[b], x);
-        add<ENTROPY>(t, x);
-    }
-    t = join_workgroup<THREADS>(t, shared);
+        for (uint32_t b = 0; b < C; ++b) {
+            float v[kPer<TYPE>];
+            hold(c[b]);
+            values_of<TYPE>(c[b], v);
+            add<ENTROPY, kBinary>(t, v);
+        }
+        return join_lanes<THREADS, kBinary>(t, shared[kBinary]);
+    };
+    const Sums two = sums(std::true_type{});
+    const bool binary = held(two);
+    const Sums t = binary ? natural(two) : sums(std::false_type{});
     const float ln = logf(t.s);
     if (lane == 0) {
         store_sums(a.f, row, t, ln);
         // the lane that holds the target's logit stores the others: dx may be x
         if (target < 0)
             a.f.log_probs[row] = 0.0f;
-        else if (target >= (int64_t)a.f.vocab)
+        else if (target >= (int64_t)vocab)
             a.f.log_probs[row] = not_a_number();
         else if (t.s == 0.0f)
             a.f.log_probs[row] = -infinity();
     }
-    const RowGrad q = row_grad(t.r, ln, t.s == 0.0f, ln - t.w / t.s, g, h, target, a.f.vocab);
+    RowGrad q = row_grad(t.r, ln, t.s == 0.0f, ln - t.w / t.s, g, h, target, vocab);
+    if (binary) {
+        const float off = (float)((double)two.r * (1.0 / (double)kLog2e) - (double)t.r);
+        make_binary(q, two.r, 1.0f / two.s, -off);
+    }
+    hold(lane);
+    const auto each = [&](auto is_binary) {
 #pragma unroll
-    for (uint32_t b = 0; b < C; ++b) {
-        const uint32_t col = column<TYPE>(lane + b * THREADS);
-        const uint32_t valid = valid_of<TYPE>(col, a.f.vocab);
-        hold(c[b]);
-        if (valid)
-            store_chunk<TYPE, true, kApart<TYPE>>(a.dx, row * a.dx.stride + col, valid,
-                                                  grad_chunk<TYPE, ENTROPY>(q, c[b], col, [&](float v) {
-                                                      a.f.log_probs[row] = log_prob(v, t, ln);
-                                                  }));
+        for (uint32_t b = 0; b < C; ++b) {
+            const uint32_t col = (lane + b * THREADS) * kPer<TYPE>;
+            hold(c[b]);
+            if (col >= vocab)
+                continue;
+            const uint32_t at = place_of<TYPE>(col, vocab);
+            // (the target is in this piece if it is within its columns, not if it is before them)
+            const u32x4 w = grad_piece<TYPE, ENTROPY, decltype(is_binary)::value>(
+                q, c[b], q.target - col < kPer<TYPE> ? q.target - at : kNoTarget,
+                [&](float v) { a.f.log_probs[row] = log_prob(v, t, ln); });
+            char *p = dx + at * (size_t)kSize<TYPE>;
+            if (at == col)
+                st_nt_at<u32x4, kSize<TYPE>>(p, w);
+            else
+                store_some<TYPE>(p, w, col - at, kPer<TYPE>);
+        }
+    };
+    if (q.binary)
+        each(std::true_type{});
+    else
+        each(std::false_type{});
+}
+
+// Rows of less than a piece: a lane a row, forward, backward or both.
+template <int TYPE, bool FORWARD, bool BACKWARD>
+__global__ __launch_bounds__(64) void short_kernel(RowArgs a, GradArgs b) {
+    const size_t row = a.base + (size_t)blockIdx.x * 64 + threadIdx.x;
+    if (row >= a.rows)
+        return;
+    const char *p = row_of<TYPE>(a.x, row);
+    float x[8];
+    float r = kLowest;
+#pragma unroll
+    for (uint32_t e = 0; e < 8; ++e) {
+        x[e] = -infinity();
+        if (e < a.vocab)
+            x[e] = TYPE == kBf16 ? bf16_lo(reinterpret_cast<const uint16_t *>(p)[e])
+                                 : reinterpret_cast<const float *>(p)[e];
+        r = __builtin_fmaxf(r, x[e]);
+    }
+    const int64_t target = a.targets[row];
+    RowGrad q;
+    if constexpr (FORWARD) {
+        Sums t{r, 0.0f, 0.0f};
+        add<true, false>(t, x);
+        const float ln = logf(t.s);
+        Target found{target, 0.0f};
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e)
+            found.x = target == (int64_t)e ? x[e] : found.x;
+        finish(a, row, found, t, ln);
+        for (uint32_t i = 0; i < (a.top ? a.vocab : 0); ++i) {
+            Key k = 0;
+            uint32_t rank = 0;
+#pragma unroll
+            for (uint32_t e = 0; e < 8; ++e)
+                k = e == i ? key_of(x[e], e) : k;
+#pragma unroll
+            for (uint32_t e = 0; e < 8; ++e)
+                rank += e < a.vocab && key_of(x[e], e) > k;
+            if (rank < a.top) {
+                a.top_ids[row * a.top + rank] = (int32_t)i;
+                a.top_log_probs[row * a.top + rank] = log_prob(value_of(k), t, ln);
+            }
+        }
+        if constexpr (BACKWARD)
+            q = row_grad(r, ln, t.s == 0.0f, ln - t.w / t.s, b.dlog_probs[row],
+                         b.dentropies ? b.dentropies[row] : 0.0f, target, a.vocab);
+    } else {
+        const float lse = b.lse[row];
+        q = row_grad(lse, 0.0f, lse == -infinity(), b.entropies ? b.entropies[row] : 0.0f,
+                     b.dlog_probs[row], b.dentropies ? b.dentropies[row] : 0.0f, target, a.vocab);
+    }
+    if constexpr (BACKWARD) {
+        char *o = row_of<TYPE>(b.dx, row);
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e) {
+            const float d = x[e] - q.r;
+            float y = exp_of(d - q.ln) * __builtin_fmaf(-q.h, __builtin_fmaxf(d, kFar), q.f);
+            y += q.target == e ? q.g : 0.0f;
+            if (e < a.vocab) {
+                if constexpr (TYPE == kBf16)
+                    reinterpret_cast<uint16_t *>(o)[e] = (uint16_t)bf16_pair(y, y);
+                else
+                    reinterpret_cast<float *>(o)[e] = y;
+            }
+        }
     }
 }
 
@@ -555,7 +936,7 @@ Cut cut_of(size_t rows, uint32_t vocab, uint32_t top) {
     if (top) {
         uint32_t slice = kThreads * 8;
         while (slice < kThreads * 8 * 4 &&
-               (rows * ((vocab + slice - 1) / slice) > kFill ||
+                   (rows * ((vocab + slice - 1) / slice) > kFill ||
                 (size_t)((vocab + slice - 1) / slice) * top > kThreads * kTopPerLane / 2))
             slice *= 2;
         return {(vocab + slice - 1) / slice, slice};
@@ -606,49 +987,83 @@ void for_rows(A &a, size_t per_row, size_t rows_per, F &&launch) {
     a.rows = rows;
 }
 
+GradArgs grad_args(const LogProbsArgs &args) {
+    return {args.x,          args.dx,         args.targets, args.lse, args.entropies,
+            args.dlog_probs, args.dentropies, args.rows,    0,        args.vocab, 0};
+}
+
+template <uint32_t N>
+using Number = std::integral_constant<uint32_t, N>;
+
+// Rows of less than a piece.
+template <int TYPE, bool FORWARD, bool BACKWARD>
+void launch_short(const LogProbsArgs &args, hipStream_t stream) {
+    RowArgs a = row_args(args, {1, args.vocab});
+    const GradArgs b = grad_args(args);
+    for_rows(a, 1, 64, [&](unsigned grid) {
+        hipLaunchKernelGGL((short_kernel<TYPE, FORWARD, BACKWARD>), dim3(grid), dim3(64), 0, stream,
+                           a, b);
+    });
+}
+
+template <int TYPE>
+void top_typed(const LogProbsArgs &args, const Cut &cut, hipStream_t stream) {
+    RowArgs a = row_args(args, cut);
+    const uint32_t per_lane = cut.slice / kThreads;
+    // lanes that have a key in every slice, the last one's aside
+    const uint32_t columns = cut.splits > 1 ? cut.slice : args.vocab;
+    a.group = group_lanes((columns + kPer<TYPE> - 1) / kPer<TYPE> < kThreads
+                              ? (columns + kPer<TYPE> - 1) / kPer<TYPE>
+                              : kThreads,
+                          args.top);
+    size_t lds = list_keys(per_lane, a.group, args.top) * sizeof(Key);
+    for_rows(a, cut.splits, 1, [&](unsigned grid) {
+        if (per_lane == 8)
+            hipLaunchKernelGGL((top_kernel<TYPE, 8>), dim3(grid), dim3(kThreads), lds, stream, a);
+        else if (per_lane == 16)
+            hipLaunchKernelGGL((top_kernel<TYPE, 16>), dim3(grid), dim3(kThreads), lds, stream, a);
+        else
+            hipLaunchKernelGGL((top_kernel<TYPE, 32>), dim3(grid), dim3(kThreads), lds, stream, a);
+    });
+    if (cut.splits == 1)
+        return;
+    const uint32_t keys = cut.splits * args.top;
+    a.group = group_lanes(keys < kThreads ? keys : kThreads, args.top);
+    lds = list_keys((keys + kThreads - 1) / kThreads, a.group, args.top) * sizeof(Key);
+    for_rows(a, 1, 1, [&](unsigned grid) {
+        hipLaunchKernelGGL(top_join_kernel<TYPE>, dim3(grid), dim3(kThreads), lds, stream, a);
+    });
+}
+
 template <int TYPE>
 void forward_typed(const LogProbsArgs &args, hipStream_t stream) {
+    if (args.vocab < kPer<TYPE>)
+        return launch_short<TYPE, true, false>(args, stream);
     const Cut cut = cut_of(args.rows, args.vocab, args.top);
+    if (args.top)
+        return top_typed<TYPE>(args, cut, stream);
     RowArgs a = row_args(args, cut);
-    if (args.top) {
-        const size_t lds = 2 * kTopPerLane * args.top * sizeof(Key);
-        const uint32_t chunks = cut.slice / (kThreads * 8);
-        for_rows(a, cut.splits, 1, [&](unsigned grid) {
-            if (chunks == 1)
-                hipLaunchKernelGGL((top_kernel<TYPE, 1>), dim3(grid), dim3(kThreads), lds, stream,
-                                   a);
-            else if (chunks == 2)
-                hipLaunchKernelGGL((top_kernel<TYPE, 2>), dim3(grid), dim3(kThreads), lds, stream,
-                                   a);
-            else
-                hipLaunchKernelGGL((top_kernel<TYPE, 4>), dim3(grid), dim3(kThreads), lds, stream,
-                                   a);
-        });
-        for_rows(a, 1, 1, [&](unsigned grid) {
-            hipLaunchKernelGGL(top_join_kernel<TYPE>, dim3(grid), dim3(kThreads), lds, stream, a);
-        });
-        return;
-    }
-    // a wave a row where that is enough lanes for it
-    if (cut.splits == 1 && args.vocab <= 2048) {
-        for_rows(a, 1, kThreads / 64, [&](unsigned grid) {
+    const auto launch = [&](auto threads, auto batch) {
+        constexpr uint32_t kLanes = decltype(threads)::value, kIn = decltype(batch)::value;
+        constexpr uint32_t kGroup = group_of(kLanes);
+        for_rows(a, cut.splits, kGroup / kLanes, [&](unsigned grid) {
             if (a.entropies)
-                hipLaunchKernelGGL((forward_kernel<TYPE, 64, true>), dim3(grid), dim3(kThreads), 0,
-                                   stream, a);
+                hipLaunchKernelGGL((forward_kernel<TYPE, kLanes, kIn, true>), dim3(grid),
+                                   dim3(kGroup), 0, stream, a);
             else
-                hipLaunchKernelGGL((forward_kernel<TYPE, 64, false>), dim3(grid), dim3(kThreads), 0,
-                                   stream, a);
+                hipLaunchKernelGGL((forward_kernel<TYPE, kLanes, kIn, false>), dim3(grid),
+                                   dim3(kGroup), 0, stream, a);
         });
-        return;
-    }
-    for_rows(a, cut.splits, 1, [&](unsigned grid) {
-        if (a.entropies)
-            hipLaunchKernelGGL((forward_kernel<TYPE, kThreads, true>), dim3(grid), dim3(kThreads),
-                               0, stream, a);
-        else
-            hipLaunchKernelGGL((forward_kernel<TYPE, kThreads, false>), dim3(grid), dim3(kThreads),
-                               0, stream, a);
-    });
+    };
+    // as many lanes a row as have work in it
+    if (args.vocab <= 16 * 8)
+        launch(Number<16>{}, Number<8>{});
+    else if (args.vocab <= 16 * 32)
+        launch(Number<16>{}, Number<32>{});
+    else if (args.vocab <= 64 * 32)
+        launch(Number<64>{}, Number<32>{});
+    else
+        launch(Number<256>{}, Number<32>{});
     if (cut.splits > 1)
         for_rows(a, 1, 1, [&](unsigned grid) {
             hipLaunchKernelGGL(join_kernel<TYPE>, dim3(grid), dim3(64), 0, stream, a);
@@ -657,54 +1072,73 @@ void forward_typed(const LogProbsArgs &args, hipStream_t stream) {
 
 template <int TYPE>
 void backward_typed(const LogProbsArgs &args, hipStream_t stream) {
-    GradArgs a{args.x,         args.dx,         args.targets,    args.lse, args.entropies,
-               args.dlog_probs, args.dentropies, args.rows,      0,        args.vocab, 0};
-    const uint32_t wave = 64 * 8 * kBatch;
-    a.per_row = (a.vocab + wave - 1) / wave;
-    // whole rows a launch, four waves to a workgroup
-    for_rows(a, a.per_row, kThreads / 64, [&](unsigned grid) {
-        if (args.dentropies)
-            hipLaunchKernelGGL((backward_kernel<TYPE, true>), dim3(grid), dim3(kThreads), 0, stream,
-                               a);
-        else
-            hipLaunchKernelGGL((backward_kernel<TYPE, false>), dim3(grid), dim3(kThreads), 0,
-                               stream, a);
-    });
+    if (args.vocab < kPer<TYPE>)
+        return launch_short<TYPE, false, true>(args, stream);
+    GradArgs a = grad_args(args);
+    const auto launch = [&](auto lanes, auto batch) {
+        constexpr uint32_t kLanes = decltype(lanes)::value, kIn = decltype(batch)::value;
+        a.per_row = (a.vocab + kLanes * kIn - 1) / (kLanes * kIn);
+        for_rows(a, a.per_row, kThreads / kLanes, [&](unsigned grid) {
+            if (args.dentropies)
+                hipLaunchKernelGGL((backward_kernel<TYPE, kLanes, kIn, true>), dim3(grid),
+                                   dim3(kThreads), 0, stream, a);
+            else
+                hipLaunchKernelGGL((backward_kernel<TYPE, kLanes, kIn, false>), dim3(grid),
+                                   dim3(kThreads), 0, stream, a);
+        });
+    };
+    if (args.vocab <= 16 * 8)
+        launch(Number<16>{}, Number<8>{});
+    else if (args.vocab <= 16 * 32)
+        launch(Number<16>{}, Number<32>{});
+    else
+        launch(Number<64>{}, Number<kBatch>{});
 }
 
-template <int TYPE, uint32_t THREADS, uint32_t C>
+// E elements a lane.
+template <int TYPE, uint32_t THREADS, uint32_t E>
 void launch_train(const LogProbsArgs &args, hipStream_t stream) {
+    constexpr uint32_t kPieces = E / kPer<TYPE>, kGroup = group_of(THREADS);
     TrainArgs a{row_args(args, {1, args.vocab}), args.dx, args.dlog_probs, args.dentropies};
-    constexpr uint32_t kGroup = THREADS < kThreads ? kThreads : THREADS;
     for_rows(a.f, 1, kGroup / THREADS, [&](unsigned grid) {
         if (args.entropies)
-            hipLaunchKernelGGL((train_kernel<TYPE, THREADS, C, true>), dim3(grid), dim3(kGroup), 0,
-                               stream, a);
+            hipLaunchKernelGGL((train_kernel<TYPE, THREADS, kPieces, true>), dim3(grid),
+                               dim3(kGroup), 0, stream, a);
         else
-            hipLaunchKernelGGL((train_kernel<TYPE, THREADS, C, false>), dim3(grid), dim3(kGroup), 0,
-                               stream, a);
+            hipLaunchKernelGGL((train_kernel<TYPE, THREADS, kPieces, false>), dim3(grid),
+                               dim3(kGroup), 0, stream, a);
     });
 }
 
-// Rows that fit a workgroup's registers are read once; longer ones take the two
-// passes, and so do rows that are few and long, which these cut into slices.
-constexpr uint32_t kMostTrain = 1024 * 8 * 8;
-bool one_pass(size_t, uint32_t vocab) { return vocab <= kMostTrain; }
+// Rows that fit a workgroup's registers, half of a CU's or, for the longest, all, are read
+// once; longer ones take the two passes.
+template <int TYPE>
+constexpr uint32_t kMostTrain = 1024 * 16 * kPer<TYPE>;
 
 template <int TYPE>
 void train_typed(const LogProbsArgs &args, hipStream_t stream) {
-    if (args.vocab <= 64 * 8 * 2)
-        launch_train<TYPE, 64, 2>(args, stream);
-    else if (args.vocab <= 64 * 8 * 4)
-        launch_train<TYPE, 64, 4>(args, stream);
-    else if (args.vocab <= 256 * 8 * 4)
-        launch_train<TYPE, 256, 4>(args, stream);
-    else if (args.vocab <= 256 * 8 * 8)
-        launch_train<TYPE, 256, 8>(args, stream);
-    else if (args.vocab <= 1024 * 8 * 4)
-        launch_train<TYPE, 1024, 4>(args, stream);
+    const uint32_t v = args.vocab;
+    constexpr uint32_t kLong = 16 * kPer<TYPE>;  // elements of 64 registers
+    if (v < kPer<TYPE>)
+        launch_short<TYPE, true, true>(args, stream);
+    else if (v <= 16 * 8)
+        launch_train<TYPE, 16, 8>(args, stream);
+    else if (v <= 16 * 32)
+        launch_train<TYPE, 16, 32>(args, stream);
+    else if (v <= 64 * 16)
+        launch_train<TYPE, 64, 16>(args, stream);
+    else if (v <= 64 * 32)
+        launch_train<TYPE, 64, 32>(args, stream);
+    else if (v <= 256 * 32)
+        launch_train<TYPE, 256, 32>(args, stream);
+    else if (v <= 512 * 32)
+        launch_train<TYPE, 512, 32>(args, stream);
+    else if (v <= 512 * kLong / 2)
+        launch_train<TYPE, 512, kLong / 2>(args, stream);
+    else if (v <= 512 * kLong)
+        launch_train<TYPE, 512, kLong>(args, stream);
     else
-        launch_train<TYPE, 1024, 8>(args, stream);
+        launch_train<TYPE, 1024, kLong>(args, stream);
 }
 
 }  // namespace
@@ -713,11 +1147,10 @@ size_t log_probs_workspace(size_t rows, size_t vocab, uint32_t top) {
     if (!rows || !vocab)
         return 0;
     const Cut cut = cut_of(rows, (uint32_t)vocab, top);
-    size_t bytes = 0;
-    if (cut.splits > 1 || top)
-        bytes = (rows * cut.splits * sizeof(Sums) + 15) / 16 * 16 +
-                rows * cut.splits * top * sizeof(Key);
-    return bytes;
+    if (cut.splits == 1)
+        return 0;
+    return (rows * cut.splits * sizeof(Sums) + 15) / 16 * 16 +
+           rows * cut.splits * top * sizeof(Key);
 }
 
 hipError_t launch_log_probs_forward(const LogProbsArgs &a, int type, hipStream_t stream) {
@@ -737,7 +1170,7 @@ hipError_t launch_log_probs_backward(const LogProbsArgs &a, int type, hipStream_
 }
 
 hipError_t launch_log_probs_train(const LogProbsArgs &a, int type, hipStream_t stream) {
-    if (!one_pass(a.rows, a.vocab)) {
+    if (a.vocab > (type == kBf16 ? kMostTrain<kBf16> : kMostTrain<kF32>)) {
         const hipError_t e = launch_log_probs_forward(a, type, stream);
         return e == hipSuccess ? launch_log_probs_backward(a, type, stream) : e;
     }
