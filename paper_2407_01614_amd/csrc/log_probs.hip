@@ -138,7 +138,6 @@ template <int TYPE>
 __device__ __forceinline__ char *row_of(const Mat &m, size_t row) {
     return reinterpret_cast<char *>(m.data) + row * m.stride * kSize<TYPE>;
 }
-
 template <int TYPE>
 __device__ __forceinline__ void values_of(const u32x4 &w, float (&x)[kPer<TYPE>]) {
 #pragma unroll
@@ -187,17 +186,31 @@ __device__ __forceinline__ uint32_t place_of(uint32_t col, uint32_t vocab) {
     return col < vocab - kPer<TYPE> ? col : vocab - kPer<TYPE>;
 }
 
-// The piece of column `col` of a row or, to `end`, a slice of it: -Inf in the place of
-// what is another piece's or past the end.
-template <int TYPE>
-__device__ __forceinline__ u32x4 load_piece(const char *row, uint32_t col, uint32_t vocab) {
-    return ld_nt_at<u32x4, kSize<TYPE>>(row + place_of<TYPE>(col, vocab) * (size_t)kSize<TYPE>);
-}
-template <int TYPE>
-__device__ __forceinline__ void mask_end(u32x4 &w, uint32_t col, uint32_t end, uint32_t vocab) {
-    if (col + kPer<TYPE> > end)
-        mask<TYPE>(w, col < end ? col - place_of<TYPE>(col, vocab) : kPer<TYPE>);
-}
+// A row (or a slice of one, whole pieces but for the row's last) as LANES lanes go through
+// it, W columns a piece of each.
+template <int TYPE, uint32_t LANES>
+struct Line {
+    static constexpr uint32_t W = LANES * kPer<TYPE>;
+    const char *row;
+    uint32_t vocab, end;
+    // Are there columns among the lanes' pieces from `first` on, and none past the end?
+    __device__ __forceinline__ bool any(uint32_t first) const { return first < end; }
+    __device__ __forceinline__ bool whole(uint32_t first) const { return first + W <= end; }
+    __device__ __forceinline__ u32x4 load(uint32_t first, uint32_t lane) const {
+        const uint32_t at = place_of<TYPE>(first + lane * kPer<TYPE>, vocab);
+        return ld_nt_at<u32x4, kSize<TYPE>>(row + at * (size_t)kSize<TYPE>);
+    }
+    // How many elements of a piece are those of the one before it (all: past the end).
+    __device__ __forceinline__ uint32_t skip(uint32_t first, uint32_t lane) const {
+        const uint32_t col = first + lane * kPer<TYPE>;
+        return col < end ? col - place_of<TYPE>(col, vocab) : kPer<TYPE>;
+    }
+    // -Inf in their place.
+    __device__ __forceinline__ void mask_end(u32x4 &w, uint32_t first, uint32_t lane) const {
+        if (!whole(first))
+            mask<TYPE>(w, skip(first, lane));
+    }
+};
 
 // Keeps what is made of a piece behind this point: values made once for all passes over
 // the pieces would take twice their registers.
@@ -246,7 +259,7 @@ struct RowArgs {
     uint32_t splits, slice;  // slices of a row, and their columns
     Sums *partials;          // [row][split]
     unsigned long long *keys;  // [row][split][top]
-    uint32_t top, group;  // group: lanes of a group of the selection
+    uint32_t top, room;  // room: keys of the list
     int32_t *top_ids;
     float *top_log_probs;
 };
@@ -266,6 +279,12 @@ __device__ __forceinline__ void store_sums(const RowArgs &a, size_t row, const S
     if (a.entropies)
         a.entropies[row] = t.s == 0.0f ? 0.0f : ln - t.w / t.s;
 }
+template <int TYPE>
+__device__ __forceinline__ float value_at(const char *row, uint32_t col) {
+    const char *p = row + col * (size_t)kSize<TYPE>;
+    return TYPE == kBf16 ? bf16_lo(*reinterpret_cast<const uint16_t *>(p))
+                         : *reinterpret_cast<const float *>(p);
+}
 // A row's target and its logit, read by one lane before the row is.
 struct Target {
     int64_t at;
@@ -274,11 +293,8 @@ struct Target {
 template <int TYPE>
 __device__ __forceinline__ Target target_of(const RowArgs &a, size_t row) {
     Target t{a.targets[row], 0.0f};
-    if (t.at >= 0 && t.at < (int64_t)a.vocab) {
-        const char *p = row_of<TYPE>(a.x, row) + (size_t)t.at * kSize<TYPE>;
-        t.x = TYPE == kBf16 ? bf16_lo(*reinterpret_cast<const uint16_t *>(p))
-                            : *reinterpret_cast<const float *>(p);
-    }
+    if (t.at >= 0 && t.at < (int64_t)a.vocab)
+        t.x = value_at<TYPE>(row_of<TYPE>(a.x, row), (uint32_t)t.at);
     return t;
 }
 __device__ __forceinline__ void finish(const RowArgs &a, size_t row, const Target &target,
@@ -292,31 +308,32 @@ __device__ __forceinline__ void finish(const RowArgs &a, size_t row, const Targe
     store_sums(a, row, t, ln);
 }
 
-// A lane's sums of columns begin .. end, one of THREADS that share them; BATCH elements in
-// flight.
+// A lane's sums of a slice from `begin` on; BATCH elements in flight.
 constexpr uint32_t kBatch = 32;
-template <int TYPE, uint32_t THREADS, uint32_t BATCH, bool ENTROPY, bool BINARY>
-__device__ __forceinline__ Sums sums_of(const char *row, uint32_t begin, uint32_t end,
-                                        uint32_t vocab, uint32_t lane) {
-    constexpr uint32_t kPieces = BATCH / kPer<TYPE>;
+template <int TYPE, uint32_t LANES, uint32_t BATCH, bool ENTROPY, bool BINARY>
+__device__ __forceinline__ Sums sums_of(const Line<TYPE, LANES> &line, uint32_t begin,
+                                        uint32_t lane) {
+    constexpr uint32_t kPieces = BATCH / kPer<TYPE>, W = LANES * kPer<TYPE>;
     Sums t = no_sums();
     float top = kLowest;
-    for (uint32_t i = begin; i < end; i += BATCH * THREADS) {
+    for (uint32_t i = begin; line.any(i); i += kPieces * W) {
         u32x4 c[kPieces];
 #pragma unroll
         for (uint32_t b = 0; b < kPieces; ++b)
-            c[b] = load_piece<TYPE>(row, i + (b * THREADS + lane) * kPer<TYPE>, vocab);
+            c[b] = line.load(i + b * W, lane);
         float x[kPieces][kPer<TYPE>];
 #pragma unroll
-        for (uint32_t b = 0; b < kPieces; ++b) {
-            mask_end<TYPE>(c[b], i + (b * THREADS + lane) * kPer<TYPE>, end, vocab);
-            values_of<TYPE>(c[b], x[b]);
-            top = __builtin_fmaxf(top, max_of(x[b]));
-        }
+        for (uint32_t b = 0; b < kPieces; ++b)
+            if (line.any(i + b * W)) {
+                line.mask_end(c[b], i + b * W, lane);
+                values_of<TYPE>(c[b], x[b]);
+                top = __builtin_fmaxf(top, max_of(x[b]));
+            }
         t = joined<BINARY>(t, reference<BINARY>(top));
 #pragma unroll
         for (uint32_t b = 0; b < kPieces; ++b)
-            add<ENTROPY, BINARY>(t, x[b]);
+            if (line.any(i + b * W))
+                add<ENTROPY, BINARY>(t, x[b]);
     }
     return t;
 }
@@ -330,6 +347,11 @@ __device__ __forceinline__ uint32_t row_in_group() {
         return 0;
     const uint32_t r = threadIdx.x / THREADS;
     return THREADS < 64 ? r : __builtin_amdgcn_readfirstlane(r);
+}
+
+__device__ __forceinline__ uint32_t slice_end(const RowArgs &a, uint32_t split) {
+    const uint32_t begin = split * a.slice;
+    return a.vocab - begin < a.slice ? a.vocab : begin + a.slice;
 }
 
 // THREADS lanes a row or slice: 16 or 64 of a workgroup of 256, or the workgroup.
@@ -348,18 +370,17 @@ __global__ __launch_bounds__(group_of(THREADS)) void forward_kernel(RowArgs a) {
         split = blockIdx.x % a.splits;
     }
     const uint32_t begin = split * a.slice;
-    const uint32_t end = a.vocab - begin < a.slice ? a.vocab : begin + a.slice;
-    const char *x = row_of<TYPE>(a.x, row);
+    const Line<TYPE, THREADS> line{row_of<TYPE>(a.x, row), a.vocab, slice_end(a, split)};
     Target target{};
     if (lane == 0 && a.splits == 1)
         target = target_of<TYPE>(a, row);
     Sums t = join_lanes<THREADS, true>(
-        sums_of<TYPE, THREADS, BATCH, ENTROPY, true>(x, begin, end, a.vocab, lane), shared[0]);
+        sums_of<TYPE, THREADS, BATCH, ENTROPY, true>(line, begin, lane), shared[0]);
     if (held(t))
         t = natural(t);
     else
         t = join_lanes<THREADS, false>(
-            sums_of<TYPE, THREADS, BATCH, ENTROPY, false>(x, begin, end, a.vocab, lane), shared[1]);
+            sums_of<TYPE, THREADS, BATCH, ENTROPY, false>(line, begin, lane), shared[1]);
     if (lane == 0) {
         if (a.splits > 1)
             a.partials[row * a.splits + split] = t;
@@ -390,102 +411,79 @@ __global__ __launch_bounds__(64) void join_kernel(RowArgs a) {
 // --------------------------------------------------------------------------
 // The most probable tokens.  An element is one 64-bit key: its value as an integer
 // of the same order, and below it its column, inverted, so that of equals the lower
-// comes first and no two keys are alike.  Every lane finds its largest key; groups of
-// 1 to 8 lanes put theirs into LDS, and the k-th largest of these is a threshold that
-// at least k elements reach, and few more: they all are in the k groups whose largest
-// key reaches it.  They are listed, and each one's rank is counted.
+// comes first and no two keys are alike.
+//
+// The lanes that share a row go through it in batches.  In the first, the `top`-th
+// largest of the lanes' largest values is a bound that at least `top` elements reach, and
+// few more; what reaches it, there and in later batches, is listed in LDS, and at the end
+// each listed key's rank is counted.  A list that overflows (values that rise along the
+// row, or many equal ones) is cut to its `top` largest, which raises the bound, and the
+// batch goes through again with the bound of its own lanes' largest keys, which no more
+// than `top` lanes' elements reach.
 // --------------------------------------------------------------------------
 typedef unsigned long long Key;
 typedef Key KeyPair __attribute__((ext_vector_type(2)));
-constexpr uint32_t kTopPerLane = 32;  // keys of a lane at most
 
-__device__ __forceinline__ Key key_of(float x, uint32_t col) {
+__device__ __forceinline__ uint32_t order_of(float x) {
     const uint32_t b = __float_as_uint(x + 0.0f);  // both zeros are one
-    const uint32_t order = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
-    return (Key)order << 32 | (0xFFFFFFFFu - col);
+    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
-__device__ __forceinline__ float value_of(Key k) {
-    const uint32_t order = (uint32_t)(k >> 32);
+__device__ __forceinline__ float ordered(uint32_t order) {
     return __uint_as_float(order & 0x80000000u ? order ^ 0x80000000u : ~order);
 }
+__device__ __forceinline__ Key key_of(float x, uint32_t col) {
+    return (Key)order_of(x) << 32 | (0xFFFFFFFFu - col);
+}
+__device__ __forceinline__ float value_of(Key k) { return ordered((uint32_t)(k >> 32)); }
 __device__ __forceinline__ uint32_t column_of(Key k) { return 0xFFFFFFFFu - (uint32_t)k; }
 
-template <int CTRL>
-__device__ __forceinline__ Key max_beside(Key k) {
-    const Key other = (Key)dpp<CTRL>((uint32_t)(k >> 32)) << 32 | dpp<CTRL>((uint32_t)k);
-    return k > other ? k : other;
+constexpr uint32_t kSpare = 8;     // lanes past `top` that a bound may let through
+constexpr uint32_t kRankStep = 8;  // keys that are ranked against at a time
+// Keys of a list: `top` from before, and those of a batch at its worst.
+constexpr uint32_t list_keys(uint32_t per_lane, uint32_t top) {
+    const uint32_t n = per_lane * (top + kSpare) + top;
+    return n < 256 ? 256 : (n + 7) / 8 * 8;
 }
 
-// Lanes of a group: the most that leave two groups with keys for each one asked for, of
-// `lanes` that have any.
-inline uint32_t group_lanes(uint32_t lanes, uint32_t top) {
-    uint32_t n = 8;
-    while (n > 1 && lanes / n < 2 * top)
-        n /= 2;
-    return n;
-}
-// The list's length: all keys of `top` groups, and to a multiple of the ranks' loop.
-constexpr uint32_t kRankStep = 8;
-inline uint32_t list_keys(uint32_t per_lane, uint32_t group, uint32_t top) {
-    return (per_lane * group * top + kRankStep - 1) / kRankStep * kRankStep + kRankStep;
+template <uint32_t THREADS>
+struct Selection {
+    __attribute__((aligned(16))) Key lanes[THREADS];
+    __attribute__((aligned(16))) Key sorted[kMostTop];
+    uint32_t counts[3];
+};
+
+// The largest number of bits from LOW on that `top` of all lanes' values reach; its lowest
+// bits stay 0 where no more than kSpare lanes beside them do.  The same in all lanes.
+template <uint32_t THREADS, int LOW, class T>
+__device__ __forceinline__ T bound_of(const Selection<THREADS> &s, uint32_t top) {
+    constexpr uint32_t kEach = THREADS / 64;
+    const T *values = reinterpret_cast<const T *>(s.lanes) + threadIdx.x % 64 * kEach;
+    T v[kEach], bound = 0;
+#pragma unroll
+    for (uint32_t j = 0; j < kEach; ++j)
+        v[j] = values[j];
+    for (int bit = 8 * (int)sizeof(T) - 1; bit >= LOW; --bit) {
+        const T trial = bound | (T)1 << bit;
+        uint32_t n = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < kEach; ++j)
+            n += (uint32_t)__builtin_popcountll(__ballot(v[j] >= trial));
+        if (n >= top) {
+            bound = trial;
+            if (n <= top + kSpare)
+                break;
+        }
+    }
+    return bound;
 }
 
-// The workgroup's `top` largest keys.  each(f) calls f with every key of the lane;
-// write(rank, key) stores one.  Returns how many were listed, which is less than `top`
-// only where there are no more.  `group` as from group_lanes.
-template <class Each, class Write>
-__device__ __forceinline__ uint32_t select_top(uint32_t top, uint32_t group, Key *list,
-                                               Each &&each, Write &&write) {
-    __shared__ __attribute__((aligned(16))) Key groups[kThreads];
-    __shared__ Key threshold;
-    __shared__ uint32_t listed;
-    Key best = 0;  // below every key
-    each([&](Key k) { best = k > best ? k : best; });
-    Key most = best;
-    if (group > 1)
-        most = max_beside<kSwap1>(most);
-    if (group > 2)
-        most = max_beside<kSwap2>(most);
-    if (group > 4)
-        most = max_beside<kMirror8>(most);
-    const uint32_t part = threadIdx.x % group;
-    if (part == 0)
-        groups[threadIdx.x / group] = most;
-    if (threadIdx.x == 0) {
-        threshold = 1;  // fewer than `top` groups with a key: all their keys
-        listed = 0;
-    }
-    __syncthreads();
-    // each lane of a group compares with its share of all groups
-    uint32_t above = 0;
-    const uint32_t share = kThreads / (group * group);
-    const KeyPair *beside = reinterpret_cast<const KeyPair *>(groups + part * share);
-#pragma unroll 4
-    for (uint32_t j = 0; j < share / 2; ++j) {
-        const KeyPair k = beside[j];
-        above += (k.x > most) + (k.y > most);
-    }
-    if (group > 1)
-        above += dpp<kSwap1>(above);
-    if (group > 2)
-        above += dpp<kSwap2>(above);
-    if (group > 4)
-        above += dpp<kMirror8>(above);
-    if (part == 0 && most && above == top - 1)
-        threshold = most;
-    __syncthreads();
-    const Key least = threshold;
-    if (best >= least)
-        each([&](Key k) {
-            if (k >= least)
-                list[atomicAdd(&listed, 1u)] = k;
-        });
-    __syncthreads();
-    const uint32_t n = listed;
+// Every listed key's rank: each(rank, key) of those below `top`.
+template <uint32_t THREADS, class F>
+__device__ __forceinline__ void rank_list(Key *list, uint32_t n, uint32_t top, F &&each) {
     if (threadIdx.x < kRankStep)
         list[n + threadIdx.x] = 0;
     __syncthreads();
-    for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
+    for (uint32_t i = threadIdx.x; i < n; i += THREADS) {
         const Key k = list[i];
         uint32_t rank = 0;
         for (uint32_t j = 0; j < n; j += kRankStep) {
@@ -496,80 +494,183 @@ __device__ __forceinline__ uint32_t select_top(uint32_t top, uint32_t group, Key
             }
         }
         if (rank < top)
-            write(rank, k);
+            each(rank, k);
     }
-    return n;
 }
 
-// A slice of a row, E elements a lane: sums and its most probable tokens; the row's
-// results where it is the only one.
-template <int TYPE, uint32_t E>
-__global__ __launch_bounds__(kThreads) void top_kernel(RowArgs a) {
+// What has been listed of a row, the same in all lanes.
+struct Listed {
+    uint32_t n = 0, round = 0;
+    float least = 0.0f;  // the bound
+};
+
+// A batch's elements, largest `m`, taken into the list.  each(f) calls f(value, column) with
+// each of the lane's whose value reaches the bound.  LOW: bits of a value that are 0, or
+// left out of the bound.
+template <uint32_t THREADS, int LOW, class Each>
+__device__ __forceinline__ void take(Selection<THREADS> &s, Key *list, uint32_t room, uint32_t top,
+                                     bool first, float m, Listed &l, Each &&each) {
+    const auto bound = [&](uint32_t order) {
+        // (below -Inf in this order: fewer than `top` lanes have a number)
+        l.least = order < 0x007FFFFFu ? -infinity() : ordered(order);
+    };
+    if (first) {
+        reinterpret_cast<uint32_t *>(s.lanes)[threadIdx.x] = order_of(m);
+        if (threadIdx.x == 0)
+            s.counts[0] = 0;
+        __syncthreads();
+        bound(bound_of<THREADS, LOW, uint32_t>(s, top));
+    }
+    // what is listed: keys from `from` on; how many those are
+    const auto push = [&](Key from) {
+        uint32_t *count = s.counts + l.round % 3;
+        l.round += 1;
+        if (threadIdx.x == 0)
+            s.counts[l.round % 3] = 0;  // last read before the barrier before this
+        if (m >= l.least) {
+            uint32_t mine = 0;
+            each([&](float x, uint32_t col) { mine += key_of(x, col) >= from; });
+            uint32_t at = l.n + atomicAdd(count, mine);
+            each([&](float x, uint32_t col) {
+                const Key k = key_of(x, col);
+                if (k >= from && at < room)
+                    list[at] = k;
+                at += k >= from;
+            });
+        }
+        __syncthreads();
+        return *count;
+    };
+    const auto cut = [&] {
+        rank_list<THREADS>(list, l.n, top, [&](uint32_t rank, Key k) { s.sorted[rank] = k; });
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < top; i += THREADS)
+            list[i] = s.sorted[i];
+        __syncthreads();
+        l.n = top;
+        l.least = value_of(list[top - 1]);
+    };
+    uint32_t n = push(0);
+    if (l.n + n > room) {
+        if (l.n > top)
+            cut();
+        Key best = 0;  // below every key
+        if (m >= l.least)
+            each([&](float x, uint32_t col) {
+                const Key k = key_of(x, col);
+                best = k > best ? k : best;
+            });
+        s.lanes[threadIdx.x] = best;
+        __syncthreads();
+        const Key from = bound_of<THREADS, 0, Key>(s, top);
+        n = push(from ? from : 1);
+    }
+    l.n += n;
+    if (l.n > room / 2 && l.n > top)
+        cut();
+}
+
+// A row's (or slice's) list's end: write(rank, key) of its `top` largest, and of ranks that no
+// number is left for, key 0.
+template <uint32_t THREADS, class F>
+__device__ __forceinline__ void write_top(Key *list, uint32_t n, uint32_t top, F &&write) {
+    rank_list<THREADS>(list, n, top, write);
+    for (uint32_t i = n + threadIdx.x; i < top; i += THREADS)
+        write(i, (Key)0);
+}
+__device__ __forceinline__ void store_top(const RowArgs &a, size_t row, uint32_t rank, Key k,
+                                          const Sums &t, float ln) {
+    // without a key (a row of NaN): some token, and no number
+    a.top_ids[row * a.top + rank] = k ? (int32_t)column_of(k) : (int32_t)rank;
+    a.top_log_probs[row * a.top + rank] = k ? log_prob(value_of(k), t, ln) : not_a_number();
+}
+
+// A row, or a slice of one: sums and its most probable tokens.  E elements a lane in a batch.
+template <int TYPE, uint32_t THREADS, uint32_t E>
+__global__ __launch_bounds__(THREADS) void top_kernel(RowArgs a) {
     extern __shared__ __attribute__((aligned(16))) Key list[];
-    __shared__ Sums shared[kThreads / 64];
-    constexpr uint32_t kPieces = E / kPer<TYPE>;
+    __shared__ Selection<THREADS> selection;
+    __shared__ Sums shared[2][THREADS / 64];
+    constexpr uint32_t kPieces = E / kPer<TYPE>, W = THREADS * kPer<TYPE>;
     const size_t row = a.base + blockIdx.x / a.splits;
     const uint32_t split = blockIdx.x % a.splits, begin = split * a.slice;
-    const uint32_t end = a.vocab - begin < a.slice ? a.vocab : begin + a.slice;
-    const char *p = row_of<TYPE>(a.x, row);
+    const uint32_t lane = threadIdx.x;
+    const Line<TYPE, THREADS> line{row_of<TYPE>(a.x, row), a.vocab, slice_end(a, split)};
     Target target{};
-    if (threadIdx.x == 0 && a.splits == 1)
+    if (lane == 0 && a.splits == 1)
         target = target_of<TYPE>(a, row);
-    u32x4 c[kPieces];
-#pragma unroll
-    for (uint32_t b = 0; b < kPieces; ++b)
-        c[b] = load_piece<TYPE>(p, begin + (b * kThreads + threadIdx.x) * kPer<TYPE>, a.vocab);
-    float x[kPieces][kPer<TYPE>];
     Sums t = no_sums();
+    float top = kLowest;
+    Listed listed;
+    for (uint32_t i = begin; line.any(i); i += kPieces * W) {
+        u32x4 c[kPieces];
 #pragma unroll
-    for (uint32_t b = 0; b < kPieces; ++b) {
-        mask_end<TYPE>(c[b], begin + (b * kThreads + threadIdx.x) * kPer<TYPE>, end, a.vocab);
-        values_of<TYPE>(c[b], x[b]);
-        t.r = __builtin_fmaxf(t.r, max_of(x[b]));
+        for (uint32_t b = 0; b < kPieces; ++b)
+            c[b] = line.load(i + b * W, lane);
+        float x[kPieces][kPer<TYPE>], m = -infinity();
+#pragma unroll
+        for (uint32_t b = 0; b < kPieces; ++b)
+            if (line.any(i + b * W)) {
+                line.mask_end(c[b], i + b * W, lane);
+                values_of<TYPE>(c[b], x[b]);
+                m = __builtin_fmaxf(m, max_of(x[b]));
+            }
+        top = __builtin_fmaxf(top, m);
+        t = joined<true>(t, reference<true>(top));
+#pragma unroll
+        for (uint32_t b = 0; b < kPieces; ++b)
+            if (line.any(i + b * W))
+                add<true, true>(t, x[b]);
+        take<THREADS, TYPE == kBf16 ? 16 : 12>(
+            selection, list, a.room, a.top, i == begin, m, listed, [&](auto &&f) {
+#pragma unroll
+                for (uint32_t b = 0; b < kPieces; ++b)
+                    if (line.any(i + b * W)) {
+                        const uint32_t col = i + (b * THREADS + lane) * kPer<TYPE>;
+                        const uint32_t at = place_of<TYPE>(col, a.vocab);
+                        const uint32_t skip = line.skip(i + b * W, lane);
+#pragma unroll
+                        for (uint32_t e = 0; e < kPer<TYPE>; ++e)
+                            if (x[b][e] >= listed.least && e >= skip)
+                                f(x[b][e], at + e);
+                    }
+            });
     }
-#pragma unroll
-    for (uint32_t b = 0; b < kPieces; ++b)
-        add<true, false>(t, x[b]);
-    t = join_lanes<kThreads, false>(t, shared);
-    float ln = 0.0f;
-    if (a.splits == 1)
-        ln = logf(t.s);
-    if (threadIdx.x == 0) {
+    t = join_lanes<THREADS, true>(t, shared[0]);
+    if (held(t))
+        t = natural(t);
+    else
+        t = join_lanes<THREADS, false>(
+            sums_of<TYPE, THREADS, E, true, false>(line, begin, lane), shared[1]);
+    const float ln = logf(t.s);
+    if (lane == 0) {
         if (a.splits == 1)
             finish(a, row, target, t, ln);
         else
             a.partials[row * a.splits + split] = t;
     }
-    const auto each = [&](auto &&f) {
-#pragma unroll
-        for (uint32_t b = 0; b < kPieces; ++b) {
-            const uint32_t col = begin + (b * kThreads + threadIdx.x) * kPer<TYPE>;
-            const uint32_t at = place_of<TYPE>(col, a.vocab);
-#pragma unroll
-            for (uint32_t e = 0; e < kPer<TYPE>; ++e)
-                if (col < end && at + e >= col)
-                    f(key_of(x[b][e], at + e));
-        }
-    };
     Key *out = a.keys + (row * a.splits + split) * a.top;
-    const uint32_t n = select_top(a.top, a.group, list, each, [&](uint32_t rank, Key k) {
-        if (a.splits == 1) {
-            a.top_ids[row * a.top + rank] = (int32_t)column_of(k);
-            a.top_log_probs[row * a.top + rank] = log_prob(value_of(k), t, ln);
-        } else {
+    write_top<THREADS>(list, listed.n, a.top, [&](uint32_t rank, Key k) {
+        if (a.splits == 1)
+            store_top(a, row, rank, k, t, ln);
+        else
             out[rank] = k;
-        }
     });
-    if (a.splits > 1)
-        for (uint32_t i = n + threadIdx.x; i < a.top; i += kThreads)
-            out[i] = 0;
 }
 
 // The slices joined: sums, and the most probable of the slices' most probable.
+constexpr uint32_t kJoined = 8;  // keys of a lane at most
 template <int TYPE>
 __global__ __launch_bounds__(kThreads) void top_join_kernel(RowArgs a) {
     extern __shared__ __attribute__((aligned(16))) Key list[];
+    __shared__ Selection<kThreads> selection;
     const size_t row = a.base + blockIdx.x;
+    const Key *keys = a.keys + row * a.splits * a.top;
+    const uint32_t n = a.splits * a.top;
+    Key k[kJoined];
+#pragma unroll
+    for (uint32_t j = 0; j < kJoined; ++j)
+        k[j] = threadIdx.x + j * kThreads < n ? keys[threadIdx.x + j * kThreads] : 0;
     Target target{};
     if (threadIdx.x == 0)
         target = target_of<TYPE>(a, row);
@@ -577,18 +678,21 @@ __global__ __launch_bounds__(kThreads) void top_join_kernel(RowArgs a) {
     const float ln = logf(t.s);
     if (threadIdx.x == 0)
         finish(a, row, target, t, ln);
-    const Key *keys = a.keys + row * a.splits * a.top;
-    const uint32_t n = a.splits * a.top;
-    select_top(
-        a.top, a.group, list,
-        [&](auto &&f) {
-            for (uint32_t i = threadIdx.x; i < n; i += kThreads)
-                f(keys[i]);
-        },
-        [&](uint32_t rank, Key k) {
-            a.top_ids[row * a.top + rank] = (int32_t)column_of(k);
-            a.top_log_probs[row * a.top + rank] = log_prob(value_of(k), t, ln);
+    float m = -infinity();
+#pragma unroll
+    for (uint32_t j = 0; j < kJoined; ++j)
+        m = __builtin_fmaxf(m, k[j] ? value_of(k[j]) : m);
+    Listed listed;
+    take<kThreads, TYPE == kBf16 ? 16 : 12>(
+        selection, list, a.room, a.top, true, m, listed, [&](auto &&f) {
+#pragma unroll
+            for (uint32_t j = 0; j < kJoined; ++j)
+                if (k[j] && value_of(k[j]) >= listed.least)
+                    f(value_of(k[j]), column_of(k[j]));
         });
+    write_top<kThreads>(list, listed.n, a.top, [&](uint32_t rank, Key key) {
+        store_top(a, row, rank, key, t, ln);
+    });
 }
 
 // --------------------------------------------------------------------------
@@ -639,34 +743,31 @@ __device__ __forceinline__ void make_binary(RowGrad &q, float k, float inv, floa
     q.binary = true;
 }
 
-// A piece's gradients; `target`: its element that is the target's, or none (kNoTarget);
-// found(x): with that one's logit.
-template <int TYPE, bool ENTROPY, bool BINARY, class F>
-__device__ __forceinline__ u32x4 grad_piece(const RowGrad &q, const u32x4 &piece, uint32_t target,
-                                            F &&found) {
+// An element's gradient, but for the target's g.
+template <bool ENTROPY, bool BINARY>
+__device__ __forceinline__ float grad_of(const RowGrad &q, float x) {
+    const float d = BINARY ? __builtin_fmaf(x, kLog2e, -q.r) : x - q.r;
+    const float p = BINARY ? __builtin_amdgcn_exp2f(d) : exp_of(d - q.ln);
+    return p * (ENTROPY ? __builtin_fmaf(-q.h, __builtin_fmaxf(d, kFar), q.f) : q.f);
+}
+template <int TYPE, bool ENTROPY, bool BINARY>
+__device__ __forceinline__ u32x4 grad_piece(const RowGrad &q, const u32x4 &piece) {
     float x[kPer<TYPE>];
     values_of<TYPE>(piece, x);
-    if (target < kPer<TYPE>) {
 #pragma unroll
-        for (uint32_t e = 0; e < kPer<TYPE>; ++e)
-            if (target == e)
-                found(x[e]);
-    }
-#pragma unroll
-    for (uint32_t e = 0; e < kPer<TYPE>; ++e) {
-        const float d = BINARY ? __builtin_fmaf(x[e], kLog2e, -q.r) : x[e] - q.r;
-        const float p = BINARY ? __builtin_amdgcn_exp2f(d) : exp_of(d - q.ln);
-        float f = q.f;
-        if (ENTROPY)
-            f = __builtin_fmaf(-q.h, __builtin_fmaxf(d, kFar), f);
-        x[e] = p * f;
-    }
-    if (target < kPer<TYPE>) {
-#pragma unroll
-        for (uint32_t e = 0; e < kPer<TYPE>; ++e)
-            x[e] += target == e ? q.g : 0.0f;
-    }
+    for (uint32_t e = 0; e < kPer<TYPE>; ++e)
+        x[e] = grad_of<ENTROPY, BINARY>(q, x[e]);
     return piece_of<TYPE>(x);
+}
+// The target's, from its logit, over what its piece's lane has stored there.
+template <int TYPE, bool ENTROPY>
+__device__ __forceinline__ void store_target(const RowGrad &q, char *dx, float x) {
+    const float y =
+        q.g + (q.binary ? grad_of<ENTROPY, true>(q, x) : grad_of<ENTROPY, false>(q, x));
+    if constexpr (TYPE == kBf16)
+        reinterpret_cast<uint16_t *>(dx)[q.target] = (uint16_t)bf16_pair(y, y);
+    else
+        reinterpret_cast<float *>(dx)[q.target] = y;
 }
 
 // Elements `from` .. `to` of a piece, whose first would lie at p.
@@ -697,6 +798,14 @@ __global__ __launch_bounds__(kThreads) void backward_kernel(GradArgs a) {
     const uint32_t first = start + threadIdx.x % LANES * kPer<TYPE>;
     const char *x = row_of<TYPE>(a.x, row);
     char *dx = row_of<TYPE>(a.dx, row);
+    // the target's logit, by the lane that has its piece; dx may be x
+    const int64_t target = a.targets[row];
+    const bool mine = target >= 0 && target < (int64_t)a.vocab &&
+                      (uint32_t)target - start < LANES * BATCH &&
+                      ((uint32_t)target - first) % (LANES * kPer<TYPE>) < kPer<TYPE>;
+    float logit = 0.0f;
+    if (mine)
+        logit = value_at<TYPE>(x, (uint32_t)target);
     const auto pass = [&](auto is_whole) {
         // the same for a wave: its part has all its columns
         constexpr bool kWhole = decltype(is_whole)::value;
@@ -723,7 +832,7 @@ __global__ __launch_bounds__(kThreads) void backward_kernel(GradArgs a) {
         }
         const float lse = a.lse[row];
         RowGrad q = row_grad(lse, 0.0f, lse == -infinity(), ENTROPY ? a.entropies[row] : 0.0f,
-                             a.dlog_probs[row], ENTROPY ? a.dentropies[row] : 0.0f, a.targets[row],
+                             a.dlog_probs[row], ENTROPY ? a.dentropies[row] : 0.0f, target,
                              a.vocab);
         if (__builtin_fabsf(lse) < kOrdinary) {
             // e^(x - lse) = 2^(x c - k) 2^-lo, with lse c = k + lo exactly
@@ -736,8 +845,7 @@ __global__ __launch_bounds__(kThreads) void backward_kernel(GradArgs a) {
                 const uint32_t col = first + b * LANES * kPer<TYPE>;
                 if (!kWhole && col >= a.vocab)
                     continue;
-                const u32x4 w = grad_piece<TYPE, ENTROPY, decltype(binary)::value>(
-                    q, c[b], q.target - col, [](float) {});
+                const u32x4 w = grad_piece<TYPE, ENTROPY, decltype(binary)::value>(q, c[b]);
                 char *p = dx + col * (size_t)kSize<TYPE>;
                 if (kWhole || col + kPer<TYPE> <= a.vocab)
                     st_nt_at<u32x4, kSize<TYPE>>(p, w);
@@ -749,6 +857,8 @@ __global__ __launch_bounds__(kThreads) void backward_kernel(GradArgs a) {
             each(std::true_type{});
         else
             each(std::false_type{});
+        if (mine && q.target != kNoTarget)
+            store_target<TYPE, ENTROPY>(q, dx, logit);
     };
     if (LANES == 64 && start + LANES * BATCH <= a.vocab)
         pass(std::true_type{});
@@ -778,79 +888,91 @@ __global__ __launch_bounds__(group_of(THREADS), train_waves(THREADS)) void train
         a.f.base + (size_t)blockIdx.x * (kGroup / THREADS) + row_in_group<THREADS>();
     if (THREADS < kThreads && row >= a.f.rows)
         return;
-    const char *x = row_of<TYPE>(a.f.x, row);
+    const Line<TYPE, THREADS> line{row_of<TYPE>(a.f.x, row), vocab, vocab};
     char *dx = row_of<TYPE>(a.dx, row);
+    constexpr uint32_t W = THREADS * kPer<TYPE>;
     u32x4 c[C];
 #pragma unroll
     for (uint32_t b = 0; b < C; ++b)
-        c[b] = load_piece<TYPE>(x, (lane + b * THREADS) * kPer<TYPE>, vocab);
+        c[b] = line.load(b * W, lane);
     const int64_t target = a.f.targets[row];
+    // the target's logit, by the lane that has its piece; dx may be x
+    const bool mine = target >= 0 && target < (int64_t)vocab &&
+                      (uint32_t)target % W / kPer<TYPE> == lane;
+    float logit = 0.0f;
+    if (mine)
+        logit = value_at<TYPE>(line.row, (uint32_t)target);
     const float g = a.dlog_probs[row], h = ENTROPY && a.dentropies ? a.dentropies[row] : 0.0f;
-    // (and the places of the pieces are not kept either)
-    hold(lane);
     float top = kLowest;
+    // (the places of the pieces are not kept either)
+    hold(lane);
 #pragma unroll
     for (uint32_t b = 0; b < C; ++b) {
-        mask_end<TYPE>(c[b], (lane + b * THREADS) * kPer<TYPE>, vocab, vocab);
+        hold(c[b]);
+        if (line.any(b * W)) {
+            line.mask_end(c[b], b * W, lane);
+            float v[kPer<TYPE>];
+            values_of<TYPE>(c[b], v);
+            top = __builtin_fmaxf(top, max_of(v));
+        }
+    }
+    Sums two{reference<true>(top), 0.0f, 0.0f};
+#pragma unroll
+    for (uint32_t b = 0; b < C; ++b) {
+        hold(c[b]);
+        if (!line.any(b * W))
+            continue;
         float v[kPer<TYPE>];
         values_of<TYPE>(c[b], v);
-        top = __builtin_fmaxf(top, max_of(v));
+        add<ENTROPY, true>(two, v);
     }
-    const auto sums = [&](auto binary) {
-        constexpr bool kBinary = decltype(binary)::value;
-        Sums t{reference<kBinary>(top), 0.0f, 0.0f};
-#pragma unroll
-        for (uint32_t b = 0; b < C; ++b) {
-            float v[kPer<TYPE>];
-            hold(c[b]);
-            values_of<TYPE>(c[b], v);
-            add<ENTROPY, kBinary>(t, v);
-        }
-        return join_lanes<THREADS, kBinary>(t, shared[kBinary]);
-    };
-    const Sums two = sums(std::true_type{});
+    two = join_lanes<THREADS, true>(two, shared[0]);
     const bool binary = held(two);
-    const Sums t = binary ? natural(two) : sums(std::false_type{});
+    Sums t;
+    if (binary)
+        t = natural(two);
+    else  // the row is read again, piece by piece
+        t = join_lanes<THREADS, false>(
+            sums_of<TYPE, THREADS, kPer<TYPE>, ENTROPY, false>(line, 0, lane), shared[1]);
     const float ln = logf(t.s);
     if (lane == 0) {
         store_sums(a.f, row, t, ln);
-        // the lane that holds the target's logit stores the others: dx may be x
         if (target < 0)
             a.f.log_probs[row] = 0.0f;
         else if (target >= (int64_t)vocab)
             a.f.log_probs[row] = not_a_number();
-        else if (t.s == 0.0f)
-            a.f.log_probs[row] = -infinity();
     }
+    if (mine)
+        a.f.log_probs[row] = log_prob(logit, t, ln);
     RowGrad q = row_grad(t.r, ln, t.s == 0.0f, ln - t.w / t.s, g, h, target, vocab);
+    const auto store = [&](uint32_t first, const u32x4 &piece, auto is_binary) {
+        const uint32_t col = first + lane * kPer<TYPE>;
+        if (col >= vocab)
+            return;
+        const uint32_t at = place_of<TYPE>(col, vocab);
+        const u32x4 w = grad_piece<TYPE, ENTROPY, decltype(is_binary)::value>(q, piece);
+        char *p = dx + at * (size_t)kSize<TYPE>;
+        if (at == col)
+            st_nt_at<u32x4, kSize<TYPE>>(p, w);
+        else
+            store_some<TYPE>(p, w, col - at, kPer<TYPE>);
+    };
     if (binary) {
         const float off = (float)((double)two.r * (1.0 / (double)kLog2e) - (double)t.r);
         make_binary(q, two.r, 1.0f / two.s, -off);
-    }
-    hold(lane);
-    const auto each = [&](auto is_binary) {
+        hold(lane);
 #pragma unroll
         for (uint32_t b = 0; b < C; ++b) {
-            const uint32_t col = (lane + b * THREADS) * kPer<TYPE>;
             hold(c[b]);
-            if (col >= vocab)
-                continue;
-            const uint32_t at = place_of<TYPE>(col, vocab);
-            // (the target is in this piece if it is within its columns, not if it is before them)
-            const u32x4 w = grad_piece<TYPE, ENTROPY, decltype(is_binary)::value>(
-                q, c[b], q.target - col < kPer<TYPE> ? q.target - at : kNoTarget,
-                [&](float v) { a.f.log_probs[row] = log_prob(v, t, ln); });
-            char *p = dx + at * (size_t)kSize<TYPE>;
-            if (at == col)
-                st_nt_at<u32x4, kSize<TYPE>>(p, w);
-            else
-                store_some<TYPE>(p, w, col - at, kPer<TYPE>);
+            if (line.any(b * W))
+                store(b * W, c[b], std::true_type{});
         }
-    };
-    if (q.binary)
-        each(std::true_type{});
-    else
-        each(std::false_type{});
+    } else {
+        for (uint32_t first = 0; line.any(first); first += W)
+            store(first, line.load(first, lane), std::false_type{});
+    }
+    if (mine && q.target != kNoTarget)
+        store_target<TYPE, ENTROPY>(q, dx, logit);
 }
 
 // Rows of less than a piece: a lane a row, forward, backward or both.
@@ -929,27 +1051,36 @@ struct Cut {
     uint32_t splits, slice;
 };
 
-// With `top` a slice is 1, 2 or 4 chunks a lane of a workgroup: the least that makes
-// no more than kFill workgroups.
-constexpr size_t kFill = 1024;
+// Rows that leave CUs without one, and the longest that a workgroup of 1024 then takes.
+constexpr size_t kFew = 256;
+constexpr uint32_t kOneGroup = 1024 * 32;
+
+// Columns of a batch of a workgroup: with the most probable tokens, and without.
+constexpr uint32_t kTopBatch = kThreads * 32, kTopSlice = kThreads * 8;
+constexpr size_t kFill = 1024;  // workgroups that keep all CUs busy
+uint32_t slices(uint32_t n, uint32_t slice) { return (n + slice - 1) / slice; }
+
 Cut cut_of(size_t rows, uint32_t vocab, uint32_t top) {
+    const uint32_t n = vocab;
+    if (rows >= kFill / 2)
+        return {1, n};
+    const size_t most = kFill / (rows ? rows : 1);
     if (top) {
-        uint32_t slice = kThreads * 8;
-        while (slice < kThreads * 8 * 4 &&
-                   (rows * ((vocab + slice - 1) / slice) > kFill ||
-                (size_t)((vocab + slice - 1) / slice) * top > kThreads * kTopPerLane / 2))
-            slice *= 2;
-        return {(vocab + slice - 1) / slice, slice};
+        // one workgroup goes through a batch in less time than a second launch takes
+        if (n <= kTopBatch)
+            return {1, n};
+        const uint32_t keys = kThreads * kJoined / top;  // slices whose keys can be joined
+        if (slices(n, kTopSlice) <= most && slices(n, kTopSlice) <= keys)
+            return {slices(n, kTopSlice), kTopSlice};
+        uint32_t splits = most < keys ? (uint32_t)most : keys;
+        const uint32_t slice = slices(slices(n, splits), kTopBatch) * kTopBatch;
+        return {slices(n, slice), slice};
     }
-    const uint32_t least = kThreads * 8;
-    if (vocab <= 2 * least || rows >= kFill / 2)
-        return {1, vocab};
-    uint32_t splits = (uint32_t)(kFill / (rows ? rows : 1));
-    const uint32_t most = (vocab + least - 1) / least;
-    splits = splits < most ? splits : most;
-    uint32_t slice = (vocab + splits - 1) / splits;
-    slice = (slice + least - 1) / least * least;
-    return {(vocab + slice - 1) / slice, slice};
+    constexpr uint32_t kLeast = kThreads * 8;
+    if (n <= kOneGroup)
+        return {1, n};
+    const uint32_t slice = slices(slices(n, (uint32_t)most), kLeast) * kLeast;
+    return {slices(n, slice), slice};
 }
 
 // Rows a launch, so that its work-items stay below 2^31.
@@ -1009,29 +1140,28 @@ void launch_short(const LogProbsArgs &args, hipStream_t stream) {
 template <int TYPE>
 void top_typed(const LogProbsArgs &args, const Cut &cut, hipStream_t stream) {
     RowArgs a = row_args(args, cut);
-    const uint32_t per_lane = cut.slice / kThreads;
-    // lanes that have a key in every slice, the last one's aside
-    const uint32_t columns = cut.splits > 1 ? cut.slice : args.vocab;
-    a.group = group_lanes((columns + kPer<TYPE> - 1) / kPer<TYPE> < kThreads
-                              ? (columns + kPer<TYPE> - 1) / kPer<TYPE>
-                              : kThreads,
-                          args.top);
-    size_t lds = list_keys(per_lane, a.group, args.top) * sizeof(Key);
-    for_rows(a, cut.splits, 1, [&](unsigned grid) {
-        if (per_lane == 8)
-            hipLaunchKernelGGL((top_kernel<TYPE, 8>), dim3(grid), dim3(kThreads), lds, stream, a);
-        else if (per_lane == 16)
-            hipLaunchKernelGGL((top_kernel<TYPE, 16>), dim3(grid), dim3(kThreads), lds, stream, a);
-        else
-            hipLaunchKernelGGL((top_kernel<TYPE, 32>), dim3(grid), dim3(kThreads), lds, stream, a);
-    });
+    const auto launch = [&](auto threads, auto each) {
+        constexpr uint32_t kLanes = decltype(threads)::value, kEach = decltype(each)::value;
+        a.room = list_keys(kEach, args.top);
+        for_rows(a, cut.splits, 1, [&](unsigned grid) {
+            hipLaunchKernelGGL((top_kernel<TYPE, kLanes, kEach>), dim3(grid), dim3(kLanes),
+                               (a.room + kRankStep) * sizeof(Key), stream, a);
+        });
+    };
+    // a wave a row where that is enough lanes for it
+    const uint32_t n = cut.splits > 1 ? cut.slice : args.vocab;
+    if (n <= 64 * 16)
+        launch(Number<64>{}, Number<16>{});
+    else if (n <= kTopSlice)
+        launch(Number<kThreads>{}, Number<8>{});
+    else
+        launch(Number<kThreads>{}, Number<32>{});
     if (cut.splits == 1)
         return;
-    const uint32_t keys = cut.splits * args.top;
-    a.group = group_lanes(keys < kThreads ? keys : kThreads, args.top);
-    lds = list_keys((keys + kThreads - 1) / kThreads, a.group, args.top) * sizeof(Key);
+    a.room = list_keys(kJoined, args.top);
     for_rows(a, 1, 1, [&](unsigned grid) {
-        hipLaunchKernelGGL(top_join_kernel<TYPE>, dim3(grid), dim3(kThreads), lds, stream, a);
+        hipLaunchKernelGGL(top_join_kernel<TYPE>, dim3(grid), dim3(kThreads),
+                           (a.room + kRankStep) * sizeof(Key), stream, a);
     });
 }
 
@@ -1062,6 +1192,8 @@ void forward_typed(const LogProbsArgs &args, hipStream_t stream) {
         launch(Number<16>{}, Number<32>{});
     else if (args.vocab <= 64 * 32)
         launch(Number<64>{}, Number<32>{});
+    else if (args.vocab > kTopBatch && args.vocab <= kOneGroup && args.rows < kFill / 2)
+        launch(Number<1024>{}, Number<32>{});
     else
         launch(Number<256>{}, Number<32>{});
     if (cut.splits > 1)
@@ -1077,7 +1209,7 @@ void backward_typed(const LogProbsArgs &args, hipStream_t stream) {
     GradArgs a = grad_args(args);
     const auto launch = [&](auto lanes, auto batch) {
         constexpr uint32_t kLanes = decltype(lanes)::value, kIn = decltype(batch)::value;
-        a.per_row = (a.vocab + kLanes * kIn - 1) / (kLanes * kIn);
+        a.per_row = slices(a.vocab, kLanes * kIn);
         for_rows(a, a.per_row, kThreads / kLanes, [&](unsigned grid) {
             if (args.dentropies)
                 hipLaunchKernelGGL((backward_kernel<TYPE, kLanes, kIn, true>), dim3(grid),
@@ -1118,27 +1250,35 @@ constexpr uint32_t kMostTrain = 1024 * 16 * kPer<TYPE>;
 template <int TYPE>
 void train_typed(const LogProbsArgs &args, hipStream_t stream) {
     const uint32_t v = args.vocab;
-    constexpr uint32_t kLong = 16 * kPer<TYPE>;  // elements of 64 registers
+    constexpr uint32_t kHalf = 8 * kPer<TYPE>;  // elements of 32 registers
+    const bool few = args.rows <= kFew;
     if (v < kPer<TYPE>)
         launch_short<TYPE, true, true>(args, stream);
     else if (v <= 16 * 8)
         launch_train<TYPE, 16, 8>(args, stream);
     else if (v <= 16 * 32)
         launch_train<TYPE, 16, 32>(args, stream);
-    else if (v <= 64 * 16)
-        launch_train<TYPE, 64, 16>(args, stream);
     else if (v <= 64 * 32)
         launch_train<TYPE, 64, 32>(args, stream);
     else if (v <= 256 * 32)
         launch_train<TYPE, 256, 32>(args, stream);
     else if (v <= 512 * 32)
         launch_train<TYPE, 512, 32>(args, stream);
-    else if (v <= 512 * kLong / 2)
-        launch_train<TYPE, 512, kLong / 2>(args, stream);
-    else if (v <= 512 * kLong)
-        launch_train<TYPE, 512, kLong>(args, stream);
+    else if (v <= 512 * kHalf && !few)
+        launch_train<TYPE, 512, kHalf>(args, stream);
+    else if (v <= 1024 * 32)
+        launch_train<TYPE, 1024, 32>(args, stream);
+    else if (v <= 1024 * kHalf)
+        launch_train<TYPE, 1024, kHalf>(args, stream);
     else
-        launch_train<TYPE, 1024, kLong>(args, stream);
+        launch_train<TYPE, 1024, 2 * kHalf>(args, stream);
+}
+
+// Do a row's logits fit a workgroup's registers?  Few rows that would take all of a CU's are
+// cut into slices instead, as the two passes do.
+template <int TYPE>
+bool one_pass(const LogProbsArgs &args) {
+    return args.vocab <= (args.rows <= kFew ? 1024 * 64 : kMostTrain<TYPE>);
 }
 
 }  // namespace
@@ -1170,7 +1310,7 @@ hipError_t launch_log_probs_backward(const LogProbsArgs &a, int type, hipStream_
 }
 
 hipError_t launch_log_probs_train(const LogProbsArgs &a, int type, hipStream_t stream) {
-    if (a.vocab > (type == kBf16 ? kMostTrain<kBf16> : kMostTrain<kF32>)) {
+    if (!(type == kBf16 ? one_pass<kBf16>(a) : one_pass<kF32>(a))) {
         const hipError_t e = launch_log_probs_forward(a, type, stream);
         return e == hipSuccess ? launch_log_probs_backward(a, type, stream) : e;
     }

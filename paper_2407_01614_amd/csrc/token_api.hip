@@ -236,6 +236,7 @@ zpp_status rotary(const zpp_heads *x, const zpp_heads *out, const zpp_heads *k,
 // Log probabilities
 // --------------------------------------------------------------------------
 constexpr size_t kMostVocab = (size_t)1 << 31;  // exclusive
+static_assert(zpp::kMostTop == ZPP_MAX_TOP);
 
 // Checks that the calls share, and the arguments that they have in common.
 zpp::LogProbsArgs log_probs_args(Arguments &args, const zpp_matrix *x, size_t rows, size_t vocab,

@@ -42,6 +42,7 @@ struct LogProbsArgs {
     size_t rows;
     uint32_t vocab, top;
 };
+constexpr uint32_t kMostTop = 64;  // ZPP_MAX_TOP
 size_t log_probs_workspace(size_t rows, size_t vocab, uint32_t top);
 hipError_t launch_log_probs_forward(const LogProbsArgs &a, int type, hipStream_t stream);
 hipError_t launch_log_probs_backward(const LogProbsArgs &a, int type, hipStream_t stream);
