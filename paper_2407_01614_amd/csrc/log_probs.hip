@@ -413,13 +413,16 @@ __global__ __launch_bounds__(64) void join_kernel(RowArgs a) {
 // of the same order, and below it its column, inverted, so that of equals the lower
 // comes first and no two keys are alike.
 //
-// The lanes that share a row go through it in batches.  In the first, the `top`-th
-// largest of the lanes' largest values is a bound that at least `top` elements reach, and
-// few more; what reaches it, there and in later batches, is listed in LDS, and at the end
-// each listed key's rank is counted.  A list that overflows (values that rise along the
-// row, or many equal ones) is cut to its `top` largest, which raises the bound, and the
-// batch goes through again with the bound of its own lanes' largest keys, which no more
-// than `top` lanes' elements reach.
+// The lanes that share a row go through it in batches.  After the first, and each time
+// their number has doubled, the `top`-th largest of the lanes' largest values so far is a
+// bound that at least `top` elements reach, and few more; what reaches it from then on is
+// listed in LDS as each wave finds it, and at the end each listed key's rank is counted.  Where the list overflows
+// (values that rise along the row, or many equal ones), the row goes through again, a batch at
+// a time: the list is cut to its `top` largest, which raises the bound, and where a batch
+// still has too many, to those from its lanes' `top`-th largest key on, which no more than
+// `top` lanes have.
+// Masked elements, -Inf, are not listed: they follow in the order of their columns where a
+// row has fewer others than asked for.
 // --------------------------------------------------------------------------
 typedef unsigned long long Key;
 typedef Key KeyPair __attribute__((ext_vector_type(2)));
@@ -455,13 +458,12 @@ struct Selection {
 // The largest number of bits from LOW on that `top` of all lanes' values reach; its lowest
 // bits stay 0 where no more than kSpare lanes beside them do.  The same in all lanes.
 template <uint32_t THREADS, int LOW, class T>
-__device__ __forceinline__ T bound_of(const Selection<THREADS> &s, uint32_t top) {
+__device__ __forceinline__ T bound_of(const T *values, uint32_t top) {
     constexpr uint32_t kEach = THREADS / 64;
-    const T *values = reinterpret_cast<const T *>(s.lanes) + threadIdx.x % 64 * kEach;
     T v[kEach], bound = 0;
 #pragma unroll
     for (uint32_t j = 0; j < kEach; ++j)
-        v[j] = values[j];
+        v[j] = values[threadIdx.x % 64 * kEach + j];
     for (int bit = 8 * (int)sizeof(T) - 1; bit >= LOW; --bit) {
         const T trial = bound | (T)1 << bit;
         uint32_t n = 0;
@@ -504,40 +506,53 @@ struct Listed {
     float least = 0.0f;  // the bound
 };
 
+// The bound after a batch, from a lane's largest value `m`; `turn`: how many bounds there
+// were before (each second one in the same place, which all have read then).  LOW: bits of a
+// value that are 0, or left out.
+template <uint32_t THREADS, int LOW>
+__device__ __forceinline__ float value_bound(Selection<THREADS> &s, uint32_t top, float m,
+                                             uint32_t turn) {
+    uint32_t *values = reinterpret_cast<uint32_t *>(s.lanes) + turn % 2 * THREADS;
+    values[threadIdx.x] = order_of(m);
+    if (turn == 0 && threadIdx.x == 0)
+        s.counts[0] = 0;
+    __syncthreads();
+    const uint32_t order = bound_of<THREADS, LOW, uint32_t>(values, top);
+    // (below the finite numbers: fewer than `top` lanes have one)
+    return order < 0x00800000u ? kLowest : ordered(order);
+}
+
+// The lane's keys from `from` on into the list, as far as there is room.
+template <class Each>
+__device__ __forceinline__ void push(Key *list, uint32_t n, uint32_t *count, uint32_t room, Key from,
+                                     Each &&each) {
+    uint32_t mine = 0;
+    each([&](float x, uint32_t col) { mine += !from || key_of(x, col) >= from; });
+    uint32_t at = n + atomicAdd(count, mine);
+    each([&](float x, uint32_t col) {
+        const Key k = key_of(x, col);
+        if (!from || k >= from) {
+            if (at < room)
+                list[at] = k;
+            ++at;
+        }
+    });
+}
+
 // A batch's elements, largest `m`, taken into the list.  each(f) calls f(value, column) with
-// each of the lane's whose value reaches the bound.  LOW: bits of a value that are 0, or
-// left out of the bound.
+// each of the lane's whose value reaches the bound.
 template <uint32_t THREADS, int LOW, class Each>
 __device__ __forceinline__ void take(Selection<THREADS> &s, Key *list, uint32_t room, uint32_t top,
                                      bool first, float m, Listed &l, Each &&each) {
-    const auto bound = [&](uint32_t order) {
-        // (below -Inf in this order: fewer than `top` lanes have a number)
-        l.least = order < 0x007FFFFFu ? -infinity() : ordered(order);
-    };
-    if (first) {
-        reinterpret_cast<uint32_t *>(s.lanes)[threadIdx.x] = order_of(m);
-        if (threadIdx.x == 0)
-            s.counts[0] = 0;
-        __syncthreads();
-        bound(bound_of<THREADS, LOW, uint32_t>(s, top));
-    }
-    // what is listed: keys from `from` on; how many those are
-    const auto push = [&](Key from) {
+    if (first)
+        l.least = value_bound<THREADS, LOW>(s, top, m, 0);
+    const auto listed = [&](Key from) {
         uint32_t *count = s.counts + l.round % 3;
         l.round += 1;
         if (threadIdx.x == 0)
             s.counts[l.round % 3] = 0;  // last read before the barrier before this
-        if (m >= l.least) {
-            uint32_t mine = 0;
-            each([&](float x, uint32_t col) { mine += key_of(x, col) >= from; });
-            uint32_t at = l.n + atomicAdd(count, mine);
-            each([&](float x, uint32_t col) {
-                const Key k = key_of(x, col);
-                if (k >= from && at < room)
-                    list[at] = k;
-                at += k >= from;
-            });
-        }
+        if (m >= l.least)
+            push(list, l.n, count, room, from, each);
         __syncthreads();
         return *count;
     };
@@ -550,7 +565,7 @@ __device__ __forceinline__ void take(Selection<THREADS> &s, Key *list, uint32_t 
         l.n = top;
         l.least = value_of(list[top - 1]);
     };
-    uint32_t n = push(0);
+    uint32_t n = listed(0);
     if (l.n + n > room) {
         if (l.n > top)
             cut();
@@ -562,27 +577,45 @@ __device__ __forceinline__ void take(Selection<THREADS> &s, Key *list, uint32_t 
             });
         s.lanes[threadIdx.x] = best;
         __syncthreads();
-        const Key from = bound_of<THREADS, 0, Key>(s, top);
-        n = push(from ? from : 1);
+        const Key from = bound_of<THREADS, 0, Key>(s.lanes, top);
+        n = listed(from ? from : 1);
     }
     l.n += n;
     if (l.n > room / 2 && l.n > top)
         cut();
 }
 
-// A row's (or slice's) list's end: write(rank, key) of its `top` largest, and of ranks that no
-// number is left for, key 0.
-template <uint32_t THREADS, class F>
-__device__ __forceinline__ void write_top(Key *list, uint32_t n, uint32_t top, F &&write) {
-    rank_list<THREADS>(list, n, top, write);
-    for (uint32_t i = n + threadIdx.x; i < top; i += THREADS)
-        write(i, (Key)0);
+// The ranks that a row's list leaves, by the first wave: its masked elements, by column.
+template <int TYPE>
+__device__ __forceinline__ void store_masked(const RowArgs &a, size_t row, uint32_t n,
+                                             const Sums &t) {
+    const char *x = row_of<TYPE>(a.x, row);
+    for (uint32_t col = threadIdx.x; n < a.top; col += 64) {
+        // (a row of NaN has no order: any tokens)
+        const bool is = t.s != t.s || (col < a.vocab && value_at<TYPE>(x, col) == -infinity());
+        const uint64_t all = __ballot(is);
+        const uint32_t rank = n + __builtin_amdgcn_mbcnt_hi(
+                                      (uint32_t)(all >> 32),
+                                      __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0));
+        if (is && rank < a.top) {
+            a.top_ids[row * a.top + rank] = (int32_t)(t.s != t.s ? rank : col);
+            a.top_log_probs[row * a.top + rank] = t.s != t.s ? t.s : -infinity();
+        }
+        n += (uint32_t)__builtin_popcountll(all);
+        if (col - threadIdx.x >= a.vocab)
+            break;  // not reached: a row has as many of both as it is long
+    }
 }
-__device__ __forceinline__ void store_top(const RowArgs &a, size_t row, uint32_t rank, Key k,
+// A row's most probable tokens from its list.
+template <int TYPE, uint32_t THREADS>
+__device__ __forceinline__ void store_top(const RowArgs &a, size_t row, Key *list, uint32_t n,
                                           const Sums &t, float ln) {
-    // without a key (a row of NaN): some token, and no number
-    a.top_ids[row * a.top + rank] = k ? (int32_t)column_of(k) : (int32_t)rank;
-    a.top_log_probs[row * a.top + rank] = k ? log_prob(value_of(k), t, ln) : not_a_number();
+    rank_list<THREADS>(list, n, a.top, [&](uint32_t rank, Key k) {
+        a.top_ids[row * a.top + rank] = (int32_t)column_of(k);
+        a.top_log_probs[row * a.top + rank] = log_prob(value_of(k), t, ln);
+    });
+    if (n < a.top && threadIdx.x < 64)
+        store_masked<TYPE>(a, row, n, t);
 }
 
 // A row, or a slice of one: sums and its most probable tokens.  E elements a lane in a batch.
@@ -599,15 +632,14 @@ __global__ __launch_bounds__(THREADS) void top_kernel(RowArgs a) {
     Target target{};
     if (lane == 0 && a.splits == 1)
         target = target_of<TYPE>(a, row);
-    Sums t = no_sums();
-    float top = kLowest;
-    Listed listed;
-    for (uint32_t i = begin; line.any(i); i += kPieces * W) {
-        u32x4 c[kPieces];
+    // The pieces of the batch from column i on, and the largest of their values.
+    u32x4 c[kPieces];
+    float x[kPieces][kPer<TYPE>];
+    const auto load = [&](uint32_t i) {
+        float m = -infinity();
 #pragma unroll
         for (uint32_t b = 0; b < kPieces; ++b)
             c[b] = line.load(i + b * W, lane);
-        float x[kPieces][kPer<TYPE>], m = -infinity();
 #pragma unroll
         for (uint32_t b = 0; b < kPieces; ++b)
             if (line.any(i + b * W)) {
@@ -615,26 +647,41 @@ __global__ __launch_bounds__(THREADS) void top_kernel(RowArgs a) {
                 values_of<TYPE>(c[b], x[b]);
                 m = __builtin_fmaxf(m, max_of(x[b]));
             }
-        top = __builtin_fmaxf(top, m);
-        t = joined<true>(t, reference<true>(top));
+        return m;
+    };
+    Listed listed;
+    const auto each_of = [&](uint32_t i) {
+        return [&, i](auto &&f) {
+#pragma unroll
+            for (uint32_t b = 0; b < kPieces; ++b)
+                if (line.any(i + b * W)) {
+                    const uint32_t col = i + (b * THREADS + lane) * kPer<TYPE>;
+                    const uint32_t at = place_of<TYPE>(col, a.vocab);
+#pragma unroll
+                    for (uint32_t e = 0; e < kPer<TYPE>; ++e)
+                        if (x[b][e] >= listed.least)
+                            f(x[b][e], at + e);
+                }
+        };
+    };
+    constexpr int kLow = TYPE == kBf16 ? 16 : 12;
+    Sums t = no_sums();
+    float most = -infinity();
+    uint32_t batches = 0, turn = 0;
+    for (uint32_t i = begin; line.any(i); i += kPieces * W) {
+        const float m = load(i);
+        most = __builtin_fmaxf(most, m);
+        t = joined<true>(t, reference<true>(__builtin_fmaxf(most, kLowest)));
 #pragma unroll
         for (uint32_t b = 0; b < kPieces; ++b)
             if (line.any(i + b * W))
                 add<true, true>(t, x[b]);
-        take<THREADS, TYPE == kBf16 ? 16 : 12>(
-            selection, list, a.room, a.top, i == begin, m, listed, [&](auto &&f) {
-#pragma unroll
-                for (uint32_t b = 0; b < kPieces; ++b)
-                    if (line.any(i + b * W)) {
-                        const uint32_t col = i + (b * THREADS + lane) * kPer<TYPE>;
-                        const uint32_t at = place_of<TYPE>(col, a.vocab);
-                        const uint32_t skip = line.skip(i + b * W, lane);
-#pragma unroll
-                        for (uint32_t e = 0; e < kPer<TYPE>; ++e)
-                            if (x[b][e] >= listed.least && e >= skip)
-                                f(x[b][e], at + e);
-                    }
-            });
+        // (the second batch lists less than a bound costs)
+        if (batches != 1 && (batches & (batches - 1)) == 0)
+            listed.least = value_bound<THREADS, kLow>(selection, a.top, most, turn++);
+        ++batches;
+        if (m >= listed.least)
+            push(list, 0, selection.counts, a.room, 0, each_of(i));
     }
     t = join_lanes<THREADS, true>(t, shared[0]);
     if (held(t))
@@ -649,13 +696,24 @@ __global__ __launch_bounds__(THREADS) void top_kernel(RowArgs a) {
         else
             a.partials[row * a.splits + split] = t;
     }
+    __syncthreads();
+    listed.n = selection.counts[0];
+    if (listed.n > a.room) {
+        __syncthreads();  // the count has been read
+        listed.n = 0;
+        for (uint32_t i = begin; line.any(i); i += kPieces * W) {
+            const float m = load(i);
+            take<THREADS, kLow>(selection, list, a.room, a.top, i == begin, m, listed, each_of(i));
+        }
+    }
+    if (a.splits == 1) {
+        store_top<TYPE, THREADS>(a, row, list, listed.n, t, ln);
+        return;
+    }
     Key *out = a.keys + (row * a.splits + split) * a.top;
-    write_top<THREADS>(list, listed.n, a.top, [&](uint32_t rank, Key k) {
-        if (a.splits == 1)
-            store_top(a, row, rank, k, t, ln);
-        else
-            out[rank] = k;
-    });
+    rank_list<THREADS>(list, listed.n, a.top, [&](uint32_t rank, Key k) { out[rank] = k; });
+    for (uint32_t i = listed.n + lane; i < a.top; i += THREADS)
+        out[i] = 0;
 }
 
 // The slices joined: sums, and the most probable of the slices' most probable.
@@ -690,9 +748,7 @@ __global__ __launch_bounds__(kThreads) void top_join_kernel(RowArgs a) {
                 if (k[j] && value_of(k[j]) >= listed.least)
                     f(value_of(k[j]), column_of(k[j]));
         });
-    write_top<kThreads>(list, listed.n, a.top, [&](uint32_t rank, Key key) {
-        store_top(a, row, rank, key, t, ln);
-    });
+    store_top<TYPE, kThreads>(a, row, list, listed.n, t, ln);
 }
 
 // --------------------------------------------------------------------------
@@ -1148,9 +1204,9 @@ void top_typed(const LogProbsArgs &args, const Cut &cut, hipStream_t stream) {
                                (a.room + kRankStep) * sizeof(Key), stream, a);
         });
     };
-    // a wave a row where that is enough lanes for it
+    // a wave a row of a batch, or of two where there are enough rows
     const uint32_t n = cut.splits > 1 ? cut.slice : args.vocab;
-    if (n <= 64 * 16)
+    if (n <= 64 * 16 || (n <= kTopSlice && args.rows >= kFill))
         launch(Number<64>{}, Number<16>{});
     else if (n <= kTopSlice)
         launch(Number<kThreads>{}, Number<8>{});
