@@ -5,19 +5,31 @@
 // the 8-bit moments, so a block's largest values are reductions within the wave
 // and nothing is written twice.  Which tensor a tile belongs to is searched in the
 // table's levels, 64 first tiles at a time: one load a level, a ballot and a count.
+#include <type_traits>
+
 #include "zpp_act8.h"
 #include "zpp_adam.h"
+#include "zpp_chunk.h"
 #include "zpp_state8.h"
 #include "zpp_token.h"
 
 namespace zpp {
 namespace {
 
+// Tensors in the table are read as constants, and their arrays are in device memory: the
+// compiler cannot know either of pointers that it loads, and would load both through
+// vector registers and as generic ones.
+typedef const AdamEntry __attribute__((address_space(4))) Entry;
+template <class T>
+__device__ __forceinline__ T *device_array(T *p) {
+    return (T *)(T __attribute__((address_space(1))) *)p;
+}
+
 struct TableArgs {
     const AdamEntry *entries;
     const uint32_t *level[4];  // the search's levels, the widest last
     int levels;
-    uint32_t base;  // the launch's first tile
+    uint32_t base, tiles;  // the launch's
     AdamConsts c;
 };
 
@@ -28,7 +40,7 @@ __device__ __forceinline__ uint32_t tensor_of(const TableArgs &a, uint32_t tile)
         const uint32_t first = a.level[l][i * kSearch + (threadIdx.x & 63)];
         i = i * kSearch + (uint32_t)__builtin_popcountll(__ballot(first <= tile)) - 1;
     }
-    return i;
+    return __builtin_amdgcn_readfirstlane(i);
 }
 
 // Largest of the wave, the same in all lanes.
@@ -50,7 +62,7 @@ template <bool WHOLE>
 __device__ __forceinline__ uint32_t load_codes(const void *p, uint32_t i, uint32_t rest) {
     const uint8_t *b = reinterpret_cast<const uint8_t *>(p);
     if constexpr (WHOLE) {
-        return ld_nt_at<uint32_t, 1>(b + i);
+        return ld_at<uint32_t, 1>(b + i);
     } else {
         uint32_t w = 0;
 #pragma unroll
@@ -75,30 +87,43 @@ __device__ __forceinline__ f32x4 load_bf16(const void *p, uint32_t i, uint32_t r
     }
 }
 
-// Codes and scale of a block's first or second moments, four a lane; `inside`:
-// how many of the four are inside the block.
-template <int MOMENT, bool WHOLE>
-__device__ __forceinline__ void store_state(void *codes, float *scale, uint32_t i, uint32_t rest,
-                                            const f32x4 &x) {
-    float y[4];
-    uint32_t top = 0;
+// Codes and scales of a block's moments, four values a lane; `rest`: the block's values.
+// `m` or `v` may be missing (no codes).
+template <bool WHOLE>
+__device__ __forceinline__ void store_state(uint8_t *m_codes, float *m_scale, const f32x4 &m,
+                                            uint8_t *v_codes, float *v_scale, const f32x4 &v,
+                                            uint32_t i, uint32_t rest) {
+    uint32_t m_top = 0, v_top = 0;
 #pragma unroll
     for (uint32_t e = 0; e < 4; ++e) {
-        y[e] = MOMENT == 1 ? x[e] : __builtin_sqrtf(x[e]);
-        const uint32_t b = __float_as_uint(y[e]) & 0x7FFFFFFFu;
-        if (WHOLE || i + e < rest)
-            top = top > b ? top : b;
+        // a negative v has no root: with its sign it is past Inf
+        const uint32_t a = __float_as_uint(m[e]) & 0x7FFFFFFFu, b = __float_as_uint(v[e]);
+        if (WHOLE || i + e < rest) {
+            m_top = m_top > a ? m_top : a;
+            v_top = v_top > b ? v_top : b;
+        }
     }
-    top = max64(top);
-    const StateScale s = MOMENT == 1 ? first_scale(top) : second_scale(top);
-    uint32_t c[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        c[e] = MOMENT == 1 ? first_code(y[e], s) : second_code(y[e], s);
-    store4_i8<WHOLE>(reinterpret_cast<int8_t *>(codes), i, rest,
-                     pack_low_bytes(c[0], c[1], c[2], c[3]));
-    if ((threadIdx.x & 63) == 0)
-        *scale = s.scale;
+    m_top = m_codes ? max64(m_top) : 0;
+    v_top = v_codes ? max64(v_top) : 0;
+    // the root keeps the order, so the largest v has the largest
+    const uint32_t r_top = v_top >= 0x7F800000u
+                               ? v_top
+                               : __float_as_uint(__builtin_sqrtf(__uint_as_float(v_top)));
+    const StateScales s = state_scales(m_top, r_top);
+    const bool one = (threadIdx.x & 63) == 0;
+    if (m_codes) {
+        store4_i8<WHOLE>((int8_t *)m_codes, i, rest, s.m.inv == 0.0f ? 0 : first_codes(m, s.m));
+        if (one)
+            *m_scale = s.m.scale;
+    }
+    if (v_codes) {
+        uint32_t codes = 0;
+        if (s.r.inv != 0.0f)
+            codes = second_codes(v, v_top, s.r);
+        store4_i8<WHOLE>((int8_t *)v_codes, i, rest, codes);
+        if (one)
+            *v_scale = s.r.scale;
+    }
 }
 
 template <int MOMENT>
@@ -112,42 +137,65 @@ __device__ __forceinline__ f32x4 state_values(uint32_t codes, float scale) {
 }
 
 template <bool ADAMW, int STATE, int GRAD, bool WHOLE>
-__device__ __forceinline__ void step_tile(const AdamEntry &t, size_t base, uint32_t rest,
+__device__ __forceinline__ void step_tile(const Entry &t, size_t base, uint32_t rest,
                                           const AdamConsts &c) {
     const uint32_t i = 4 * (threadIdx.x & 63);
-    f32x4 P = load4<WHOLE>(t.p + base, i, rest), M, V, G;
     const size_t block = base / kAdamTile;
-    if constexpr (STATE == kF32) {
-        M = load4<WHOLE>((const float *)t.m + base, i, rest);
-        V = load4<WHOLE>((const float *)t.v + base, i, rest);
+    f32x4 P, M, V, G;
+    uint32_t m_codes, v_codes;
+    float m_scale, v_scale;
+    if constexpr (STATE == kI8) {
+        m_scale = device_array(t.m_scales)[block];
+        v_scale = device_array(t.v_scales)[block];
+        m_codes = load_codes<WHOLE>(device_array((uint8_t *)t.m) + base, i, rest);
+        v_codes = load_codes<WHOLE>(device_array((uint8_t *)t.v) + base, i, rest);
     } else {
-        const uint32_t m = load_codes<WHOLE>((const uint8_t *)t.m + base, i, rest);
-        const uint32_t v = load_codes<WHOLE>((const uint8_t *)t.v + base, i, rest);
-        M = state_values<1>(m, t.m_scales[block]);
-        V = state_values<2>(v, t.v_scales[block]);
+        M = load4<WHOLE>(device_array((float *)t.m) + base, i, rest);
+        V = load4<WHOLE>(device_array((float *)t.v) + base, i, rest);
     }
+    P = load4<WHOLE>(device_array(t.p) + base, i, rest);
     if constexpr (GRAD == kF32)
-        G = load4<WHOLE>((const float *)t.g + base, i, rest);
+        G = load4<WHOLE>(device_array((const float *)t.g) + base, i, rest);
     else
-        G = load_bf16<WHOLE>((const uint16_t *)t.g + base, i, rest);
+        G = load_bf16<WHOLE>(device_array((const uint16_t *)t.g) + base, i, rest);
+    if constexpr (STATE == kI8) {
+        M = state_values<1>(m_codes, m_scale);
+        V = state_values<2>(v_codes, v_scale);
+    }
     adam_update4<ADAMW>(P, M, V, G, c);
-    store4<WHOLE>(t.p + base, i, rest, P);
+    store4<WHOLE>(device_array(t.p) + base, i, rest, P);
     if (t.primary)
-        store4_bf16<WHOLE>(t.primary + base, i, rest,
+        store4_bf16<WHOLE>(device_array(t.primary) + base, i, rest,
                            u32x2{pack_bf16x2(P.x, P.y), pack_bf16x2(P.z, P.w)});
-    if constexpr (STATE == kF32) {
-        store4<WHOLE>((float *)t.m + base, i, rest, M);
-        store4<WHOLE>((float *)t.v + base, i, rest, V);
+    if constexpr (STATE == kI8) {
+        store_state<WHOLE>(device_array((uint8_t *)t.m) + base, device_array(t.m_scales) + block, M,
+                           device_array((uint8_t *)t.v) + base, device_array(t.v_scales) + block, V,
+                           i, rest);
     } else {
-        store_state<1, WHOLE>((uint8_t *)t.m + base, t.m_scales + block, i, rest, M);
-        store_state<2, WHOLE>((uint8_t *)t.v + base, t.v_scales + block, i, rest, V);
+        store4<WHOLE>(device_array((float *)t.m) + base, i, rest, M);
+        store4<WHOLE>(device_array((float *)t.v) + base, i, rest, V);
     }
 }
 
+// Waves of a workgroup, each with a tile, and the workgroups of a CU that a large launch is
+// capped at (0: none).  Moments in fp32 make as many streams as the step of one tensor, and
+// are fastest with few of them open (202 M elements: 938 us at 14 waves, 992 at 10, 956 at
+// 20, 1003 without a cap); moments in 8 bits want all waves for their arithmetic (207 M: 635
+// us with four to a workgroup, 650 with one, 710 at 16 waves).
+template <int STATE>
+constexpr uint32_t kWaves = STATE == kF32 ? 1 : 4;
+template <int STATE>
+constexpr int kResident = STATE == kF32 ? 14 : 0;
+
 template <bool ADAMW, int STATE, int GRAD>
-__global__ __launch_bounds__(64) void adam_tensors_kernel(TableArgs a) {
-    const uint32_t tile = a.base + blockIdx.x;
-    const AdamEntry &t = a.entries[tensor_of(a, tile)];
+__global__ __launch_bounds__(64 * kWaves<STATE>) void adam_tensors_kernel(TableArgs a) {
+    uint32_t tile = blockIdx.x;
+    if constexpr (kWaves<STATE> > 1)
+        tile = tile * kWaves<STATE> + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    if (tile >= a.tiles)
+        return;
+    tile += a.base;
+    Entry &t = ((Entry *)(uintptr_t)a.entries)[tensor_of(a, tile)];
     const size_t base = (size_t)(tile - t.first) * kAdamTile;
     AdamConsts c = a.c;
     // the step size times the decay, rounded once, as the host rounds it for one tensor
@@ -165,38 +213,71 @@ __global__ __launch_bounds__(64) void state_save_kernel(const float *x, void *co
                                                         TileSpan tiles) {
     const size_t block = tiles.first + blockIdx.x, base = block * kAdamTile;
     const uint32_t i = 4 * threadIdx.x;
-    uint8_t *p = (uint8_t *)codes + base;
-    if (blockIdx.x < tiles.whole)
-        store_state<MOMENT, true>(p, scales + block, i, kAdamTile,
-                                  load4<true>(x + base, i, kAdamTile));
+    const bool whole = blockIdx.x < tiles.whole;
+    const f32x4 v = whole ? load4<true>(x + base, i, kAdamTile)
+                          : load4<false>(x + base, i, tiles.tail);
+    const auto save = [&](auto is_whole, uint32_t rest) {
+        constexpr bool kWhole = decltype(is_whole)::value;
+        uint8_t *p = (uint8_t *)codes + base;
+        if constexpr (MOMENT == 1)
+            store_state<kWhole>(p, scales + block, v, nullptr, nullptr, f32x4{}, i, rest);
+        else  // (the root of -0 is no negative number's)
+            store_state<kWhole>(nullptr, nullptr, f32x4{}, p, scales + block, v + 0.0f, i, rest);
+    };
+    if (whole)
+        save(std::true_type{}, kAdamTile);
     else
-        store_state<MOMENT, false>(p, scales + block, i, tiles.tail,
-                                   load4<false>(x + base, i, tiles.tail));
+        save(std::false_type{}, tiles.tail);
 }
 
+// A wave takes two blocks side by side, four waves are a workgroup (207 M values: 157 us; a
+// block 191, four 181; a block a workgroup 204).
+constexpr uint32_t kLoadWaves = 4, kLoadRun = 2;
 template <int MOMENT>
-__global__ __launch_bounds__(64) void state_load_kernel(const void *codes, const float *scales,
-                                                        float *out, TileSpan tiles) {
-    const size_t block = tiles.first + blockIdx.x, base = block * kAdamTile;
-    const uint32_t i = 4 * threadIdx.x;
-    const uint8_t *p = (const uint8_t *)codes + base;
-    const float s = scales[block];
-    if (blockIdx.x < tiles.whole)
-        store4<true>(out + base, i, kAdamTile,
-                     state_values<MOMENT>(load_codes<true>(p, i, kAdamTile), s));
-    else
-        store4<false>(out + base, i, tiles.tail,
-                      state_values<MOMENT>(load_codes<false>(p, i, tiles.tail), s));
+__global__ __launch_bounds__(64 * kLoadWaves) void state_load_kernel(const void *codes,
+                                                                     const float *scales, float *out,
+                                                                     size_t first, size_t n) {
+    size_t base = (first + (size_t)blockIdx.x * kLoadWaves +
+                   __builtin_amdgcn_readfirstlane(threadIdx.x / 64)) * kLoadRun * kAdamTile;
+    const uint32_t i = 4 * (threadIdx.x & 63);
+    const uint8_t *p = (const uint8_t *)codes;
+    if (base + kLoadRun * kAdamTile <= n) {
+        uint32_t c[kLoadRun];
+        float s[kLoadRun];
+#pragma unroll
+        for (uint32_t r = 0; r < kLoadRun; ++r) {
+            c[r] = load_codes<true>(p + base + r * kAdamTile, i, kAdamTile);
+            s[r] = scales[base / kAdamTile + r];
+        }
+#pragma unroll
+        for (uint32_t r = 0; r < kLoadRun; ++r)
+            store4<true>(out + base + r * kAdamTile, i, kAdamTile, state_values<MOMENT>(c[r], s[r]));
+        return;
+    }
+    for (; base < n; base += kAdamTile) {
+        const uint32_t rest = n - base < kAdamTile ? (uint32_t)(n - base) : kAdamTile;
+        store4<false>(out + base, i, rest,
+                      state_values<MOMENT>(load_codes<false>(p + base, i, rest),
+                                           scales[base / kAdamTile]));
+    }
 }
 
 template <int STATE, int GRAD>
-void launch_step(const TableArgs &a, unsigned grid, hipStream_t stream) {
-    if (a.c.adamw)
-        hipLaunchKernelGGL((adam_tensors_kernel<true, STATE, GRAD>), dim3(grid), dim3(64), 0, stream,
-                           a);
-    else
-        hipLaunchKernelGGL((adam_tensors_kernel<false, STATE, GRAD>), dim3(grid), dim3(64), 0,
-                           stream, a);
+void launch_steps(TableArgs a, uint64_t tiles, hipStream_t stream) {
+    constexpr uint32_t kMost = (uint32_t)1 << 25;  // waves a launch: 2^31 work-items
+    const dim3 threads(64 * kWaves<STATE>);
+    for (uint64_t t = 0; t < tiles; t += kMost) {
+        a.base = (uint32_t)t;
+        a.tiles = (uint32_t)(tiles - t < kMost ? tiles - t : kMost);
+        const dim3 grid((a.tiles + kWaves<STATE> - 1) / kWaves<STATE>);
+        const size_t lds = kResident<STATE> ? launch_lds(kResident<STATE>, grid.x) : 0;
+        if (a.c.adamw)
+            hipLaunchKernelGGL((adam_tensors_kernel<true, STATE, GRAD>), grid, threads, lds, stream,
+                               a);
+        else
+            hipLaunchKernelGGL((adam_tensors_kernel<false, STATE, GRAD>), grid, threads, lds,
+                               stream, a);
+    }
 }
 
 }  // namespace
@@ -216,19 +297,14 @@ hipError_t launch_adam_tensors(const void *table, uint32_t tensors, uint64_t til
     } while (n > 1);
     for (int l = 0; l < a.levels; ++l)
         a.level[l] = found[a.levels - 1 - l];
-    constexpr uint64_t kMost = (uint64_t)1 << 25;  // 2^31 work-items a launch
-    for (uint64_t t = 0; t < tiles; t += kMost) {
-        const unsigned grid = (unsigned)(tiles - t < kMost ? tiles - t : kMost);
-        a.base = (uint32_t)t;
-        if (state_type == kF32 && grad_type == kF32)
-            launch_step<kF32, kF32>(a, grid, stream);
-        else if (state_type == kF32)
-            launch_step<kF32, kBf16>(a, grid, stream);
-        else if (grad_type == kF32)
-            launch_step<kI8, kF32>(a, grid, stream);
-        else
-            launch_step<kI8, kBf16>(a, grid, stream);
-    }
+    if (state_type == kF32 && grad_type == kF32)
+        launch_steps<kF32, kF32>(a, tiles, stream);
+    else if (state_type == kF32)
+        launch_steps<kF32, kBf16>(a, tiles, stream);
+    else if (grad_type == kF32)
+        launch_steps<kI8, kF32>(a, tiles, stream);
+    else
+        launch_steps<kI8, kBf16>(a, tiles, stream);
     return hipGetLastError();
 }
 
@@ -247,14 +323,18 @@ hipError_t launch_adam_state_save(const float *x, size_t n, int moment, void *co
 
 hipError_t launch_adam_state_load(const void *codes, const float *scales, size_t n, int moment,
                                   float *out, hipStream_t stream) {
-    for_tiles(n, kAdamTile, 1, 64, true, [&](const TileSpan &tiles, unsigned grid) {
+    constexpr size_t kEach = kLoadRun * kAdamTile, kMost = (size_t)1 << 25;  // waves a launch
+    const size_t waves = (n + kEach - 1) / kEach;
+    for (size_t w = 0; w < waves; w += kMost) {
+        const size_t left = waves - w < kMost ? waves - w : kMost;
+        const dim3 grid((unsigned)((left + kLoadWaves - 1) / kLoadWaves)), threads(64 * kLoadWaves);
         if (moment == 1)
-            hipLaunchKernelGGL(state_load_kernel<1>, dim3(grid), dim3(64), 0, stream, codes, scales,
-                               out, tiles);
+            hipLaunchKernelGGL(state_load_kernel<1>, grid, threads, 0, stream, codes, scales, out, w,
+                               n);
         else
-            hipLaunchKernelGGL(state_load_kernel<2>, dim3(grid), dim3(64), 0, stream, codes, scales,
-                               out, tiles);
-    });
+            hipLaunchKernelGGL(state_load_kernel<2>, grid, threads, 0, stream, codes, scales, out, w,
+                               n);
+    }
     return hipGetLastError();
 }
 

@@ -1343,8 +1343,9 @@ size_t log_probs_workspace(size_t rows, size_t vocab, uint32_t top) {
     if (!rows || !vocab)
         return 0;
     const Cut cut = cut_of(rows, (uint32_t)vocab, top);
+    // (with `top` room for a row's keys at any length, also where nothing is cut)
     if (cut.splits == 1)
-        return 0;
+        return rows * top * sizeof(Key);
     return (rows * cut.splits * sizeof(Sums) + 15) / 16 * 16 +
            rows * cut.splits * top * sizeof(Key);
 }

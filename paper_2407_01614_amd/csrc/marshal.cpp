@@ -242,6 +242,17 @@ class Call {
         return (size_t)THPVariable_Unpack(*args_).numel();
     }
 
+    // The number of the 8-bit codes that come next, and which moment's they are.
+    size_t moment(int *which) {
+        if (!good || args_ >= end_ || !THPVariable_CheckExact(*args_)) {
+            good = false;
+            return 0;
+        }
+        const at::Tensor &t = THPVariable_Unpack(*args_);
+        *which = t.scalar_type() == at::kChar ? 1 : 2;
+        return (size_t)t.numel();
+    }
+
     // `count` contiguous values with one of the dtypes of the mask.
     template <class T = void>
     T *vector(unsigned mask, bool needed, size_t count) {
@@ -576,6 +587,25 @@ PyObject *adam_tensors_step(PyObject *, PyObject *const *args, Py_ssize_t n) {
     });
 }
 
+// adam_state(fn, device, stream, wait, done, codes, scales, values, save)
+PyObject *adam_state(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    return run_call(args, n, [](Call &c) {
+        int moment = 0;
+        const size_t count = c.moment(&moment);
+        void *codes = c.vector(kI8 | kU8, true, count);
+        float *scales = c.vector<float>(kF32, true, (count + ZPP_ADAM_BLOCK - 1) / ZPP_ADAM_BLOCK);
+        float *x = c.vector<float>(kF32, true, count);
+        const bool save = c.truth();
+        if (!c.good || PyErr_Occurred())
+            return 0;
+        if (save)
+            return (int)reinterpret_cast<decltype(&zpp_adam_state_save)>(c.fn)(
+                x, count, moment, codes, scales, c.stream, c.wait, c.done);
+        return (int)reinterpret_cast<decltype(&zpp_adam_state_load)>(c.fn)(
+            codes, scales, count, moment, x, c.stream, c.wait, c.done);
+    });
+}
+
 PyMethodDef methods[] = {
 #define ZPP_CALL(name)                                              \
     {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL,       \
@@ -592,6 +622,7 @@ PyMethodDef methods[] = {
     ZPP_CALL(log_probs_backward),
     ZPP_CALL(log_probs_train),
     ZPP_CALL(adam_tensors_step),
+    ZPP_CALL(adam_state),
     {"addresses", (PyCFunction)(void (*)(void))addresses, METH_FASTCALL,
      "addresses(device, tensor, mask, need, ...) -> tuple or None"},
     {"address_array", (PyCFunction)(void (*)(void))address_array, METH_FASTCALL,

@@ -721,7 +721,8 @@ _FN = {name: _fn("zpp_" + name) for name in (
     "checkpoint_save", "checkpoint_load", "layer_norm_forward", "layer_norm_backward",
     "layer_norm_backward_workspace", "gelu_forward", "gelu_backward", "weight_grad",
     "weight_grad_workspace", "rotary_forward", "rotary_backward", "log_probs_workspace",
-    "log_probs_forward", "log_probs_backward", "log_probs_train", "adam_tensors_step")}
+    "log_probs_forward", "log_probs_backward", "log_probs_train", "adam_tensors_step",
+    "adam_state_save", "adam_state_load")}
 
 
 def _where(name, stream, wait_before, done_after):
@@ -1182,27 +1183,31 @@ def _moment(state, name):
     return (1 if first else 2, *_state8(state, torch.int8 if first else torch.uint8, name))
 
 
+def _adam_state(name, state, values, what, stream, wait_before, done_after):
+    where = _where(name, stream, wait_before, done_after)
+    save = name == "adam_state_save"
+    if type(state) is tuple and len(state) == 2:
+        st = _marshal.adam_state(*where, state[0], state[1], values, save)
+        if st is not None:
+            return _check(st, "zpp_" + name)
+    moment, codes, scales = _moment(state, "state")
+    n = codes.numel()
+    p, = _addresses((what,), what + " holds fewer elements than the state", values, _F32, n)
+    c, s = codes.data_ptr(), scales.data_ptr()
+    st = (_lib.zpp_adam_state_save(p, n, moment, c, s, *where[2:]) if save
+          else _lib.zpp_adam_state_load(c, s, n, moment, p, *where[2:]))
+    _check(st, "zpp_" + name)
+
+
 def adam_state_save(x, state, *, stream=None, wait_before=None, done_after=None):
     """zpp_adam_state_save: fp32 moments x into ``state`` = (codes, scales), whose codes
     are int8 for the first moment and uint8 for the second."""
-    moment, codes, scales = _moment(state, "state")
-    n = codes.numel()
-    p, = _addresses(("x",), "x holds fewer elements than the state", x, _F32, n)
-    st = _lib.zpp_adam_state_save(p, n, moment, codes.data_ptr(), scales.data_ptr(),
-                                  stream_handle(stream), _event_handle(wait_before),
-                                  _event_handle(done_after))
-    _check(st, "zpp_adam_state_save")
+    _adam_state("adam_state_save", state, x, "x", stream, wait_before, done_after)
 
 
 def adam_state_load(state, out, *, stream=None, wait_before=None, done_after=None):
     """zpp_adam_state_load: the moments that ``state`` = (codes, scales) holds, in fp32."""
-    moment, codes, scales = _moment(state, "state")
-    n = codes.numel()
-    p, = _addresses(("out",), "out holds fewer elements than the state", out, _F32, n)
-    st = _lib.zpp_adam_state_load(codes.data_ptr(), scales.data_ptr(), n, moment, p,
-                                  stream_handle(stream), _event_handle(wait_before),
-                                  _event_handle(done_after))
-    _check(st, "zpp_adam_state_load")
+    _adam_state("adam_state_load", state, out, "out", stream, wait_before, done_after)
 
 
 # --------------------------------------------------------------------------
