@@ -5,8 +5,10 @@
 // once, a pair a lane, and kept in LDS for all heads: the angle is a product in 64
 // bits of which the fraction of a turn is taken there, so that far positions lose
 // nothing, and the rest is at most an eighth of a turn, where Taylor's polynomials
-// hold.  The heads then pass through registers, P pairs a lane: 16 bytes of u and
-// 16 of v of halves, 32 in a row of neighbours.
+// hold.  The heads pass through registers, P pairs a lane: 16 bytes of u and 16 of v of
+// halves, 32 in a row of neighbours; a lane's first two are on their way while the angles
+// are computed.  Where P does not divide the pairs, the last P of a head are loaded whole,
+// and those of them that are another lane's are not stored.
 #include "zpp_act8.h"
 #include "zpp_token.h"
 
@@ -64,134 +66,110 @@ __device__ __forceinline__ f32x2 turned(double t) {
 
 template <int TYPE>
 using Element = std::conditional_t<TYPE == kBf16, uint16_t, float>;
+template <int TYPE>
+constexpr int kSize = TYPE == kBf16 ? 2 : 4;
 
-// N elements in a row at p as fp32, and back.
+// N elements in a row at p, as they lie in up to four words, and back.
 template <int TYPE, int N>
-__device__ __forceinline__ void load_row(const Element<TYPE> *p, float (&x)[N]) {
-    if constexpr (TYPE == kF32) {
-        if constexpr (N % 4 == 0) {
-#pragma unroll
-            for (int i = 0; i < N; i += 4) {
-                const f32x4 v = ld_at<f32x4, 4>(p + i);
-                x[i] = v.x, x[i + 1] = v.y, x[i + 2] = v.z, x[i + 3] = v.w;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                x[i] = p[i];
-        }
-    } else if constexpr (N >= 2) {
-        uint32_t w[N / 2];
-        if constexpr (N % 8 == 0) {
-#pragma unroll
-            for (int i = 0; i < N / 2; i += 4) {
-                const u32x4 v = ld_at<u32x4, 2>(p + 2 * i);
-                w[i] = v.x, w[i + 1] = v.y, w[i + 2] = v.z, w[i + 3] = v.w;
-            }
-        } else if constexpr (N == 4) {
-            const u32x2 v = ld_at<u32x2, 2>(p);
-            w[0] = v.x, w[1] = v.y;
-        } else {
-            w[0] = ld_at<uint32_t, 2>(p);
-        }
-#pragma unroll
-        for (int i = 0; i < N / 2; ++i) {
-            x[2 * i] = bf16_lo(w[i]);
-            x[2 * i + 1] = bf16_hi(w[i]);
-        }
+__device__ __forceinline__ void load_row(const Element<TYPE> *p, uint32_t (&w)[4]) {
+    constexpr int kBytes = N * kSize<TYPE>;
+    if constexpr (kBytes == 16) {
+        const u32x4 v = ld_at<u32x4, kSize<TYPE>>(p);
+        w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+    } else if constexpr (kBytes == 8) {
+        const u32x2 v = ld_at<u32x2, kSize<TYPE>>(p);
+        w[0] = v.x, w[1] = v.y;
+    } else if constexpr (kBytes == 4) {
+        w[0] = ld_at<uint32_t, kSize<TYPE>>(p);
     } else {
-        x[0] = bf16_lo(p[0]);
+        w[0] = *reinterpret_cast<const uint16_t *>(p);
     }
 }
-
 template <int TYPE, int N>
-__device__ __forceinline__ void store_row(Element<TYPE> *p, const float (&x)[N]) {
+__device__ __forceinline__ void store_row(Element<TYPE> *p, const uint32_t (&w)[4]) {
+    constexpr int kBytes = N * kSize<TYPE>;
+    if constexpr (kBytes == 16)
+        st_at<u32x4, kSize<TYPE>>(p, u32x4{w[0], w[1], w[2], w[3]});
+    else if constexpr (kBytes == 8)
+        st_at<u32x2, kSize<TYPE>>(p, u32x2{w[0], w[1]});
+    else if constexpr (kBytes == 4)
+        st_at<uint32_t, kSize<TYPE>>(p, w[0]);
+    else
+        *reinterpret_cast<uint16_t *>(p) = (uint16_t)w[0];
+}
+// Elements `from` .. N of them, `from` the same in all lanes: in as few stores as there are
+// ones in their number of words.
+template <int TYPE, int N>
+__device__ __forceinline__ void store_end(Element<TYPE> *p, const uint32_t (&w)[4], uint32_t from) {
+    constexpr uint32_t kWords = N * kSize<TYPE> / 4, kIn = 4 / kSize<TYPE>;
+    if (from == 0)
+        return store_row<TYPE, N>(p, w);
+    uint32_t word = (from + kIn - 1) / kIn;
+    if constexpr (TYPE == kBf16 && N > 1) {
+#pragma unroll
+        for (uint32_t i = 0; i < kWords; ++i)
+            if (2 * i + 1 == from)
+                p[2 * i + 1] = (uint16_t)(w[i] >> 16);
+    }
+    if constexpr (kWords == 4) {
+        if (word == 1)
+            st_at<uint32_t, kSize<TYPE>>(p + kIn, w[1]);
+        if (word <= 2)
+            st_at<u32x2, kSize<TYPE>>(p + 2 * kIn, u32x2{w[2], w[3]});
+        if (word == 3)
+            st_at<uint32_t, kSize<TYPE>>(p + 3 * kIn, w[3]);
+    } else if constexpr (kWords == 2) {
+        if (word == 1)
+            st_at<uint32_t, kSize<TYPE>>(p + kIn, w[1]);
+    }
+}
+template <int TYPE, int N>
+__device__ __forceinline__ void unpack(const uint32_t (&w)[4], float *x) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        x[i] = TYPE == kF32  ? __uint_as_float(w[i])
+               : i % 2 == 0 ? bf16_lo(w[i / 2])
+                            : bf16_hi(w[i / 2]);
+}
+template <int TYPE, int N>
+__device__ __forceinline__ void pack(const float *x, uint32_t (&w)[4]) {
     if constexpr (TYPE == kF32) {
-        if constexpr (N % 4 == 0) {
 #pragma unroll
-            for (int i = 0; i < N; i += 4)
-                st_at<f32x4, 4>(p + i, f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]});
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                p[i] = x[i];
-        }
-    } else if constexpr (N >= 2) {
-        uint32_t w[N / 2];
+        for (int i = 0; i < N; ++i)
+            w[i] = __float_as_uint(x[i]);
+    } else if constexpr (N == 1) {
+        w[0] = bf16_pair(x[0], x[0]);
+    } else {
 #pragma unroll
         for (int i = 0; i < N / 2; ++i)
             w[i] = bf16_pair(x[2 * i], x[2 * i + 1]);
-        if constexpr (N % 8 == 0) {
-#pragma unroll
-            for (int i = 0; i < N / 2; i += 4)
-                st_at<u32x4, 2>(p + 2 * i, u32x4{w[i], w[i + 1], w[i + 2], w[i + 3]});
-        } else if constexpr (N == 4) {
-            st_at<u32x2, 2>(p, u32x2{w[0], w[1]});
-        } else {
-            st_at<uint32_t, 2>(p, w[0]);
-        }
-    } else {
-        p[0] = (uint16_t)bf16_pair(x[0], x[0]);
     }
 }
 
-// P pairs of a head from pair i on.
-template <int TYPE, bool NEAR, int P>
-__device__ __forceinline__ void rotate(const Element<TYPE> *x, Element<TYPE> *out, uint32_t i,
-                                       uint32_t pairs, const f32x2 *angle) {
-    float u[P], v[P];
-    if constexpr (NEAR) {
-        float w[2 * P];
-        load_row<TYPE>(x + 2 * i, w);
-#pragma unroll
-        for (int j = 0; j < P; ++j)
-            u[j] = w[2 * j], v[j] = w[2 * j + 1];
-    } else {
-        load_row<TYPE>(x + i, u);
-        load_row<TYPE>(x + pairs + i, v);
-    }
-#pragma unroll
-    for (int j = 0; j < P; ++j) {
-        const f32x2 a = angle[i + j];
-        const float turned_u = u[j] * a.x - v[j] * a.y;
-        v[j] = u[j] * a.y + v[j] * a.x;
-        u[j] = turned_u;
-    }
-    if constexpr (NEAR) {
-        float w[2 * P];
-#pragma unroll
-        for (int j = 0; j < P; ++j)
-            w[2 * j] = u[j], w[2 * j + 1] = v[j];
-        store_row<TYPE>(out + 2 * i, w);
-    } else {
-        store_row<TYPE>(out + i, u);
-        store_row<TYPE>(out + pairs + i, v);
-    }
-}
+// Features of a chunk that is copied; fewer are copied one by one.
+template <int TYPE>
+constexpr uint32_t kCopied = 32 / kSize<TYPE>;
 
-constexpr uint32_t kCopied = 8;  // features of a chunk that is copied
-
+// A lane's part of a head: P pairs that turn, or features that are copied.
 template <int TYPE, bool NEAR, int P>
-__global__ __launch_bounds__(kThreads) void rotary_kernel(Args a) {
-    extern __shared__ f32x2 angles[];  // [tokens of the tile][pairs]
-    const uint32_t tile = blockIdx.x / a.slices, slice = blockIdx.x % a.slices;
-    const size_t token0 = a.base + (size_t)tile * a.tile;
-    const uint32_t tokens = (uint32_t)(a.tokens - token0 < a.tile ? a.tokens - token0 : a.tile);
-    for (uint32_t i = threadIdx.x; i < tokens * a.pairs; i += kThreads) {
-        const uint32_t t = a.by_pairs(i);
-        const f32x2 cs = turned((double)a.positions[token0 + t] * a.turns[i - t * a.pairs]);
-        angles[i] = f32x2{cs.x * a.scale, cs.y * a.scale * a.sign};
-    }
-    __syncthreads();
-    const uint32_t head0 = slice * a.share;
-    const uint32_t heads = a.heads - head0 < a.share ? a.heads - head0 : a.share;
-    const uint32_t chunks = a.rot_chunks + a.copy_chunks;
-    // the last slice may have fewer heads: its items are numbered as the others'
-    for (uint32_t i = threadIdx.x; i < tokens * a.share * chunks; i += kThreads) {
-        const uint32_t t = a.by_token(i), in_token = i - t * a.share * chunks;
+struct Part {
+    static constexpr int kHalf = kCopied<TYPE> / 2;
+    uint32_t w[2][4];
+    Element<TYPE> *out;
+    uint32_t first, skip, token;  // its first pair or feature, pairs not its own, which token
+    enum { kNone, kTurn, kCopy, kOne } what;
+
+    // Item i of a workgroup's.
+    __device__ __forceinline__ void load(const Args &a, size_t token0, uint32_t tokens,
+                                         uint32_t head0, uint32_t heads, uint32_t i) {
+        const uint32_t chunks = a.rot_chunks + a.copy_chunks;
+        what = kNone;
+        token = a.by_token(i);
+        const uint32_t in_token = i - token * a.share * chunks;
         const uint32_t h = a.by_chunks(in_token), chunk = in_token - h * chunks;
-        if (h >= heads)
-            continue;
+        // the last slice may have fewer heads: its items are numbered as the others'
+        if (token >= tokens || h >= heads)
+            return;
         uint32_t head = head0 + h;
         const bool is_x = head < a.heads_x;
         if (!is_x)
@@ -200,30 +178,107 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Args a) {
         const uint32_t g = is_x ? a.by_group_x(head) : a.by_group_k(head);
         const uint32_t m = head - g * from.heads;
         const Element<TYPE> *x = reinterpret_cast<const Element<TYPE> *>(from.data) +
-                                 (token0 + t) * from.token + g * from.group + m * from.head;
-        Element<TYPE> *out = reinterpret_cast<Element<TYPE> *>(to.data) +
-                             (token0 + t) * to.token + g * to.group + m * to.head;
+                                 (token0 + token) * from.token + g * from.group + m * from.head;
+        out = reinterpret_cast<Element<TYPE> *>(to.data) + (token0 + token) * to.token +
+              g * to.group + m * to.head;
         if (chunk < a.rot_chunks) {
-            rotate<TYPE, NEAR, P>(x, out, chunk * P, a.pairs, angles + t * a.pairs);
+            what = kTurn;
+            first = chunk * P < a.pairs - P ? chunk * P : a.pairs - P;
+            skip = chunk * P - first;
+            load_row<TYPE, P>(x + (NEAR ? 2 * first : first), w[0]);
+            load_row<TYPE, P>(x + (NEAR ? 2 * first + P : a.pairs + first), w[1]);
         } else if (is_x ? a.copy_x : a.copy_k) {
-            const uint32_t f = a.rotated + (chunk - a.rot_chunks) * kCopied;
-            if (f + kCopied <= a.dim) {
-                float w[kCopied];
-                load_row<TYPE>(x + f, w);
-                store_row<TYPE>(out + f, w);
-            } else {
-                for (uint32_t e = f; e < a.dim; ++e)
-                    out[e] = x[e];
+            first = chunk - a.rot_chunks;
+            if (a.dim - a.rotated < kCopied<TYPE>) {
+                what = kOne;
+                first += a.rotated;
+                load_row<TYPE, 1>(x + first, w[0]);
+                return;
             }
+            // the last is copied whole as well: what it shares with the one before is the same
+            what = kCopy;
+            first = a.rotated + first * kCopied<TYPE>;
+            first = first < a.dim - kCopied<TYPE> ? first : a.dim - kCopied<TYPE>;
+            load_row<TYPE, kHalf>(x + first, w[0]);
+            load_row<TYPE, kHalf>(x + first + kHalf, w[1]);
         }
+    }
+
+    __device__ __forceinline__ void store(const Args &a, const f32x2 *angles) {
+        if (what == kTurn) {
+            float x[2 * P];
+            unpack<TYPE, P>(w[0], x);
+            unpack<TYPE, P>(w[1], x + P);
+            const f32x2 *angle = angles + token * a.pairs + first;
+#pragma unroll
+            for (int j = 0; j < P; ++j) {
+                float &u = x[NEAR ? 2 * j : j], &v = x[NEAR ? 2 * j + 1 : P + j];
+                const f32x2 c = angle[j];
+                const float turned_u = u * c.x - v * c.y;
+                v = u * c.y + v * c.x;
+                u = turned_u;
+            }
+            pack<TYPE, P>(x, w[0]);
+            pack<TYPE, P>(x + P, w[1]);
+            Element<TYPE> *p = out + (NEAR ? 2 * first : first);
+            Element<TYPE> *q = out + (NEAR ? 2 * first + P : a.pairs + first);
+            if (skip == 0) {
+                store_row<TYPE, P>(p, w[0]);
+                store_row<TYPE, P>(q, w[1]);
+            } else {
+                // the same in all lanes that come here
+                const uint32_t s = __builtin_amdgcn_readfirstlane(skip);
+                store_end<TYPE, P>(p, w[0], NEAR ? (2 * s < P ? 2 * s : P) : s);
+                store_end<TYPE, P>(q, w[1], NEAR ? (2 * s < P ? 0 : 2 * s - P) : s);
+            }
+        } else if (what == kCopy) {
+            store_row<TYPE, kHalf>(out + first, w[0]);
+            store_row<TYPE, kHalf>(out + first + kHalf, w[1]);
+        } else if (what == kOne) {
+            store_row<TYPE, 1>(out + first, w[0]);
+        }
+    }
+};
+
+template <int TYPE, bool NEAR, int P>
+__global__ __launch_bounds__(kThreads) void rotary_kernel(Args a) {
+    extern __shared__ f32x2 angles[];  // [tokens of the tile][pairs]
+    const uint32_t tile = blockIdx.x / a.slices, slice = blockIdx.x % a.slices;
+    const size_t token0 = a.base + (size_t)tile * a.tile;
+    const uint32_t tokens = (uint32_t)(a.tokens - token0 < a.tile ? a.tokens - token0 : a.tile);
+    const uint32_t head0 = slice * a.share;
+    const uint32_t heads = a.heads - head0 < a.share ? a.heads - head0 : a.share;
+    const uint32_t items = tokens * a.share * (a.rot_chunks + a.copy_chunks);
+    constexpr int kParts = 2;
+    Part<TYPE, NEAR, P> part[kParts];
+    const auto load = [&](uint32_t first) {
+#pragma unroll
+        for (int j = 0; j < kParts; ++j)
+            part[j].load(a, token0, tokens, head0, heads, first + threadIdx.x + j * kThreads);
+    };
+    load(0);
+    for (uint32_t i = threadIdx.x; i < tokens * a.pairs; i += kThreads) {
+        const uint32_t t = a.by_pairs(i);
+        const f32x2 cs = turned((double)a.positions[token0 + t] * a.turns[i - t * a.pairs]);
+        angles[i] = f32x2{cs.x * a.scale, cs.y * a.scale * a.sign};
+    }
+    __syncthreads();
+    for (uint32_t first = 0;;) {
+#pragma unroll
+        for (int j = 0; j < kParts; ++j)
+            part[j].store(a, angles);
+        first += kParts * kThreads;
+        if (first >= items)
+            break;
+        load(first);
     }
 }
 
 template <int TYPE, bool NEAR>
 void launch_pairs(const Args &a, uint32_t per, unsigned grid, size_t lds, hipStream_t stream) {
     const dim3 g(grid), b(kThreads);
-    if (per == 8)
-        hipLaunchKernelGGL((rotary_kernel<TYPE, NEAR, 8>), g, b, lds, stream, a);
+    if (TYPE == kBf16 && per == 8)
+        hipLaunchKernelGGL((rotary_kernel<TYPE, NEAR, TYPE == kBf16 ? 8 : 4>), g, b, lds, stream, a);
     else if (per == 4)
         hipLaunchKernelGGL((rotary_kernel<TYPE, NEAR, 4>), g, b, lds, stream, a);
     else if (per == 2)
@@ -243,12 +298,15 @@ hipError_t launch_rotary(const RotaryArgs &r, int type, hipStream_t stream) {
     a.heads = a.heads_x + r.k.groups * r.k.heads;
     a.scale = r.scale, a.sign = r.backward ? -1.0f : 1.0f;
     a.copy_x = r.copy_x, a.copy_k = r.copy_k;
-    // pairs of a lane: whole chunks only
+    // pairs of a lane: 16 bytes of each half, or a power of two that there are
     uint32_t per = type == kBf16 ? 8 : 4;
-    while (a.pairs % per)
+    while (per > 1 && a.pairs < per)
         per /= 2;
-    a.rot_chunks = a.pairs / per;
-    a.copy_chunks = r.copy_x || r.copy_k ? (r.dim - r.rotated + kCopied - 1) / kCopied : 0;
+    a.rot_chunks = (a.pairs + per - 1) / per;
+    const uint32_t rest = r.dim - r.rotated, copied = type == kBf16 ? kCopied<kBf16> : kCopied<kF32>;
+    a.copy_chunks = !(r.copy_x || r.copy_k) ? 0
+                    : rest < copied        ? rest
+                                           : (rest + copied - 1) / copied;
     const uint32_t chunks = a.rot_chunks + a.copy_chunks;
     if (!chunks)
         return hipSuccess;
@@ -287,9 +345,9 @@ hipError_t launch_rotary(const RotaryArgs &r, int type, hipStream_t stream) {
         else if (type == kBf16)
             launch_pairs<kBf16, false>(a, per, grid, lds, stream);
         else if (r.interleaved)
-            launch_pairs<kF32, true>(a, per > 4 ? 4 : per, grid, lds, stream);
+            launch_pairs<kF32, true>(a, per, grid, lds, stream);
         else
-            launch_pairs<kF32, false>(a, per > 4 ? 4 : per, grid, lds, stream);
+            launch_pairs<kF32, false>(a, per, grid, lds, stream);
     }
     return hipGetLastError();
 }
