@@ -6,9 +6,13 @@
 // bits of which the fraction of a turn is taken there, so that far positions lose
 // nothing, and the rest is at most an eighth of a turn, where Taylor's polynomials
 // hold.  The heads pass through registers, P pairs a lane: 16 bytes of u and 16 of v of
-// halves, 32 in a row of neighbours; a lane's first two are on their way while the angles
+// halves, 16 in a row of neighbours; a lane's first pieces are on their way while the angles
 // are computed.  Where P does not divide the pairs, the last P of a head are loaded whole,
 // and those of them that are another lane's are not stored.
+//
+// Whole heads into another array are stored as a stream (4096 tokens of 64 heads of 128 in
+// bf16: 22.8 us, 29.0 without; where pieces share lines a stream costs, 55.6 for 39.4 with 20
+// of 80 features turning, and in place it gains nothing).
 #include "zpp_act8.h"
 #include "zpp_token.h"
 
@@ -85,10 +89,12 @@ __device__ __forceinline__ void load_row(const Element<TYPE> *p, uint32_t (&w)[4
         w[0] = *reinterpret_cast<const uint16_t *>(p);
     }
 }
-template <int TYPE, int N>
+template <int TYPE, int N, bool STREAM = false>
 __device__ __forceinline__ void store_row(Element<TYPE> *p, const uint32_t (&w)[4]) {
     constexpr int kBytes = N * kSize<TYPE>;
-    if constexpr (kBytes == 16)
+    if constexpr (kBytes == 16 && STREAM)
+        st_nt_at<u32x4, kSize<TYPE>>(p, u32x4{w[0], w[1], w[2], w[3]});
+    else if constexpr (kBytes == 16)
         st_at<u32x4, kSize<TYPE>>(p, u32x4{w[0], w[1], w[2], w[3]});
     else if constexpr (kBytes == 8)
         st_at<u32x2, kSize<TYPE>>(p, u32x2{w[0], w[1]});
@@ -151,7 +157,7 @@ template <int TYPE>
 constexpr uint32_t kCopied = 32 / kSize<TYPE>;
 
 // A lane's part of a head: P pairs that turn, or features that are copied.
-template <int TYPE, bool NEAR, int P>
+template <int TYPE, bool NEAR, int P, bool STREAM>
 struct Part {
     static constexpr int kHalf = kCopied<TYPE> / 2;
     uint32_t w[2][4];
@@ -185,8 +191,12 @@ struct Part {
             what = kTurn;
             first = chunk * P < a.pairs - P ? chunk * P : a.pairs - P;
             skip = chunk * P - first;
-            load_row<TYPE, P>(x + (NEAR ? 2 * first : first), w[0]);
-            load_row<TYPE, P>(x + (NEAR ? 2 * first + P : a.pairs + first), w[1]);
+            if constexpr (NEAR) {
+                load_row<TYPE, 2 * P>(x + 2 * first, w[0]);
+            } else {
+                load_row<TYPE, P>(x + first, w[0]);
+                load_row<TYPE, P>(x + a.pairs + first, w[1]);
+            }
         } else if (is_x ? a.copy_x : a.copy_k) {
             first = chunk - a.rot_chunks;
             if (a.dim - a.rotated < kCopied<TYPE>) {
@@ -207,8 +217,12 @@ struct Part {
     __device__ __forceinline__ void store(const Args &a, const f32x2 *angles) {
         if (what == kTurn) {
             float x[2 * P];
-            unpack<TYPE, P>(w[0], x);
-            unpack<TYPE, P>(w[1], x + P);
+            if constexpr (NEAR) {
+                unpack<TYPE, 2 * P>(w[0], x);
+            } else {
+                unpack<TYPE, P>(w[0], x);
+                unpack<TYPE, P>(w[1], x + P);
+            }
             const f32x2 *angle = angles + token * a.pairs + first;
 #pragma unroll
             for (int j = 0; j < P; ++j) {
@@ -218,18 +232,24 @@ struct Part {
                 v = u * c.y + v * c.x;
                 u = turned_u;
             }
-            pack<TYPE, P>(x, w[0]);
-            pack<TYPE, P>(x + P, w[1]);
-            Element<TYPE> *p = out + (NEAR ? 2 * first : first);
-            Element<TYPE> *q = out + (NEAR ? 2 * first + P : a.pairs + first);
-            if (skip == 0) {
-                store_row<TYPE, P>(p, w[0]);
-                store_row<TYPE, P>(q, w[1]);
+            // (the same in all lanes where it is not 0)
+            const auto from = [&] { return __builtin_amdgcn_readfirstlane(skip); };
+            if constexpr (NEAR) {
+                pack<TYPE, 2 * P>(x, w[0]);
+                if (STREAM || skip == 0)
+                    store_row<TYPE, 2 * P, STREAM>(out + 2 * first, w[0]);
+                else
+                    store_end<TYPE, 2 * P>(out + 2 * first, w[0], 2 * from());
             } else {
-                // the same in all lanes that come here
-                const uint32_t s = __builtin_amdgcn_readfirstlane(skip);
-                store_end<TYPE, P>(p, w[0], NEAR ? (2 * s < P ? 2 * s : P) : s);
-                store_end<TYPE, P>(q, w[1], NEAR ? (2 * s < P ? 0 : 2 * s - P) : s);
+                pack<TYPE, P>(x, w[0]);
+                pack<TYPE, P>(x + P, w[1]);
+                if (STREAM || skip == 0) {
+                    store_row<TYPE, P, STREAM>(out + first, w[0]);
+                    store_row<TYPE, P, STREAM>(out + a.pairs + first, w[1]);
+                } else {
+                    store_end<TYPE, P>(out + first, w[0], from());
+                    store_end<TYPE, P>(out + a.pairs + first, w[1], from());
+                }
             }
         } else if (what == kCopy) {
             store_row<TYPE, kHalf>(out + first, w[0]);
@@ -240,7 +260,7 @@ struct Part {
     }
 };
 
-template <int TYPE, bool NEAR, int P>
+template <int TYPE, bool NEAR, int P, bool STREAM>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(Args a) {
     extern __shared__ f32x2 angles[];  // [tokens of the tile][pairs]
     const uint32_t tile = blockIdx.x / a.slices, slice = blockIdx.x % a.slices;
@@ -250,7 +270,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Args a) {
     const uint32_t heads = a.heads - head0 < a.share ? a.heads - head0 : a.share;
     const uint32_t items = tokens * a.share * (a.rot_chunks + a.copy_chunks);
     constexpr int kParts = 2;
-    Part<TYPE, NEAR, P> part[kParts];
+    Part<TYPE, NEAR, P, STREAM> part[kParts];
     const auto load = [&](uint32_t first) {
 #pragma unroll
         for (int j = 0; j < kParts; ++j)
@@ -274,17 +294,31 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(Args a) {
     }
 }
 
+// Pairs of a lane: 16 bytes of each half, or of both.
 template <int TYPE, bool NEAR>
-void launch_pairs(const Args &a, uint32_t per, unsigned grid, size_t lds, hipStream_t stream) {
+constexpr uint32_t kMostPer = 16 / kSize<TYPE> / (NEAR ? 2 : 1);
+uint32_t most_per(int type, bool near) {
+    return type == kBf16 ? (near ? kMostPer<kBf16, true> : kMostPer<kBf16, false>)
+                         : (near ? kMostPer<kF32, true> : kMostPer<kF32, false>);
+}
+
+template <int TYPE, bool NEAR>
+void launch_pairs(const Args &a, uint32_t per, bool whole, unsigned grid, size_t lds,
+                  hipStream_t stream) {
+    constexpr int kMost = kMostPer<TYPE, NEAR>;
     const dim3 g(grid), b(kThreads);
-    if (TYPE == kBf16 && per == 8)
-        hipLaunchKernelGGL((rotary_kernel<TYPE, NEAR, TYPE == kBf16 ? 8 : 4>), g, b, lds, stream, a);
+    if (whole)
+        hipLaunchKernelGGL((rotary_kernel<TYPE, NEAR, kMost, true>), g, b, lds, stream, a);
+    else if (per == kMost)
+        hipLaunchKernelGGL((rotary_kernel<TYPE, NEAR, kMost, false>), g, b, lds, stream, a);
     else if (per == 4)
-        hipLaunchKernelGGL((rotary_kernel<TYPE, NEAR, 4>), g, b, lds, stream, a);
+        hipLaunchKernelGGL((rotary_kernel<TYPE, NEAR, kMost < 4 ? kMost : 4, false>), g, b, lds,
+                           stream, a);
     else if (per == 2)
-        hipLaunchKernelGGL((rotary_kernel<TYPE, NEAR, 2>), g, b, lds, stream, a);
+        hipLaunchKernelGGL((rotary_kernel<TYPE, NEAR, kMost < 2 ? kMost : 2, false>), g, b, lds,
+                           stream, a);
     else
-        hipLaunchKernelGGL((rotary_kernel<TYPE, NEAR, 1>), g, b, lds, stream, a);
+        hipLaunchKernelGGL((rotary_kernel<TYPE, NEAR, 1, false>), g, b, lds, stream, a);
 }
 
 }  // namespace
@@ -298,8 +332,8 @@ hipError_t launch_rotary(const RotaryArgs &r, int type, hipStream_t stream) {
     a.heads = a.heads_x + r.k.groups * r.k.heads;
     a.scale = r.scale, a.sign = r.backward ? -1.0f : 1.0f;
     a.copy_x = r.copy_x, a.copy_k = r.copy_k;
-    // pairs of a lane: 16 bytes of each half, or a power of two that there are
-    uint32_t per = type == kBf16 ? 8 : 4;
+    // (or a power of two that there are)
+    uint32_t per = most_per(type, r.interleaved);
     while (per > 1 && a.pairs < per)
         per /= 2;
     a.rot_chunks = (a.pairs + per - 1) / per;
@@ -334,6 +368,8 @@ hipError_t launch_rotary(const RotaryArgs &r, int type, hipStream_t stream) {
     a.by_token = make_div(items);
     a.by_group_x = make_div(r.x.heads ? r.x.heads : 1);
     a.by_group_k = make_div(r.k.heads ? r.k.heads : 1);
+    const bool whole = r.rotated == r.dim && a.pairs % most_per(type, r.interleaved) == 0 &&
+                       (r.copy_x || !r.x.heads) && (r.copy_k || !r.k.heads);
     const size_t lds = (size_t)a.tile * a.pairs * sizeof(f32x2);
     // 2^22 workgroups a launch
     const size_t most = (((size_t)1 << 22) / a.slices) * a.tile;
@@ -341,13 +377,13 @@ hipError_t launch_rotary(const RotaryArgs &r, int type, hipStream_t stream) {
         const size_t left = r.tokens - a.base < most ? r.tokens - a.base : most;
         const unsigned grid = (unsigned)((left + a.tile - 1) / a.tile * a.slices);
         if (type == kBf16 && r.interleaved)
-            launch_pairs<kBf16, true>(a, per, grid, lds, stream);
+            launch_pairs<kBf16, true>(a, per, whole, grid, lds, stream);
         else if (type == kBf16)
-            launch_pairs<kBf16, false>(a, per, grid, lds, stream);
+            launch_pairs<kBf16, false>(a, per, whole, grid, lds, stream);
         else if (r.interleaved)
-            launch_pairs<kF32, true>(a, per, grid, lds, stream);
+            launch_pairs<kF32, true>(a, per, whole, grid, lds, stream);
         else
-            launch_pairs<kF32, false>(a, per, grid, lds, stream);
+            launch_pairs<kF32, false>(a, per, whole, grid, lds, stream);
     }
     return hipGetLastError();
 }
