@@ -111,6 +111,11 @@ def gradient(x, targets, lse, g, h=None, entropy=None, rel_s=None):
     if rel_s is not None:
         rel = rel + rel_s[:, None]
     bound = p * (rel * c.abs() + 5 * U * size) + 1e-37
+    # the exponential has no results below the normal numbers: relative to the largest logit
+    # or to lse, whose sum is 1 or more, e^d < 2^-126 counts as 0, and then p |c| is missing,
+    # which is below 2^-126 |c| (|c| is past 8, and this past 1e-37, where h is not 0 and
+    # log p is near -87)
+    bound = bound + torch.where(p < 2.0 ** -125, 2.0 ** -126 * c.abs(), torch.zeros_like(p))
     if rel_s is not None and h is not None:
         bound = bound + p * h.double().abs()[:, None] * (2 * rel_s * (1 + entropy.abs()))[:, None]
     rows = torch.arange(x.shape[0], device=x.device)
