@@ -332,7 +332,7 @@ hipError_t launch_rotary(const RotaryArgs &r, int type, hipStream_t stream) {
     a.heads = a.heads_x + r.k.groups * r.k.heads;
     a.scale = r.scale, a.sign = r.backward ? -1.0f : 1.0f;
     a.copy_x = r.copy_x, a.copy_k = r.copy_k;
-    // (or a power of two that there are)
+    // (or the largest power of two that there are)
     uint32_t per = most_per(type, r.interleaved);
     while (per > 1 && a.pairs < per)
         per /= 2;
@@ -344,14 +344,15 @@ hipError_t launch_rotary(const RotaryArgs &r, int type, hipStream_t stream) {
     const uint32_t chunks = a.rot_chunks + a.copy_chunks;
     if (!chunks)
         return hipSuccess;
-    // a workgroup has at most 16384 items (the divisions hold to 65535) and at most
-    // kMostPairs angles: tokens, or where one token has more, some of its heads
+    // a workgroup has about kItems items, a head's at least (below 4096; the divisions hold to
+    // 65535), and at most kMostPairs angles: tokens, or where one token has more, some of its
+    // heads
     constexpr uint32_t kItems = 4 * kThreads;
     a.share = a.heads;
     if ((size_t)a.heads * chunks > kItems) {
         const uint32_t most = kItems / chunks ? kItems / chunks : 1;
-        a.slices = (a.heads + most - 1) / most;
-        a.share = (a.heads + a.slices - 1) / a.slices;
+        const uint32_t slices = (a.heads + most - 1) / most;
+        a.share = (a.heads + slices - 1) / slices;
     }
     // few tokens: a lane an item, so that no lane waits twice
     if (r.tokens < 1024) {

@@ -106,6 +106,40 @@ def test_lists_that_overflow(zpp, rows, vocab, top, dtype):
     check_forward(x, targets, lp, lse, h)
 
 
+@pytest.mark.parametrize("vocab", [9, 100, 1500, 9000, 70000])
+@pytest.mark.parametrize("shift", [1e3, -3e4, 3e5, 1e6, -1e7, 1e8])
+def test_large_logits(zpp, vocab, shift):
+    """Logits far from 0 in fp32: log probabilities and gradients depend on their differences,
+    which are exact."""
+    rows = 5
+    ulp = float(np.spacing(np.float32(abs(shift))))
+    steps = torch.randn(rows, vocab, device="cuda",
+                        generator=torch.Generator(device="cuda").manual_seed(vocab))
+    x = (shift + (3 * steps / ulp).round().double() * ulp).float()
+    targets = torch.arange(rows, device="cuda")
+    g, dh = ref.numbers((rows,), 5, F32), ref.numbers((rows,), 6, F32, 0.1)
+    w_lse, ln, w_h, mean_d = ref.softmax_parts(x)
+    ws = workspace(zpp, rows, vocab)
+    lp, lse, h = outputs(rows)
+    zpp.log_probs_forward(x, targets, lp, lse, ws, entropies=h)
+    check_forward(x, targets, lp, lse, h)
+    top = min(vocab, 5)
+    ids, tlp = torch.empty(rows, top, dtype=torch.int32, device="cuda"), torch.empty(rows, top, device="cuda")
+    zpp.log_probs_forward(x, targets, lp, lse, workspace(zpp, rows, vocab, top), entropies=h,
+                          top_ids=ids, top_log_probs=tlp)
+    check_forward(x, targets, lp, lse, h)
+    assert torch.equal(ids.long(), ref.top_ids(x, top))
+    dx = torch.empty_like(x)
+    zpp.log_probs_train(x, targets, lp, lse, g, dx, ws, entropies=h, dentropies=dh)
+    check_forward(x, targets, lp, lse, h)
+    if vocab <= 65536:  # (longer rows' second pass has lse as fp32 holds it)
+        rel = ref.sum_bound(vocab, mean_d) + 2 * ref.U * (ln.abs() + 1)
+        # relative to the row's largest logit, as the kernel takes them: no rounding of lse
+        largest = x.double().amax(1)
+        want, bound = ref.gradient(x.double() - largest[:, None], targets, ln, g, dh, w_h, rel_s=rel)
+        assert_within(dx, want, bound)
+
+
 # --------------------------------------------------------------------------
 # Moments in 8 bits
 # --------------------------------------------------------------------------
