@@ -57,7 +57,7 @@ __device__ __forceinline__ uint32_t second_code(float r, const StateScale &s) {
 // within a unit in the last place: r within 2^-23 of itself and half a step for its own
 // rounding, t's root within half of that, another step and 2^-24 for the products, below
 // 2^-22 together, 2^-14 at 255.  Only where some lane's t has a root within 2^-13 of a border
-// (3 in 100 waves) are all taken again from correct ones.  Blocks whose largest is below 2^-96
+// (6 in 100 waves) are all taken again from correct ones.  Blocks whose largest is below 2^-96
 // too; in others v of less than 2^-126, whose roots the hardware does not have, are of code 1
 // or 0: t < 2^-63 / 2^-48 65025 < 2.
 __device__ __forceinline__ uint32_t second_codes(const f32x4 &v, uint32_t top,
