@@ -498,11 +498,11 @@ struct Selection {
     uint32_t counts[3];
 };
 
-// The largest number of bits from LOW on that `top` of all lanes' values reach; its lowest
-// bits stay 0 where no more than kSpare lanes beside them do.  The same in all lanes.
-template <uint32_t THREADS, int LOW, class T>
+// The largest number of bits from LOW on that `top` of COUNT values reach; its lowest bits
+// stay 0 where no more than kSpare beside them do.  The same in all lanes.
+template <uint32_t COUNT, int LOW, class T>
 __device__ __forceinline__ T bound_of(const T *values, uint32_t top) {
-    constexpr uint32_t kEach = THREADS / 64;
+    constexpr uint32_t kEach = COUNT / 64;
     T v[kEach], bound = 0;
 #pragma unroll
     for (uint32_t j = 0; j < kEach; ++j)
@@ -556,11 +556,19 @@ template <uint32_t THREADS, int LOW>
 __device__ __forceinline__ float value_bound(Selection<THREADS> &s, uint32_t top, float m,
                                              uint32_t turn) {
     uint32_t *values = reinterpret_cast<uint32_t *>(s.lanes) + turn % 2 * THREADS;
-    values[threadIdx.x] = order_of(m);
+    // of 1024 lanes, the largest of four each: 256 values are enough for 64
+    constexpr uint32_t kGroup = THREADS > kThreads ? THREADS / kThreads : 1;
+    static_assert(kGroup == 1 || kGroup == 4);
+    if constexpr (kGroup == 4) {
+        m = __builtin_fmaxf(m, dpp<kSwap1>(m));
+        m = __builtin_fmaxf(m, dpp<kSwap2>(m));
+    }
+    if (threadIdx.x % kGroup == 0)
+        values[threadIdx.x / kGroup] = order_of(m);
     if (turn == 0 && threadIdx.x == 0)
         s.counts[0] = 0;
     __syncthreads();
-    const uint32_t order = bound_of<THREADS, LOW, uint32_t>(values, top);
+    const uint32_t order = bound_of<THREADS / kGroup, LOW, uint32_t>(values, top);
     // (below the finite numbers: fewer than `top` lanes have one)
     return order < 0x00800000u ? kLowest : ordered(order);
 }
@@ -1172,8 +1180,11 @@ Cut cut_of(size_t rows, uint32_t vocab, uint32_t top) {
     const size_t most = kFill / (rows ? rows : 1);
     if (top) {
         // one workgroup goes through a batch in less time than a second launch takes (1x8192
-        // 6.3 us, 8.9 in slices)
-        if (n <= kTopBatch)
+        // 6.3 us, 8.9 in slices; with 1024 lanes 1x16384 7.0 and 9.7, 1x40000 9.8 and 11.3),
+        // and through several where the slices of other rows would wait for CUs (128x65024
+        // with the 32 best 14.2 and 16.2, 200x131072 23.9 and 30.5; 16x65024 13.6 and 13.3,
+        // 64x131072 23.1 and 16.6)
+        if (n <= kOneGroup + kOneGroup / 4 || (size_t)n * 48 <= rows * kOneGroup)
             return {1, n};
         const uint32_t keys = kThreads * kJoined / top;  // slices whose keys can be joined
         if (slices(n, kTopSlice) <= most && slices(n, kTopSlice) <= keys)
@@ -1189,8 +1200,8 @@ Cut cut_of(size_t rows, uint32_t vocab, uint32_t top) {
     return {slices(n, slice), slice};
 }
 
-// Rows a launch, so that its work-items stay below 2^31.
-constexpr size_t kMostWorkgroups = (size_t)1 << 22;
+// Workgroups a launch, of up to 1024: 2^30 work-items.
+constexpr size_t kMostWorkgroups = (size_t)1 << 20;
 
 RowArgs row_args(const LogProbsArgs &a, const Cut &cut) {
     RowArgs r{};
@@ -1256,11 +1267,16 @@ void top_typed(const LogProbsArgs &args, const Cut &cut, hipStream_t stream) {
     };
     // a wave a row of a batch, or of two where there are enough rows (4000x2000 with the 5
     // best 11.1 us, 16.3 with four waves; 128x2048 with 20 8.6 and 6.0)
+    // 1024 lanes where each row has a CU, one whose registers hold one of these workgroups,
+    // or half of one and rows are long (512x65024 24.2 and 28.7, 512x10000 14.0 and 9.1)
     const uint32_t n = cut.splits > 1 ? cut.slice : args.vocab;
     if (n <= 64 * 16 || (n <= kTopSlice && args.rows >= kFill))
         launch(Number<64>{}, Number<16>{});
     else if (n <= kTopSlice)
         launch(Number<kThreads>{}, Number<8>{});
+    else if (cut.splits == 1 && n > kTopBatch &&
+             (args.rows <= kFew || (args.rows <= 2 * kFew && n > kOneGroup)))
+        launch(Number<1024>{}, Number<32>{});
     else
         launch(Number<kThreads>{}, Number<32>{});
     if (cut.splits == 1)

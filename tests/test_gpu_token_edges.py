@@ -83,6 +83,7 @@ def test_rows_that_begin_inside_a_word(zpp, vocab, offset):
 @TYPES
 @pytest.mark.parametrize("rows,vocab,top", [(2, 1000, 64), (2, 2048, 64), (3, 8192, 64),
                                             (520, 30000, 64), (1100, 2048, 64), (2, 70000, 64),
+                                            (5, 33000, 64), (200, 100003, 7), (300, 9000, 9),
                                             (2, 524288, 1), (600, 20000, 2)])
 def test_lists_that_overflow(zpp, rows, vocab, top, dtype):
     """Rows that rise, equal rows, rows of two values, a row masked but for a few, in turn."""
@@ -262,3 +263,16 @@ def test_a_step_of_a_model(zpp):
                                 step=1, weight_decay=decay, **HP)
         assert same(weights[i], one[0][i]) and same(copies[i], copy)
         assert same(moments[0][i], one[1][i]) and same(moments[1][i], one[2][i])
+
+
+def test_more_rows_than_a_launch_takes(zpp):
+    """2^20 workgroups are a launch: the rows past them are a second one's."""
+    rows, vocab = (1 << 20) + 77, 16
+    x, targets = logits(rows, vocab, 0, BF16, 11)
+    lp, lse, h = outputs(rows)
+    ids = torch.empty(rows, 2, dtype=torch.int32, device="cuda")
+    tlp = torch.empty(rows, 2, device="cuda")
+    zpp.log_probs_forward(x, targets, lp, lse, workspace(zpp, rows, vocab, 2), entropies=h,
+                          top_ids=ids, top_log_probs=tlp)
+    check_forward(x, targets, lp, lse, h)
+    assert torch.equal(ids.long(), ref.top_ids(x, 2))
