@@ -1158,9 +1158,7 @@ struct Cut {
     uint32_t splits, slice;
 };
 
-// Rows that leave CUs without one, and the longest row that one workgroup of 1024 takes
-// where there are few: a second launch, to join slices, costs more (1x32003 5.4 us, 7.5 in
-// slices).
+// Rows that leave CUs without one, and the columns of a batch of a workgroup of 1024.
 constexpr size_t kFew = 256;
 constexpr uint32_t kOneGroup = 1024 * 32;
 
@@ -1172,20 +1170,18 @@ uint32_t slices(uint32_t n, uint32_t slice) { return (n + slice - 1) / slice; }
 
 Cut cut_of(size_t rows, uint32_t vocab, uint32_t top) {
     const uint32_t n = vocab;
-    if (rows >= kFill / 2)
+    // One workgroup goes through a batch in less time than a second launch takes (1x32003
+    // 5.4 us, 7.5 in slices; with the best tokens 1x8192 6.3 and 8.9, with 1024 lanes
+    // 1x40000 9.8 and 11.3), and through several where the slices of other rows would wait
+    // for CUs (256x65024 8.7 and 11.1, 256x100000 12.3 and 14.4, 64x100000 10.3 and 7.7; with
+    // the 32 best 128x65024 14.2 and 16.2, 200x131072 23.9 and 30.5, 64x131072 23.1 and 16.6).
+    if (rows >= kFill / 2 || n <= kOneGroup + kOneGroup / 4 || (size_t)n * 48 <= rows * kOneGroup)
         return {1, n};
-    // (the fewer the slices the sooner they are joined, but a slice of 2048 is there sooner
-    // than one of 8192: 1x65024 with the 20 best 10.3 us, 1x262144, whose 128 of 2048 would
-    // have too many keys to join, 11.8)
     const size_t most = kFill / (rows ? rows : 1);
     if (top) {
-        // one workgroup goes through a batch in less time than a second launch takes (1x8192
-        // 6.3 us, 8.9 in slices; with 1024 lanes 1x16384 7.0 and 9.7, 1x40000 9.8 and 11.3),
-        // and through several where the slices of other rows would wait for CUs (128x65024
-        // with the 32 best 14.2 and 16.2, 200x131072 23.9 and 30.5; 16x65024 13.6 and 13.3,
-        // 64x131072 23.1 and 16.6)
-        if (n <= kOneGroup + kOneGroup / 4 || (size_t)n * 48 <= rows * kOneGroup)
-            return {1, n};
+        // the fewer the slices the sooner they are joined, but a slice of 2048 is there sooner
+        // than one of 8192 (1x65024 with the 20 best 10.3 us; 1x262144, whose 128 of 2048 would
+        // have too many keys to join, 11.8)
         const uint32_t keys = kThreads * kJoined / top;  // slices whose keys can be joined
         if (slices(n, kTopSlice) <= most && slices(n, kTopSlice) <= keys)
             return {slices(n, kTopSlice), kTopSlice};
@@ -1194,8 +1190,6 @@ Cut cut_of(size_t rows, uint32_t vocab, uint32_t top) {
         return {slices(n, slice), slice};
     }
     constexpr uint32_t kLeast = kThreads * 8;
-    if (n <= kOneGroup)
-        return {1, n};
     const uint32_t slice = slices(slices(n, (uint32_t)most), kLeast) * kLeast;
     return {slices(n, slice), slice};
 }
@@ -1315,7 +1309,7 @@ void forward_typed(const LogProbsArgs &args, hipStream_t stream) {
         launch(Number<16>{}, Number<32>{});
     else if (args.vocab <= 64 * 32)
         launch(Number<64>{}, Number<32>{});
-    else if (args.vocab > kTopBatch && args.vocab <= kOneGroup && args.rows < kFill / 2)
+    else if (cut.splits == 1 && args.vocab > kTopBatch && args.rows < kFill / 2)
         launch(Number<1024>{}, Number<32>{});
     else
         launch(Number<256>{}, Number<32>{});

@@ -52,6 +52,21 @@ def test_rows_in_registers(zpp, rows, vocab, pad, dtype):
     assert all(same(a, b) for a, b in zip((lp, lse, h), first))
 
 
+@TYPES
+@pytest.mark.parametrize("rows,vocab,pad", [(1, 40000, 0), (100, 65024, 0), (150, 100003, 1),
+                                            (257, 131073, 0)])
+def test_rows_of_one_workgroup(zpp, rows, vocab, pad, dtype):
+    """Few rows, too long for one batch, whole in a workgroup of 1024."""
+    x, targets = logits(rows, vocab, pad, dtype, rows)
+    lp, lse, h = outputs(rows)
+    ws = workspace(zpp, rows, vocab)
+    zpp.log_probs_forward(x, targets, lp, lse, ws, entropies=h)
+    check_forward(x, targets, lp, lse, h)
+    lp2, lse2, _ = outputs(rows)
+    zpp.log_probs_forward(x, targets, lp2, lse2, ws)
+    check_forward(x, targets, lp2, lse2, None)
+
+
 @pytest.mark.parametrize("vocab", [9, 130, 2047, 8200, 33000])
 @pytest.mark.parametrize("offset", [1, 2, 7])
 def test_rows_that_begin_inside_a_word(zpp, vocab, offset):
