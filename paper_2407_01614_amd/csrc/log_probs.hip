@@ -19,6 +19,7 @@
 #include <type_traits>
 
 #include "zpp_act8.h"
+#include "zpp_chunk.h"
 #include "zpp_token.h"
 
 namespace zpp {
@@ -979,8 +980,7 @@ struct TrainArgs {
     const float *dlog_probs, *dentropies;
 };
 
-// Waves of a SIMD to leave registers for: two workgroups a CU where 128 (of 1024 lanes, 64)
-// hold a row's share, so that one's loads and stores run beside the other's arithmetic.
+// Waves of a SIMD to leave registers for: those of a workgroup of 1024, or of two of 512.
 constexpr uint32_t train_waves(uint32_t threads) { return threads > kThreads ? 4 : 1; }
 
 // A row held in registers, C pieces a lane: read once, its sums, then its gradient.
@@ -1282,6 +1282,10 @@ void top_typed(const LogProbsArgs &args, const Cut &cut, hipStream_t stream) {
     });
 }
 
+// Workgroups of a CU that the pass over many long rows is capped at (8192x65024 159.3 us with
+// 5, 163.2 without; 16384x6000, whose rows are one batch, 45.5 and 42.3).
+constexpr int kForwardResident = 5;
+
 template <int TYPE>
 void forward_typed(const LogProbsArgs &args, hipStream_t stream) {
     if (args.vocab < kPer<TYPE>)
@@ -1294,12 +1298,15 @@ void forward_typed(const LogProbsArgs &args, hipStream_t stream) {
         constexpr uint32_t kLanes = decltype(threads)::value, kIn = decltype(batch)::value;
         constexpr uint32_t kGroup = group_of(kLanes);
         for_rows(a, cut.splits, kGroup / kLanes, [&](unsigned grid) {
+            const bool streams = kLanes == kThreads && args.vocab > 2 * kTopBatch &&
+                                 grid >= 8 * kCUs;
+            const size_t lds = streams ? residency_lds(kForwardResident) : 0;
             if (a.entropies)
                 hipLaunchKernelGGL((forward_kernel<TYPE, kLanes, kIn, true>), dim3(grid),
-                                   dim3(kGroup), 0, stream, a);
+                                   dim3(kGroup), lds, stream, a);
             else
                 hipLaunchKernelGGL((forward_kernel<TYPE, kLanes, kIn, false>), dim3(grid),
-                                   dim3(kGroup), 0, stream, a);
+                                   dim3(kGroup), lds, stream, a);
         });
     };
     // as many lanes a row as have work in it (12449x64 in fp32: 16 lanes 5.4 us, 64 10.9)
@@ -1319,21 +1326,28 @@ void forward_typed(const LogProbsArgs &args, hipStream_t stream) {
         });
 }
 
+// Workgroups of a CU that a large gradient's launch in bf16 is capped at, rows at whole words:
+// its two streams are fastest with few of them open (4096x32000 81.9 us with 3, 86.6 with 5 or
+// no cap; 3000x40128 75.3 and 76.2, but 40129 apart 85.1 and 83.2).
+constexpr int kGradResident = 3;
+
 template <int TYPE>
 void backward_typed(const LogProbsArgs &args, hipStream_t stream) {
     if (args.vocab < kPer<TYPE>)
         return launch_short<TYPE, false, true>(args, stream);
     GradArgs a = grad_args(args);
+    const bool words = TYPE == kBf16 && (uintptr_t)args.x.data % 4 == 0 && args.x.stride % 2 == 0;
     const auto launch = [&](auto lanes, auto batch) {
         constexpr uint32_t kLanes = decltype(lanes)::value, kIn = decltype(batch)::value;
         a.per_row = slices(a.vocab, kLanes * kIn);
         for_rows(a, a.per_row, kThreads / kLanes, [&](unsigned grid) {
+            const size_t lds = kLanes == 64 && words ? launch_lds(kGradResident, grid) : 0;
             if (args.dentropies)
                 hipLaunchKernelGGL((backward_kernel<TYPE, kLanes, kIn, true>), dim3(grid),
-                                   dim3(kThreads), 0, stream, a);
+                                   dim3(kThreads), lds, stream, a);
             else
                 hipLaunchKernelGGL((backward_kernel<TYPE, kLanes, kIn, false>), dim3(grid),
-                                   dim3(kThreads), 0, stream, a);
+                                   dim3(kThreads), lds, stream, a);
         });
     };
     if (args.vocab <= 16 * 8)
